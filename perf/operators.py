@@ -174,7 +174,7 @@ def _quantised(x):
     """float32 [..., dims] -> e4m3 values and the scales [..., 1] they are multiples of."""
     amax = torch.where(torch.isfinite(x), x.abs(), 0.0).amax(-1, keepdim=True)
     m, e = torch.frexp(amax)  # amax = m 2^e, m in [0.5, 1): the least 2^e' with amax <= 448 2^e'
-    e = (e - 9 + (m > 0.875)).clamp(min=-126)
+    e = (e - 9 + (m > 0.875)).clamp(min=-117)
     scale = torch.where(amax > 0, torch.ldexp(torch.ones_like(amax), e), 1.0)
     return (x / scale).clamp(-448.0, 448.0).to(torch.float8_e4m3fn), scale
 
