@@ -520,6 +520,168 @@ hisparse_status_t hisparse_sparse_decode_pool(const void* d_pool, int64_t record
                                               void* d_workspace, size_t workspace_bytes,
                                               void* stream);
 
+/* ---- Token records: writing, reading and attending to pools of K and V rows ----------------
+ *
+ * The calls below work on any device memory laid out as records, with no cache handle: a layer's
+ * GPU cache (hisparse_layer_cache), the records handed to hisparse_append or hisparse_stage, or a
+ * pool of pages of the caller's own. A record holds tokens_per_record tokens of one kv head;
+ * hisparse_kv_desc_t says how a token lies in it and where the records are. */
+
+/* What a token is made of: rows K and V. */
+typedef enum {
+  HISPARSE_KV_GROUPED = 0,  /* K 128 dims, V 128 dims: the (128, 128, 128) shape of
+                               hisparse_attn_desc_t */
+  HISPARSE_KV_LATENT = 1    /* K 512 latent dims, V 64 rotary dims: key = both (576), value = the
+                               latent dims; the (576, 512, 0) shape */
+} hisparse_kv_layout_t;
+
+/* How its dims are stored. */
+typedef enum {
+  /* bf16 [tokens_per_record][K | V], the record layout of the sparse decode attention; token t
+   * starts at t * (record_bytes / tokens_per_record). */
+  HISPARSE_KV_BF16 = 0,
+  /* 8 bits, n = tokens_per_record:
+   *   grouped  e4m3 [n][K 128 | V 128], then float32 [n][2], the scales of K and of V;
+   *   latent   e4m3 [n][512], then bf16 [n][64] (the rotary dims keep 16 bits), then float32
+   *            [n], the scale of the latent dims.
+   * A stored value stands for e4m3 * scale. The scale is a power of two per token and part, the
+   * least one with (largest finite magnitude of the part) <= 448 * scale, at least 2^-117, and 1
+   * for a part without a finite nonzero value. Values round to nearest even, infinities become
+   * +-448 * scale, NaN stays NaN. Being powers of two, the scales round nothing: reading back gives
+   * exactly the rounded values, and writing those again gives the same values. */
+  HISPARSE_KV_FP8 = 1
+} hisparse_kv_type_t;
+
+/* Where the records are: record r of kv head h of request q is the record_bytes bytes at
+ *   pool + q * request_stride + h * head_stride + r * record_stride.
+ * Of a layer's GPU cache with B slots: num_records B, record_stride R, head_stride B * R,
+ * request_stride units_per_request * B * R. Of one pool of pages shared by all requests, pages of
+ * all heads [page][head]: record_stride heads * R, head_stride R, request_stride 0. */
+typedef struct {
+  int32_t layout;             /* hisparse_kv_layout_t */
+  int32_t type;               /* hisparse_kv_type_t */
+  int32_t tokens_per_record;  /* 1, 2, 4, ... 4096 */
+  int32_t record_bytes;       /* multiple of 16, at least hisparse_kv_record_bytes, at most 8 MiB;
+                                 for bf16 each token's share of it a multiple of 16 as well */
+  int64_t num_records;        /* 1 .. 2^31 - 1: indices outside [0, num_records) are padding */
+  int64_t record_stride;      /* bytes, multiples of 16, >= 0; record_stride >= record_bytes */
+  int64_t head_stride;
+  int64_t request_stride;
+} hisparse_kv_desc_t;
+
+/* [pure host] The least record_bytes of a layout, type and tokens_per_record; 0 if there is no
+ * such record. */
+int32_t hisparse_kv_record_bytes(int32_t layout, int32_t type, int32_t tokens_per_record);
+
+/* [pure host] Check a record descriptor. */
+hisparse_status_t hisparse_validate_kv(const hisparse_kv_desc_t* kv);
+
+/* [async] Write the rows of num_tokens tokens into their token slots, quantising them if the
+ * records are 8-bit.
+ *   d_k, d_v  bf16, row of token t and head h at t * {k,v}_token_stride + h * dims elements, dims
+ *             128 and 128 (grouped) or 512 and 64 (latent): [tokens][heads][dims] arrays, or
+ *             slices of a wider projection. Any alignment.
+ *   d_slots   int64 [num_tokens]: token t goes to token (slot % tokens_per_record) of record
+ *             (slot / tokens_per_record) of each head. A slot outside the pool (negative, or its
+ *             record >= num_records) is padding: nothing is written. Slots must differ from one
+ *             another; if two tokens name the same one, what it holds afterwards is unspecified
+ *             (other slots are not affected). NULL: token t goes to slot t.
+ * request_stride is not used: with request_stride = m * record_stride, request q's record r is
+ * record q * m + r (num_records is then the bound over all requests).
+ * Nothing but the slots' own rows and scales is written. num_tokens 0 does nothing.
+ * HISPARSE_ERR_INVALID_ARG for a bad descriptor, null pointers, d_pool not a multiple of 16, heads
+ * < 1, num_tokens < 0, negative strides, or head_stride < record_bytes with several heads;
+ * HISPARSE_ERR_UNSUPPORTED if num_tokens * heads is 2^31 or more. */
+hisparse_status_t hisparse_write_tokens(const hisparse_kv_desc_t* kv, int32_t heads,
+                                        int32_t num_tokens, const void* d_k,
+                                        int64_t k_token_stride, const void* d_v,
+                                        int64_t v_token_stride, const int64_t* d_slots,
+                                        void* d_pool, void* stream);
+
+/* [async] The reverse: the rows that num_tokens token slots hold, in bf16 (8-bit values exactly), to
+ * d_k and d_v laid out as above. A slot outside the pool
+ * gives rows of zeros. Slots may repeat. Errors as above; a token stride below heads * dims is
+ * HISPARSE_ERR_INVALID_ARG too where num_tokens > 1 (the rows would overlap). */
+hisparse_status_t hisparse_read_tokens(const hisparse_kv_desc_t* kv, int32_t heads,
+                                       int32_t num_tokens, const void* d_pool,
+                                       const int64_t* d_slots, void* d_k, int64_t k_token_stride,
+                                       void* d_v, int64_t v_token_stride, void* stream);
+
+/* hisparse_chunk_desc_t.flags: new token i of n sees the cached tokens up to its own, number
+ * len - n + i of its request's len. Without it every new token sees all of them (selected
+ * records, which all precede the new tokens). */
+#define HISPARSE_CHUNK_CAUSAL 1
+
+/* Attention of a chunk of new tokens of each request over its records. */
+typedef struct {
+  int32_t num_requests;        /* >= 1 */
+  int32_t kv_heads;            /* kv heads (units) of a request, >= 1; at most 2^20 of all requests */
+  int32_t q_heads;             /* query heads on each kv head: 1 .. 256 */
+  int32_t total_tokens;        /* rows of d_q and d_out: new tokens of all requests, or more */
+  int32_t max_chunk;           /* new tokens of the longest request, >= 1; with d_chunk_start a hint
+                                  that only picks the plan */
+  int32_t max_records;         /* entries of a record table row: the longest request's records;
+                                  max_records * tokens_per_record at most 2^30 */
+  int64_t q_token_stride;      /* elements from one new token's heads to the next one's, >= 0 */
+  int64_t out_token_stride;    /* >= kv_heads * q_heads * d_v */
+  int64_t table_request_stride;  /* entries from one request's table to the next one's, >= 0 */
+  int64_t table_head_stride;     /* and from one kv head's row to the next one's; 0: the heads
+                                    share one row (a block table) */
+  int32_t window;              /* 0, or the newest tokens a new token sees, its own included
+                                  (needs HISPARSE_CHUNK_CAUSAL) */
+  int32_t num_splits;          /* parts the cached tokens are split into, 1 .. 64, merged in a fixed
+                                  order; 0 = chosen from the shape alone */
+  float scale;                 /* softmax scale applied to q.k, > 0, at most 1e6 */
+  int32_t flags;               /* 0 or HISPARSE_CHUNK_CAUSAL */
+} hisparse_chunk_desc_t;
+
+/* [pure host] Check a chunk attention's descriptors. */
+hisparse_status_t hisparse_validate_chunk(const hisparse_kv_desc_t* kv,
+                                          const hisparse_chunk_desc_t* chunk);
+
+/* [pure host] Bytes of device scratch the call needs (0: none, d_workspace may be NULL); 0 too for
+ * invalid descriptors. */
+size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
+                                      const hisparse_chunk_desc_t* chunk);
+
+/* [async] out = softmax(scale * q.k) v over the cached tokens that each new token sees, for every
+ * query head; one call serves decoding requests (chunks of 1), drafted tokens to verify and
+ * chunks of prompts side by side. The new tokens' own rows are in the cache already
+ * (hisparse_write_tokens).
+ *   d_table        int32, row of request q and kv head h at q * table_request_stride + h *
+ *                  table_head_stride: the records that hold the request's cached tokens, in
+ *                  order: cached token j is token (j % tokens_per_record) of record
+ *                  table[j / tokens_per_record]. The tokens of an entry outside [0, num_records)
+ *                  (padding) are not seen.
+ *   d_chunk_start  int32 [num_requests + 1], ascending: request q's new tokens are rows start[q] ..
+ *                  start[q + 1] - 1 of d_q and d_out. Rows outside every chunk (a batch padded to
+ *                  a fixed size) are neither read nor written. Values are held to [0,
+ *                  total_tokens]. NULL: every request has max_chunk new tokens, request q's from
+ *                  row q * max_chunk; total_tokens >= num_requests * max_chunk.
+ *   d_kv_len       int32 [num_requests]: cached tokens of each request, its new ones included; held
+ *                  to [0, max_records * tokens_per_record]. NULL: that many everywhere. A request
+ *                  with fewer cached than new tokens has new tokens that see nothing.
+ *   d_q            bf16, token i's heads at i * q_token_stride, [kv_heads * q_heads][d_qk]: query
+ *                  head e on kv head e / q_heads; d_qk 128 (grouped) or 576 (latent). Any
+ *                  alignment.
+ *   d_out          bf16 likewise with out_token_stride and d_v 128 or 512.
+ *   d_lse          float32 [total_tokens][kv_heads * q_heads] or NULL: the natural logarithm of the
+ *                  softmax's sum, to join results over parts of a cache. May be NULL.
+ *   d_workspace    at least hisparse_chunk_workspace_bytes bytes, a multiple of 16; calls that may
+ *                  overlap (other streams, graphs replayed side by side) need one each.
+ * A new token that sees no cached token gives zeros and an lse of -inf. Scores, their maximum and
+ * sums are kept in fp32; softmax weights are rounded to bf16 for the product with V. Rows that are
+ * not seen (padding, later tokens, tokens before the window, page ends) have no influence, whatever
+ * they hold, infinities and NaN included. Results do not depend on where records lie.
+ * HISPARSE_ERR_INVALID_ARG for bad descriptors, null or misaligned pointers, or a workspace too
+ * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more. */
+hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
+                                           const hisparse_chunk_desc_t* chunk, const void* d_pool,
+                                           const int32_t* d_table, const int32_t* d_chunk_start,
+                                           const int32_t* d_kv_len, const void* d_q, void* d_out,
+                                           float* d_lse, void* d_workspace,
+                                           size_t workspace_bytes, void* stream);
+
 /* [sync] Copy an anchor layer's resolve state into host buffers (any may be NULL):
  * slot_pos int32 [units][B], slot_ts uint32 [units][B], page_table int32 [units][L],
  * order int32 [units][B] (slots by ascending (timestamp, slot)), clock uint32 [units]. */

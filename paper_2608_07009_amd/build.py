@@ -15,7 +15,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libhisparse.so")
-SOURCES = ["api.hip", "resolve.hip", "attention.hip"]
+SOURCES = ["api.hip", "resolve.hip", "attention.hip", "tokens.hip", "chunk_attention.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions stay off: only plain fp32 VALU code is generated.

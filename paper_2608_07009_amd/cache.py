@@ -69,6 +69,14 @@ class HiSparseCache:
     def layer_cache(self, layer: int) -> tuple[int, int]:
         return hs.hisparse_layer_cache(self.handle, layer)
 
+    def kv_desc(self, layout: int, type: int, tokens_per_record: int,
+                host_pool: bool = False) -> hs.KvDesc:
+        """The token records of any layer's GPU cache (its address: layer_cache(layer)[0]), or of
+        a buffer laid out like a layer's host pool, [units][L][R]."""
+        n = self.L if host_pool else self.B
+        return hs.KvDesc(layout, type, tokens_per_record, self.R, n, self.R, n * self.R,
+                         self.desc.units_per_request * n * self.R)
+
     def read_state(self, layer: int, page_table: bool = True) -> dict:
         U, B, L = self.units, self.B, self.L
         st = dict(slot_pos=np.empty((U, B), np.int32), slot_ts=np.empty((U, B), np.uint32),

@@ -34,6 +34,12 @@ HISPARSE_ATTN_BESIDE_FETCH = 2
 HISPARSE_ATTN_CARRIES_REPLAY = 4
 HISPARSE_NOALLOC_SCRATCH_BYTES = 64 << 20
 
+HISPARSE_KV_GROUPED = 0
+HISPARSE_KV_LATENT = 1
+HISPARSE_KV_BF16 = 0
+HISPARSE_KV_FP8 = 1
+HISPARSE_CHUNK_CAUSAL = 1
+
 HISPARSE_RESOLVE_PHASE_SLOTS = 16
 HISPARSE_RESOLVE_PHASE_UNITS = 64
 
@@ -55,6 +61,9 @@ EXPORTED = (
     "hisparse_sparse_decode_prefetch", "hisparse_sparse_decode_prefetch_part",
     "hisparse_attention_merge_prefetch",
     "hisparse_sparse_decode_pool", "hisparse_sparse_decode_noalloc",
+    "hisparse_kv_record_bytes", "hisparse_validate_kv", "hisparse_write_tokens",
+    "hisparse_read_tokens", "hisparse_validate_chunk", "hisparse_chunk_workspace_bytes",
+    "hisparse_chunk_attention",
     "hisparse_read_state", "hisparse_read_plan", "hisparse_check_errors",
     "hisparse_debug_resolve_phases",
 )
@@ -74,6 +83,23 @@ class AttnDesc(ctypes.Structure):
                 ("v_offset", ctypes.c_int32), ("tokens_per_record", ctypes.c_int32),
                 ("num_splits", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("flags", ctypes.c_int32)]
+
+
+class KvDesc(ctypes.Structure):
+    _fields_ = [("layout", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("tokens_per_record", ctypes.c_int32), ("record_bytes", ctypes.c_int32),
+                ("num_records", ctypes.c_int64), ("record_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("request_stride", ctypes.c_int64)]
+
+
+class ChunkDesc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("q_heads", ctypes.c_int32), ("total_tokens", ctypes.c_int32),
+                ("max_chunk", ctypes.c_int32), ("max_records", ctypes.c_int32),
+                ("q_token_stride", ctypes.c_int64), ("out_token_stride", ctypes.c_int64),
+                ("table_request_stride", ctypes.c_int64), ("table_head_stride", ctypes.c_int64),
+                ("window", ctypes.c_int32), ("num_splits", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("flags", ctypes.c_int32)]
 
 
 class HisparseError(RuntimeError):
@@ -147,6 +173,19 @@ def lib() -> ctypes.CDLL:
             "hisparse_sparse_decode_pool": (_I32, [_V, ctypes.c_int64, _I32, _I32, _I32, _V, _V,
                                                    _V, ctypes.POINTER(AttnDesc), _V,
                                                    ctypes.c_size_t, _V]),
+            "hisparse_kv_record_bytes": (_I32, [_I32, _I32, _I32]),
+            "hisparse_validate_kv": (_I32, [ctypes.POINTER(KvDesc)]),
+            "hisparse_write_tokens": (_I32, [ctypes.POINTER(KvDesc), _I32, _I32, _V,
+                                             ctypes.c_int64, _V, ctypes.c_int64, _V, _V, _V]),
+            "hisparse_read_tokens": (_I32, [ctypes.POINTER(KvDesc), _I32, _I32, _V, _V, _V,
+                                            ctypes.c_int64, _V, ctypes.c_int64, _V]),
+            "hisparse_validate_chunk": (_I32, [ctypes.POINTER(KvDesc),
+                                               ctypes.POINTER(ChunkDesc)]),
+            "hisparse_chunk_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(KvDesc),
+                                                                 ctypes.POINTER(ChunkDesc)]),
+            "hisparse_chunk_attention": (_I32, [ctypes.POINTER(KvDesc),
+                                                ctypes.POINTER(ChunkDesc), _V, _V, _V, _V, _V,
+                                                _V, _V, _V, ctypes.c_size_t, _V]),
             "hisparse_read_state": (_I32, [_V, _I32, _V, _V, _V, _V, _V]),
             "hisparse_read_plan": (_I32, [_V, _I32, _V, _V]),
             "hisparse_check_errors": (_I32, [_V, _V]),
@@ -395,6 +434,48 @@ def hisparse_sparse_decode_pool(d_pool, records_per_unit: int, record_bytes: int
                                              top_k, _p(d_q), _p(d_idx), _p(d_out),
                                              ctypes.byref(attn), _p(d_workspace),
                                              workspace_bytes, _s(stream)))
+
+
+def hisparse_kv_record_bytes(layout: int, type: int, tokens_per_record: int) -> int:
+    return lib().hisparse_kv_record_bytes(layout, type, tokens_per_record)
+
+
+def hisparse_validate_kv(kv: KvDesc) -> int:
+    return lib().hisparse_validate_kv(ctypes.byref(kv))
+
+
+def hisparse_write_tokens(kv: KvDesc, heads: int, num_tokens: int, d_k, k_token_stride: int, d_v,
+                          v_token_stride: int, d_slots, d_pool, stream=None) -> None:
+    _check("hisparse_write_tokens",
+           lib().hisparse_write_tokens(ctypes.byref(kv), heads, num_tokens, _p(d_k),
+                                       k_token_stride, _p(d_v), v_token_stride, _p(d_slots),
+                                       _p(d_pool), _s(stream)))
+
+
+def hisparse_read_tokens(kv: KvDesc, heads: int, num_tokens: int, d_pool, d_slots, d_k,
+                         k_token_stride: int, d_v, v_token_stride: int, stream=None) -> None:
+    _check("hisparse_read_tokens",
+           lib().hisparse_read_tokens(ctypes.byref(kv), heads, num_tokens, _p(d_pool),
+                                      _p(d_slots), _p(d_k), k_token_stride, _p(d_v),
+                                      v_token_stride, _s(stream)))
+
+
+def hisparse_validate_chunk(kv: KvDesc, chunk: ChunkDesc) -> int:
+    return lib().hisparse_validate_chunk(ctypes.byref(kv), ctypes.byref(chunk))
+
+
+def hisparse_chunk_workspace_bytes(kv: KvDesc, chunk: ChunkDesc) -> int:
+    return lib().hisparse_chunk_workspace_bytes(ctypes.byref(kv), ctypes.byref(chunk))
+
+
+def hisparse_chunk_attention(kv: KvDesc, chunk: ChunkDesc, d_pool, d_table, d_chunk_start,
+                             d_kv_len, d_q, d_out, d_lse, d_workspace, workspace_bytes: int,
+                             stream=None) -> None:
+    _check("hisparse_chunk_attention",
+           lib().hisparse_chunk_attention(ctypes.byref(kv), ctypes.byref(chunk), _p(d_pool),
+                                          _p(d_table), _p(d_chunk_start), _p(d_kv_len), _p(d_q),
+                                          _p(d_out), _p(d_lse), _p(d_workspace),
+                                          workspace_bytes, _s(stream)))
 
 
 def hisparse_read_state(cache: int, layer: int, slot_pos=None, slot_ts=None, page_table=None,
