@@ -7,14 +7,24 @@
 //
 // One wave per (new token, query head); its lanes share the dims, tokens one after the other with
 // the running maximum and sum in fp32.
-#include <math.h>
-
 #include <algorithm>
 
+#include "attention_device.h"
+#include "fetch_device.h"
 #include "tokens.h"
 
 namespace hisparse {
 namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+// Exponentials are taken against a running reference that moves only when a row's scores outgrow it
+// by more than this (powers of two): exact softmax arithmetic with another reference point.
+constexpr float kSlack = 8.0f;
+// Up to this reference a weight comes from one fused multiply-add; beyond it the product is rounded
+// first, as the reference was, or a weight could leave the float range.
+constexpr float kFused = 16777216.f;
+constexpr int kMaxSplits = 128;  // parts of one request's cached tokens
+constexpr int kMinSplitTokens = 256;
 
 struct ChunkArgs {
   const uint8_t* pool;
@@ -22,15 +32,661 @@ struct ChunkArgs {
   const uint16_t* q;
   uint16_t* out;
   float* lse;
+  float* part_o;    // [part rows][d_v]: unnormalised outputs of splits
+  float2* part_ml;  // [part rows] (reference in log2 units, sum)
   int64_t record_stride, head_stride, request_stride;
   int64_t q_stride, out_stride, table_request_stride, table_head_stride;
-  int64_t num_records;
+  int64_t num_records, head_part_rows;
   KvLayout l;
   int32_t requests, kv_heads, g, total, max_chunk, max_tokens, window, causal;
+  int32_t target;               // workgroups that splitting aims at (0: no splits)
+  int32_t num_splits;           // asked for (0: chosen)
+  int32_t uni_tiles, uni_splits;  // of every request, where they are alike (start and kv_len null)
+  FastDiv div_g;
   float scale_log2;
 };
 
-__device__ inline float bf16_to_f32(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
+// ---- which piece of the call a workgroup does ------------------------------------------------
+
+// Rows (new token, query head of the kv head) of one workgroup: 32 per row wave, as many row waves as
+// the request's rows fill, up to eight; the other waves of the workgroup take other tokens.
+__device__ __host__ inline int row_waves(int rows) {
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+}
+
+struct Request {
+  int begin, n, len;
+};
+__device__ __forceinline__ Request request_of(const ChunkArgs& a, int r) {
+  Request q;
+  if (a.start) {
+    q.begin = min(max(a.start[r], 0), a.total);
+    q.n = min(min(max(a.start[r + 1], q.begin), a.total) - q.begin, a.max_chunk);
+  } else {
+    q.begin = r * a.max_chunk;
+    q.n = a.max_chunk;
+  }
+  q.len = a.kv_len ? min(max(a.kv_len[r], 0), a.max_tokens) : a.max_tokens;
+  return q;
+}
+
+struct Work {
+  Request q;
+  int req, waves, tile, split, splits;
+  int64_t part_row;  // first partial-result row of the tile's split 0
+};
+
+__device__ inline float wave_sum(float x) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
+  return x;
+}
+__device__ inline int wave_prefix(int x) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d, 64);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// Item `item` of a kv head's work: MERGE: row tiles, else (row tile, split)s, request by request,
+// each request's tiles from the last (which see most) to the first. Splits follow from the
+// requests' lengths alone: cached tokens in parts of W / target, W the tokens of all row tiles.
+// False if there are fewer items. Wave-uniform.
+template <bool MERGE>
+__device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w) {
+  const int lane = threadIdx.x & 63;
+  if (!a.start && !a.kv_len) {
+    const int bm = 32 * row_waves(a.max_chunk * a.g);
+    const int per = MERGE ? a.uni_tiles : a.uni_tiles * a.uni_splits;
+    w.req = item / per;
+    if (w.req >= a.requests) return false;
+    w.q = request_of(a, w.req);
+    const int x = item - w.req * per;
+    w.waves = bm / 32;
+    w.splits = a.uni_splits;
+    w.tile = MERGE ? x : x / w.splits;
+    w.split = MERGE ? 0 : x - w.tile * w.splits;
+    w.part_row = (int64_t)(w.req * a.uni_tiles + w.tile) * w.splits * bm;
+    w.tile = a.uni_tiles - 1 - w.tile;
+    return true;
+  }
+  auto tiles_of = [&](const Request& q, int& waves) {
+    const int rows = q.n * a.g;
+    waves = row_waves(rows);
+    return (rows + 32 * waves - 1) / (32 * waves);
+  };
+  auto span_of = [&](const Request& q) {
+    return a.window ? min(q.len, a.window + q.n - 1) : q.len;
+  };
+  int part = 0x7fffffff;  // tokens of a split
+  if (a.target && !a.num_splits) {
+    float sum = 0.f;  // 64-token blocks (a rounding of it moves the parts, nothing else)
+    for (int base = 0; base < a.requests; base += 64) {
+      const int r = base + lane;
+      float x = 0.f;
+      if (r < a.requests) {
+        const Request q = request_of(a, r);
+        int waves;
+        x = (float)tiles_of(q, waves) * (float)((span_of(q) + 63) >> 6);
+      }
+      sum += wave_sum(x);
+    }
+    // a little more than their share, so that there are no more items than the host allows for
+    const float p = sum * (float)a.kv_heads * (64.01f / (float)a.target) + 1.f;
+    part = (int)fminf(fmaxf(p, (float)kMinSplitTokens), 1.5e9f);
+  }
+  int items = 0;
+  int64_t rows = 0;
+  for (int base = 0; base < a.requests; base += 64) {
+    const int r = base + lane;
+    Request q{0, 0, 0};
+    int waves = 1, tiles = 0, splits = 1;
+    if (r < a.requests) {
+      q = request_of(a, r);
+      tiles = tiles_of(q, waves);
+      const int span = span_of(q);
+      if (a.num_splits) splits = min(a.num_splits, max(1, (span + 63) >> 6));
+      else if (a.target) splits = min(max((span + part - 1) / part, 1), kMaxSplits);
+    }
+    const int mine = MERGE ? tiles : tiles * splits, mine_rows = tiles * splits * waves;
+    const int pi = wave_prefix(mine), pr = wave_prefix(mine_rows);
+    const uint64_t hit = __ballot(items + pi > item);
+    if (hit) {
+      const int src = __builtin_ctzll(hit);
+      auto get = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
+      w.req = base + src;
+      w.q = Request{get(q.begin), get(q.n), get(q.len)};
+      w.waves = get(waves);
+      w.splits = get(splits);
+      const int x = item - items - get(pi - mine);
+      w.tile = MERGE ? x : x / w.splits;
+      w.split = MERGE ? 0 : x - w.tile * w.splits;
+      w.part_row = (rows + get(pr - mine_rows) + (int64_t)w.tile * w.splits * w.waves) * 32;
+      w.tile = get(tiles) - 1 - w.tile;
+      return true;
+    }
+    items += __builtin_amdgcn_readlane(pi, 63);
+    rows += __builtin_amdgcn_readlane(pr, 63);
+  }
+  return false;
+}
+
+// ---- grouped-query records -------------------------------------------------------------------
+//
+// A workgroup is eight waves, RW row waves of 32 rows each in TG = 8 / RW token groups; a group's
+// waves share tiles of CT tokens (K | V in bf16) in LDS, staged by way of registers: the next
+// tile's loads are in flight while one is computed on, 8-bit rows are widened on their way to LDS
+// (exact: the scale is a power of two), and tokens that nobody may see are stored as zeros.
+//   S^T[token][row] = K[token][:] . Q^T[:][row]    v_mfma_f32_32x32x16_bf16, Q in registers
+//   O^T[dim][row]  += V^T[dim][token] P^T[token][row]   the same, V by LDS transpose reads
+// A lane holds one row: 16 of a tile's 32 scores (lane ^ 32 holds the others), which in the token
+// order of mla_row are its P operands, and the row's reference, sum and limits are one register
+// each.
+
+using GTile = Tile<32>;  // 32 tokens of 32 pieces: K 0..15, V 16..31
+
+// What a workgroup's rows see, and where its tokens are.
+struct View {
+  const int32_t* table;
+  const uint8_t* pool;
+  int t0, t1;          // this split's tokens [t0, t1)
+  int hi_min, lo_max;  // tokens in [lo_max, hi_min) are seen by every row
+};
+
+// LDS of a workgroup, whichever its path: tiles, bad-token marks, the groups' (max, sum) pairs.
+constexpr int kGroupedMarks = 8 * GTile::BYTES;
+constexpr int kGroupedMl = kGroupedMarks + 8 * 2 * 65 * 4;
+constexpr int kGroupedLds = kGroupedMl + 8 * 32 * 8;
+
+template <bool FP8, int RW, int TG, int CT>
+struct Grouped {
+  static constexpr int NB = RW == 1 ? 1 : 2;  // tile buffers (one wave alone needs one)
+  static constexpr int NS = CT / 32;
+  static constexpr int TILE = NS * GTile::BYTES;
+  static constexpr int RGW = CT / 8 / RW;  // groups of eight rows that a wave stages
+  static constexpr int NLD = FP8 ? 2 : 4;  // 16-byte loads of a lane's row
+  static constexpr int LDS_TILES = TG * NB * TILE;
+  static_assert(LDS_TILES <= kGroupedMarks && TG * NB * (CT + 1) * 4 <= kGroupedMl - kGroupedMarks,
+                "LDS");
+  static_assert(RW * TG == 8 && CT % (8 * RW) == 0 && CT <= 64, "shape");
+
+  struct Staged {
+    u32x4 x[RGW][NLD];
+    f32x2 sc[RGW];
+  };
+
+  // 8 e4m3 values times the power of two s, in bf16.
+  static __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float s) {
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true));
+    return r;
+  }
+  // x with its non-finite bf16 values cleared; true if there was one.
+  static __device__ __forceinline__ bool clear_bad(u32x4& x) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+      bad |= lo | hi;
+      x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    }
+    return bad;
+  }
+
+  static __device__ __forceinline__ void run(const ChunkArgs& a, const Work& w, int h,
+                                             uint8_t* s_mem) {
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int hg = wave % RW, tg = wave / RW;
+    uint8_t* s_tiles = s_mem + tg * NB * TILE;
+    // tokens whose V is not finite in a tile that not every row sees: the tile's number + 1
+    int* s_bad = reinterpret_cast<int*>(s_mem + kGroupedMarks) + tg * NB * (CT + 1);
+
+    // ---- rows ----
+    const int n_rows = w.q.n * a.g, row0 = w.tile * 32 * RW;
+    auto hi_of = [&](int tok) {
+      return a.causal ? min(w.q.len, w.q.len - w.q.n + tok + 1) : w.q.len;
+    };
+    auto lo_of = [&](int tok) {
+      return a.window ? max(0, w.q.len - w.q.n + tok + 1 - a.window) : 0;
+    };
+    const int tok_first = (int)fastdiv(row0, a.div_g);
+    const int tok_last = (int)fastdiv(min(n_rows, row0 + 32 * RW) - 1, a.div_g);
+    const int lo_wg = lo_of(tok_first), hi_wg = max(hi_of(tok_last), 0);
+    View v;
+    v.hi_min = hi_of(tok_first);
+    v.lo_max = lo_of(tok_last);
+    v.table = a.table + w.req * a.table_request_stride + h * a.table_head_stride;
+    v.pool = a.pool + w.req * a.request_stride + h * a.head_stride;
+    {
+      const int base = lo_wg & ~63, n_blocks = max(0, hi_wg - base + 63) >> 6;
+      const int c = (n_blocks + w.splits - 1) / w.splits;
+      v.t0 = base + w.split * c * 64;
+      v.t1 = min(hi_wg, v.t0 + c * 64);
+    }
+    // this lane's row; one past the end stands in for the last
+    const int row_w = row0 + 32 * hg;
+    const int row = min(row_w + col, n_rows - 1);
+    const bool wave_rows = row_w < n_rows;
+    const int tok = (int)fastdiv(row, a.div_g), head = h * a.g + row - tok * a.g;
+    const int row_hi = hi_of(tok), row_lo = lo_of(tok);
+    // of the wave: tokens in [w_lo, w_hi) are seen by all its rows, none from w_end on by any
+    const int w_hi = __builtin_amdgcn_readfirstlane(
+        hi_of((int)fastdiv(min(row_w, n_rows - 1), a.div_g)));
+    const int w_last = (int)fastdiv(min(row_w + 31, n_rows - 1), a.div_g);
+    const int w_lo = __builtin_amdgcn_readfirstlane(lo_of(w_last));
+    const int w_end = __builtin_amdgcn_readfirstlane(hi_of(w_last));
+
+    // ---- staging ----
+    const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
+    auto tile_base = [&](int it) { return v.t0 + (it * TG + tg) * CT; };
+    int32_t e[RGW], ev;  // table entries of the tile to load next, and of its token `lane`
+    auto entry = [&](int t) {
+      return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1;
+    };
+    auto load_entries = [&](int it) {
+      const int base = tile_base(it);
+#pragma unroll
+      for (int i = 0; i < RGW; ++i) e[i] = entry(base + 8 * (hg * RGW + i) + (lane >> 3));
+      ev = entry(base + (lane & (CT - 1)));
+    };
+    Staged st;
+    uint64_t vmask = 0;  // of the staged tile: bit t, token t exists
+    auto ok_entry = [&](int32_t r) { return r >= 0 && r < a.num_records; };
+    auto issue = [&](int it) {
+      const int base = tile_base(it);
+      vmask = __ballot(ok_entry(ev));
+#pragma unroll
+      for (int i = 0; i < RGW; ++i) {
+        const int t = base + 8 * (hg * RGW + i) + (lane >> 3);
+        const int in = t & ((1 << a.l.tpr_shift) - 1);
+        const uint8_t* rec = v.pool + (int64_t)e[i] * a.record_stride;
+        const uint8_t* src = rec + in * a.l.row_bytes + 16 * (lane & 7);
+        if (ok_entry(e[i])) {
+#pragma unroll
+          for (int x = 0; x < NLD; ++x)
+            st.x[i][x] = *reinterpret_cast<const u32x4*>(src + 128 * x);
+          if constexpr (FP8)
+            st.sc[i] = *reinterpret_cast<const f32x2*>(rec + a.l.scale_offset + 8 * in);
+        } else {
+#pragma unroll
+          for (int x = 0; x < NLD; ++x) st.x[i][x] = u32x4{};
+          if constexpr (FP8) st.sc[i] = f32x2{1.f, 1.f};
+        }
+      }
+    };
+    auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
+    auto store = [&](int it) {
+      uint8_t* tile = s_tiles + (it % NB) * TILE;
+      const bool part = partial(tile_base(it));
+#pragma unroll
+      for (int i = 0; i < RGW; ++i) {
+        const int r = 8 * (hg * RGW + i) + (lane >> 3);
+        uint8_t* dst = tile + (r >> 5) * GTile::BYTES + GTile::row(r & 31);
+        const int sw = tile_swizzle(r);
+        bool bad = false;
+        if constexpr (FP8) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {  // K, V
+            u32x4 p0 = widen(st.x[i][x][0], st.x[i][x][1], st.sc[i][x]);
+            u32x4 p1 = widen(st.x[i][x][2], st.x[i][x][3], st.sc[i][x]);
+            if (x == 1 && part) {
+              bad |= clear_bad(p0);
+              bad |= clear_bad(p1);
+            }
+            uint8_t* seg = dst + (2 * x + ((lane & 7) >> 2)) * 1024;
+            const int p = 2 * (lane & 3);
+            *reinterpret_cast<u32x4*>(seg + ((p ^ sw) << 4)) = p0;
+            *reinterpret_cast<u32x4*>(seg + (((p + 1) ^ sw) << 4)) = p1;
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            u32x4 p = st.x[i][x];
+            if (x >= 2 && part) bad |= clear_bad(p);
+            *reinterpret_cast<u32x4*>(dst + x * 1024 + (((lane & 7) ^ sw) << 4)) = p;
+          }
+        }
+        if (part && bad) {
+          s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
+          s_bad[(it % NB) * (CT + 1)] = it + 1;
+        }
+      }
+    };
+
+    load_entries(0);
+    for (int i = lane + 64 * hg; i < NB * (CT + 1); i += 64 * RW) s_bad[i] = 0;
+    // Q^T operand: this lane's row, dims 16 kk + 8 half .. +7
+    bf16x8_t qreg[8];
+    {
+      typedef u32x4 any_u32x4 __attribute__((aligned(2)));
+      const uint16_t* q = a.q + (int64_t)(w.q.begin + tok) * a.q_stride + (int64_t)head * 128;
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        qreg[kk] = __builtin_bit_cast(
+            bf16x8_t, (u32x4)*reinterpret_cast<const any_u32x4*>(q + 16 * kk + 8 * half));
+    }
+    f32x16 o[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) o[n] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+    uint64_t mask_now = 0;
+    if (n_it > 0) {
+      issue(0);
+      load_entries(1);
+      if (RW > 1 || TG > 1) __syncthreads();  // s_bad is clear
+      store(0);
+      mask_now = vmask;
+    }
+
+    for (int it = 0; it < n_it; ++it) {
+      if constexpr (RW > 1) __syncthreads();  // tile `it` is stored, tile it - 1 read by all
+      else __builtin_amdgcn_wave_barrier();
+      if (it + 1 < n_it) {
+        issue(it + 1);
+        load_entries(it + 2);
+      }
+      const int base = tile_base(it);
+      if (wave_rows && base < w_end) {
+        const uint8_t* tile = s_tiles + (it % NB) * TILE;
+        f32x16 s[NS];
+        const int kr = mla_row(col), ksw = tile_swizzle(kr);
+#pragma unroll
+        for (int j = 0; j < NS; ++j) {
+          s[j] = f32x16{};
+          const uint8_t* krow = tile + j * GTile::BYTES + GTile::row(kr);
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) {
+            const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
+                krow + (kk / 4) * 1024 + ((((2 * kk + half) & 7) ^ ksw) << 4));
+            s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qreg[kk], s[j], 0, 0, 0);
+          }
+        }
+        constexpr uint64_t kFull = CT == 64 ? ~0ull : 0xffffffffull;
+        if (base + CT > w_hi || base < w_lo || (mask_now & kFull) != kFull) {
+          const int hi = row_hi - base - half, lo = row_lo - base - half;
+          const uint64_t m = mask_now >> half;
+#pragma unroll
+          for (int j = 0; j < NS; ++j)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const int t = 32 * j + 16 * (i >> 3) + 4 * (i & 3) + 2 * ((i >> 2) & 1);
+              const bool seen = t < hi && t >= lo && ((m >> t) & 1);
+              s[j][i] = seen ? s[j][i] : -INFINITY;
+            }
+        }
+        float cmax = s[0][0];
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) cmax = fmaxf(cmax, s[j][i]);
+        cmax *= a.scale_log2;
+        if (__ballot(cmax > m_run + kSlack || (m_run == -INFINITY && cmax > -INFINITY))) {
+          const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
+          const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_run *= alpha;
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
+        }
+        const float ref = m_run == -INFINITY ? 0.f : m_run;
+        const bool wide = __ballot(!(__builtin_fabsf(ref) <= kFused)) != 0;
+        uint32_t pw[NS][8];
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+          for (int i = 0; i < 16; i += 2) {
+            float x0 = __builtin_fmaf(s[j][i], a.scale_log2, -ref);
+            float x1 = __builtin_fmaf(s[j][i + 1], a.scale_log2, -ref);
+            if (wide) {
+              x0 = over_reference(s[j][i], a.scale_log2, ref);
+              x1 = over_reference(s[j][i + 1], a.scale_log2, ref);
+            }
+            const f32x2 p = {__builtin_amdgcn_exp2f(x0), __builtin_amdgcn_exp2f(x1)};
+            sum[i & 2] += p[0];
+            sum[(i & 2) + 1] += p[1];
+            pw[j][i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
+          }
+        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        // V^T operand by transpose reads: in each 16-lane group lane 4s + q addresses row 16 kb +
+        // 4s + half (+ 2 for the second read), dims 32 n + 16 (col >> 4) + 4q .. +3; lane t of the
+        // group then holds those rows of dim 32 n + 16 (col >> 4) + t, in P's token order.
+        const int vr = 4 * ((lane & 15) >> 2) + half;
+        const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int j = 0; j < NS; ++j)
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb) {
+            const bf16x8_t p = __builtin_bit_cast(
+                bf16x8_t, u32x4{pw[j][4 * kb], pw[j][4 * kb + 1], pw[j][4 * kb + 2],
+                                pw[j][4 * kb + 3]});
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+              auto vread = [&](int y) {
+                const int r = vr + 2 * y;  // + 16 kb: two row groups further
+                const uint8_t* at = tile + j * GTile::BYTES + GTile::row(r) + kb * 2 * 4096 +
+                                    (2 + n / 2) * 1024 +
+                                    (((vp + 4 * (n & 1)) ^ tile_swizzle(r)) << 4) + 8 * (lane & 1);
+                return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (lds_v4i16*)const_cast<uint8_t*>(at));
+              };
+              const bf16x8_t vt = __builtin_bit_cast(
+                  bf16x8_t,
+                  __builtin_shufflevector(vread(0), vread(1), 0, 1, 2, 3, 4, 5, 6, 7));
+              o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p, o[n], 0, 0, 0);
+            }
+          }
+        // Infinities and NaN in V of a tile that only some rows see were stored as zeros (zero
+        // weights would have made NaN of them): they go to the rows that see them here.
+        if (partial(base) &&
+            __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
+          for (int t = 0; t < CT; ++t) {
+            if (s_bad[(it % NB) * (CT + 1) + 1 + t] != it + 1) continue;
+            const int tk = base + t;
+            if (tk >= row_hi || tk < row_lo) continue;
+            const uint8_t* rec =
+                v.pool + (int64_t)v.table[tk >> a.l.tpr_shift] * a.record_stride;
+            const int in = tk & ((1 << a.l.tpr_shift) - 1);
+            const uint8_t* vrow = rec + (int64_t)in * a.l.row_bytes + (FP8 ? 128 : 256);
+            float sc = 1.f;
+            if constexpr (FP8)
+              sc = reinterpret_cast<const float*>(rec + a.l.scale_offset)[2 * in + 1];
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const int d = 32 * n + 8 * (i >> 2) + 4 * half + (i & 3);
+                float x;
+                if constexpr (FP8) x = __builtin_amdgcn_cvt_f32_fp8(vrow[d], 0) * sc;
+                else x = bf16_to_f32(reinterpret_cast<const uint16_t*>(vrow)[d]);
+                if (!(__builtin_fabsf(x) <= 3.3895314e38f)) o[n][i] += x;
+              }
+          }
+        }
+      }
+      if (it + 1 < n_it) {
+        if constexpr (RW == 1) __builtin_amdgcn_wave_barrier();
+        store(it + 1);
+        mask_now = vmask;
+      }
+    }
+    l_run += __shfl_xor(l_run, 32, 64);
+
+    // ---- the token groups' results merged through LDS, in group order ----
+    float m = m_run, l = l_run;
+    if constexpr (TG > 1) {
+      float2* s_ml = reinterpret_cast<float2*>(s_mem + kGroupedMl);
+      __syncthreads();
+      f32x4* s_o = reinterpret_cast<f32x4*>(s_mem);  // [TG][RW][16 quads][64 lanes]
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          s_o[(wave * 16 + n * 4 + x) * 64 + lane] =
+              f32x4{o[n][4 * x], o[n][4 * x + 1], o[n][4 * x + 2], o[n][4 * x + 3]};
+      if (half == 0) s_ml[wave * 32 + col] = make_float2(m_run, l_run);
+      __syncthreads();
+      m = -INFINITY;
+      float2 ml[TG];
+#pragma unroll
+      for (int t = 0; t < TG; ++t) {
+        ml[t] = s_ml[(t * RW + hg) * 32 + col];
+        m = fmaxf(m, ml[t].x);
+      }
+      l = 0.f;
+      float wt[TG];
+#pragma unroll
+      for (int t = 0; t < TG; ++t) {
+        wt[t] = ml[t].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[t].x - m);
+        l += ml[t].y * wt[t];
+      }
+      // this wave finishes 16 / TG quads of its rows
+      constexpr int NQ = 16 / TG;
+      f32x4 r[NQ];
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        r[x] = f32x4{};
+#pragma unroll
+        for (int t = 0; t < TG; ++t)
+          r[x] += s_o[((t * RW + hg) * 16 + tg * NQ + x) * 64 + lane] * wt[t];
+      }
+      if (row_w + col < n_rows)
+        finish<NQ>(a, w, h, r, tg * NQ, tok, head, hg * 32 + col, m, l, half);
+    } else {
+      f32x4 r[16];
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          r[4 * n + x] = f32x4{o[n][4 * x], o[n][4 * x + 1], o[n][4 * x + 2], o[n][4 * x + 3]};
+      if (row_w + col < n_rows) finish<16>(a, w, h, r, 0, tok, head, hg * 32 + col, m, l, half);
+    }
+  }
+
+  // NQ quads of a row's result from quad q0 on (quad 4n + x: dims 32n + 8x + 4 half .. +3).
+  template <int NQ>
+  static __device__ __forceinline__ void finish(const ChunkArgs& a, const Work& w, int h,
+                                                const f32x4* r, int q0, int tok, int head,
+                                                int tile_row, float m, float l, int half) {
+    const bool first = q0 == 0 && half == 0;
+    if (w.splits > 1) {
+      const int64_t pr = h * a.head_part_rows + w.part_row + w.split * 32 * RW + tile_row;
+#pragma unroll
+      for (int x = 0; x < NQ; ++x) {
+        const int q = q0 + x;
+        *reinterpret_cast<f32x4*>(a.part_o + pr * 128 + 32 * (q >> 2) + 8 * (q & 3) + 4 * half) =
+            r[x];
+      }
+      if (first) a.part_ml[pr] = make_float2(m, l);
+      return;
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    uint16_t* out = a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * 128;
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef u32x2 any_u32x2 __attribute__((aligned(2)));
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+      const int q = q0 + x;
+      const f32x4 y = r[x] * inv;
+      const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
+      const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
+      *reinterpret_cast<any_u32x2*>(out + 32 * (q >> 2) + 8 * (q & 3) + 4 * half) =
+          u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
+    }
+    if (a.lse && first)
+      a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] = natural(m, l);
+  }
+  static __device__ __forceinline__ float natural(float m, float l) {
+    return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+  }
+};
+
+template <bool FP8>
+__global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
+  __shared__ __align__(1024) uint8_t s_mem[kGroupedLds];
+  const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
+  Work w;
+  if (!find_work<false>(a, item, w)) return;
+  if (w.waves == 1) Grouped<FP8, 1, 8, 32>::run(a, w, h, s_mem);
+  else if (w.waves == 2) Grouped<FP8, 2, 4, 32>::run(a, w, h, s_mem);
+  else if (w.waves == 4) Grouped<FP8, 4, 2, 64>::run(a, w, h, s_mem);
+  else Grouped<FP8, 8, 1, 64>::run(a, w, h, s_mem);
+}
+
+// Merge of the splits' partial results of a row tile: 256 threads, SG groups of 32 lanes per row,
+// each over every SG-th split; the groups' sums joined through LDS in their order.
+template <int DV, int SG>
+__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
+  constexpr int ROWS = 8 / SG, NX = DV / 128;
+  __shared__ f32x4 s_o[8][NX][32];
+  const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
+  Work w;
+  if (!find_work<true>(a, item, w) || w.splits == 1) return;
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sg = grp % SG;
+  const int bm = 32 * w.waves, tile_row = blockIdx.y * ROWS + grp / SG;
+  const int row = w.tile * bm + tile_row;
+  const bool live = tile_row < bm && row < w.q.n * a.g;
+  const int64_t base = h * a.head_part_rows + w.part_row + tile_row;
+  float m = -INFINITY, l = 0.f;
+  f32x4 r[NX];
+#pragma unroll
+  for (int x = 0; x < NX; ++x) r[x] = f32x4{};
+  if (live) {
+    for (int s = lane; s < w.splits; s += 32) m = fmaxf(m, a.part_ml[base + (int64_t)s * bm].x);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+#pragma unroll 4
+    for (int s = sg; s < w.splits; s += SG) {
+      const int64_t pr = base + (int64_t)s * bm;
+      const float2 ml = a.part_ml[pr];
+      const float wt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      l += ml.y * wt;
+#pragma unroll
+      for (int x = 0; x < NX; ++x)
+        r[x] += *reinterpret_cast<const f32x4*>(a.part_o + pr * DV + 128 * x + 4 * lane) * wt;
+    }
+  }
+  if constexpr (SG > 1) {
+    __shared__ float s_l[8];
+#pragma unroll
+    for (int x = 0; x < NX; ++x) s_o[grp][x][lane] = r[x];
+    if (lane == 0) s_l[grp] = l;
+    __syncthreads();
+    if (sg != 0) return;
+    for (int t = 1; t < SG; ++t) {
+      l += s_l[grp + t];
+#pragma unroll
+      for (int x = 0; x < NX; ++x) r[x] += s_o[grp + t][x][lane];
+    }
+  }
+  if (!live) return;
+  const int tok = (int)fastdiv(row, a.div_g), head = h * a.g + row - tok * a.g;
+  const float inv = l > 0.f ? 1.f / l : l;
+  uint16_t* out = a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * DV;
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef u32x2 any_u32x2 __attribute__((aligned(2)));
+#pragma unroll
+  for (int x = 0; x < NX; ++x) {
+    const f32x4 y = r[x] * inv;
+    const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
+    const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
+    *reinterpret_cast<any_u32x2*>(out + 128 * x + 4 * lane) =
+        u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
+  }
+  if (a.lse && lane == 0)
+    a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] =
+        l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
 __device__ inline uint16_t f32_to_bf16(float x) {
   return __builtin_bit_cast(uint16_t, (__bf16)x);
 }
@@ -115,6 +771,59 @@ __global__ __launch_bounds__(64) void chunk_rows_kernel(ChunkArgs a) {
     a.lse[(int64_t)tok * H + e] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
+// ---- host: the call's plan ----------------------------------------------------------------
+
+struct ChunkPlan {
+  int64_t tiles, items;  // at most so many row tiles, (tile, split)s of a kv head
+  int64_t part_rows;     // rows of partial results, all kv heads
+  int32_t d_v, target, uni_tiles, uni_splits, max_splits, merge_rows;
+  size_t workspace_bytes;
+};
+
+// Workgroups that splitting aims at. With that many unsplit row tiles the chip is full.
+constexpr int kTargetWorkgroups = 512;
+
+ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& c) {
+  ChunkPlan p{};
+  p.d_v = kv.layout == HISPARSE_KV_GROUPED ? 128 : 512;
+  if (kv.layout != HISPARSE_KV_GROUPED) return p;
+  const int64_t chunk = std::min<int64_t>(c.max_chunk, std::max(c.total_tokens, 1));
+  const int64_t max_rows = chunk * c.q_heads;
+  const int64_t bm = 32 * row_waves((int)std::min<int64_t>(max_rows, 1 << 20));
+  const int64_t tokens = (int64_t)c.max_records * kv.tokens_per_record;
+  // every request has a last row tile that may not be full; the others are of 256 rows
+  p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
+  p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / 256 + c.num_requests,
+                              (int64_t)c.num_requests * p.uni_tiles);
+  const int64_t span =
+      c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
+  const int64_t blocks = (span + 63) / 64 + 1;  // a first token inside a block adds one
+  p.max_splits = 1;
+  p.uni_splits = 1;
+  p.items = p.tiles;
+  if (c.num_splits > 0) {
+    p.max_splits = (int32_t)std::min<int64_t>(c.num_splits, blocks);
+    p.uni_splits = p.max_splits;
+    p.items = p.tiles * p.max_splits;
+  } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > kMinSplitTokens) {
+    p.target = kTargetWorkgroups;
+    const int64_t part = std::max<int64_t>(
+        kMinSplitTokens, ((int64_t)c.num_requests * p.uni_tiles * c.kv_heads * span + p.target -
+                          1) / p.target);
+    p.uni_splits = (int32_t)std::min<int64_t>((span + part - 1) / part, kMaxSplits);
+    p.max_splits = (int32_t)std::min<int64_t>((span + kMinSplitTokens - 1) / kMinSplitTokens,
+                                              kMaxSplits);
+    p.items = std::min(p.tiles * p.max_splits, p.tiles + p.target / c.kv_heads + 1);
+    p.items = std::max(p.items, (int64_t)c.num_requests * p.uni_tiles * p.uni_splits);
+  }
+  if (p.max_splits > 1) {
+    p.merge_rows = (int32_t)bm;
+    p.part_rows = p.items * bm * c.kv_heads;
+    p.workspace_bytes = (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2));
+  }
+  return p;
+}
+
 }  // namespace
 }  // namespace hisparse
 
@@ -141,13 +850,16 @@ hisparse_status_t hisparse_validate_chunk(const hisparse_kv_desc_t* kv,
     return HISPARSE_ERR_INVALID_ARG;
   if (!(c->scale > 0.f) || c->scale > 1e6f) return HISPARSE_ERR_INVALID_ARG;
   if (c->total_tokens * H > (int64_t)INT32_MAX) return HISPARSE_ERR_UNSUPPORTED;
+  // a launch's threads are counted in 32 bits
+  if (hisparse::plan_chunk(*kv, *c).items * c->kv_heads * 512 > (int64_t)UINT32_MAX)
+    return HISPARSE_ERR_UNSUPPORTED;
   return HISPARSE_OK;
 }
 
 size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
                                       const hisparse_chunk_desc_t* c) {
   if (hisparse_validate_chunk(kv, c) != HISPARSE_OK) return 0;
-  return 0;
+  return hisparse::plan_chunk(*kv, *c).workspace_bytes;
 }
 
 hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
@@ -167,6 +879,10 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
       (uintptr_t)d_kv_len % 4 != 0 || (uintptr_t)d_q % 2 != 0 || (uintptr_t)d_out % 2 != 0 ||
       (uintptr_t)d_lse % 4 != 0)
     return HISPARSE_ERR_INVALID_ARG;
+  const ChunkPlan p = plan_chunk(*kv, *c);
+  if (p.workspace_bytes > 0 && (!d_workspace || (uintptr_t)d_workspace % 16 != 0 ||
+                                workspace_bytes < p.workspace_bytes))
+    return HISPARSE_ERR_INVALID_ARG;
   ChunkArgs a{};
   a.pool = reinterpret_cast<const uint8_t*>(d_pool);
   a.table = d_table;
@@ -175,6 +891,8 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.q = reinterpret_cast<const uint16_t*>(d_q);
   a.out = reinterpret_cast<uint16_t*>(d_out);
   a.lse = d_lse;
+  a.part_o = reinterpret_cast<float*>(d_workspace);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + p.part_rows * p.d_v);
   a.record_stride = kv->record_stride;
   a.head_stride = kv->head_stride;
   a.request_stride = kv->request_stride;
@@ -183,24 +901,39 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.table_request_stride = c->table_request_stride;
   a.table_head_stride = c->table_head_stride;
   a.num_records = kv->num_records;
+  a.head_part_rows = p.part_rows / c->kv_heads;
   a.l = kv_layout(*kv);
   a.requests = c->num_requests;
   a.kv_heads = c->kv_heads;
   a.g = c->q_heads;
   a.total = c->total_tokens;
-  a.max_chunk = c->max_chunk;
+  a.max_chunk = std::min(c->max_chunk, c->total_tokens);
   a.max_tokens = c->max_records << a.l.tpr_shift;
   a.window = c->window;
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
+  a.target = p.target;
+  a.num_splits = c->num_splits;
+  a.uni_tiles = p.uni_tiles;
+  a.uni_splits = p.uni_splits;
+  a.div_g = make_fastdiv((uint32_t)c->q_heads);
   a.scale_log2 = c->scale * 1.4426950408889634f;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const StreamDevice device(s);
-  const dim3 grid((unsigned)(c->total_tokens * c->kv_heads * c->q_heads));
   const bool fp8 = kv->type == HISPARSE_KV_FP8;
   if (kv->layout == HISPARSE_KV_GROUPED) {
-    if (fp8) hipLaunchKernelGGL((chunk_rows_kernel<false, true>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((chunk_rows_kernel<false, false>), grid, dim3(64), 0, s, a);
+    const dim3 grid((unsigned)(p.items * c->kv_heads));
+    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
+    if (p.workspace_bytes > 0) {
+      const unsigned x = (unsigned)(p.tiles * c->kv_heads);
+      if (p.max_splits <= 4)
+        hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), dim3(x, p.merge_rows / 8), dim3(256), 0,
+                           s, a);
+      else
+        hipLaunchKernelGGL((chunk_merge_kernel<128, 8>), dim3(x, p.merge_rows), dim3(256), 0, s, a);
+    }
   } else {
+    const dim3 grid((unsigned)(c->total_tokens * c->kv_heads * c->q_heads));
     if (fp8) hipLaunchKernelGGL((chunk_rows_kernel<true, true>), grid, dim3(64), 0, s, a);
     else hipLaunchKernelGGL((chunk_rows_kernel<true, false>), grid, dim3(64), 0, s, a);
   }
