@@ -4,9 +4,6 @@
 //   out = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j - m),  m the largest score,
 // over the cached tokens j that it sees: j < len, j <= len - n + i (causal), j > len - n + i -
 // window, and its record not padding.
-//
-// One wave per (new token, query head); its lanes share the dims, tokens one after the other with
-// the running maximum and sum in fp32.
 #include <algorithm>
 
 #include "attention_device.h"
@@ -48,10 +45,11 @@ struct ChunkArgs {
 
 // ---- which piece of the call a workgroup does ------------------------------------------------
 
-// Rows (new token, query head of the kv head) of one workgroup: 32 per row wave, as many row waves as
-// the request's rows fill, up to eight; the other waves of the workgroup take other tokens.
-__device__ __host__ inline int row_waves(int rows) {
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+// Rows (new token, query head of the kv head) of one workgroup: groups of 32, as many as the
+// request's rows fill, up to eight (grouped-query records) or four (latent ones). What waves are
+// left over take other tokens or other dims.
+__device__ __host__ inline int row_groups(int rows, bool latent) {
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : (rows <= 128 || latent) ? 4 : 8;
 }
 
 struct Request {
@@ -72,7 +70,7 @@ __device__ __forceinline__ Request request_of(const ChunkArgs& a, int r) {
 
 struct Work {
   Request q;
-  int req, waves, tile, split, splits;
+  int req, groups, tile, split, splits;
   int64_t part_row;  // first partial-result row of the tile's split 0
 };
 
@@ -95,17 +93,17 @@ __device__ inline int wave_prefix(int x) {  // inclusive
 // each request's tiles from the last (which see most) to the first. Splits follow from the
 // requests' lengths alone: cached tokens in parts of W / target, W the tokens of all row tiles.
 // False if there are fewer items. Wave-uniform.
-template <bool MERGE>
+template <bool LATENT, bool MERGE>
 __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w) {
   const int lane = threadIdx.x & 63;
   if (!a.start && !a.kv_len) {
-    const int bm = 32 * row_waves(a.max_chunk * a.g);
+    const int bm = 32 * row_groups(a.max_chunk * a.g, LATENT);
     const int per = MERGE ? a.uni_tiles : a.uni_tiles * a.uni_splits;
     w.req = item / per;
     if (w.req >= a.requests) return false;
     w.q = request_of(a, w.req);
     const int x = item - w.req * per;
-    w.waves = bm / 32;
+    w.groups = bm / 32;
     w.splits = a.uni_splits;
     w.tile = MERGE ? x : x / w.splits;
     w.split = MERGE ? 0 : x - w.tile * w.splits;
@@ -113,10 +111,10 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     w.tile = a.uni_tiles - 1 - w.tile;
     return true;
   }
-  auto tiles_of = [&](const Request& q, int& waves) {
+  auto tiles_of = [&](const Request& q, int& groups) {
     const int rows = q.n * a.g;
-    waves = row_waves(rows);
-    return (rows + 32 * waves - 1) / (32 * waves);
+    groups = row_groups(rows, LATENT);
+    return (rows + 32 * groups - 1) / (32 * groups);
   };
   auto span_of = [&](const Request& q) {
     return a.window ? min(q.len, a.window + q.n - 1) : q.len;
@@ -129,8 +127,8 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
       float x = 0.f;
       if (r < a.requests) {
         const Request q = request_of(a, r);
-        int waves;
-        x = (float)tiles_of(q, waves) * (float)((span_of(q) + 63) >> 6);
+        int groups;
+        x = (float)tiles_of(q, groups) * (float)((span_of(q) + 63) >> 6);
       }
       sum += wave_sum(x);
     }
@@ -143,15 +141,15 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
   for (int base = 0; base < a.requests; base += 64) {
     const int r = base + lane;
     Request q{0, 0, 0};
-    int waves = 1, tiles = 0, splits = 1;
+    int groups = 1, tiles = 0, splits = 1;
     if (r < a.requests) {
       q = request_of(a, r);
-      tiles = tiles_of(q, waves);
+      tiles = tiles_of(q, groups);
       const int span = span_of(q);
       if (a.num_splits) splits = min(a.num_splits, max(1, (span + 63) >> 6));
       else if (a.target) splits = min(max((span + part - 1) / part, 1), kMaxSplits);
     }
-    const int mine = MERGE ? tiles : tiles * splits, mine_rows = tiles * splits * waves;
+    const int mine = MERGE ? tiles : tiles * splits, mine_rows = tiles * splits * groups;
     const int pi = wave_prefix(mine), pr = wave_prefix(mine_rows);
     const uint64_t hit = __ballot(items + pi > item);
     if (hit) {
@@ -159,12 +157,12 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
       auto get = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
       w.req = base + src;
       w.q = Request{get(q.begin), get(q.n), get(q.len)};
-      w.waves = get(waves);
+      w.groups = get(groups);
       w.splits = get(splits);
       const int x = item - items - get(pi - mine);
       w.tile = MERGE ? x : x / w.splits;
       w.split = MERGE ? 0 : x - w.tile * w.splits;
-      w.part_row = (rows + get(pr - mine_rows) + (int64_t)w.tile * w.splits * w.waves) * 32;
+      w.part_row = (rows + get(pr - mine_rows) + (int64_t)w.tile * w.splits * w.groups) * 32;
       w.tile = get(tiles) - 1 - w.tile;
       return true;
     }
@@ -172,6 +170,129 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     rows += __builtin_amdgcn_readlane(pr, 63);
   }
   return false;
+}
+
+  // 8 e4m3 values times the power of two s, in bf16.
+  __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float s) {
+    u32x4 r;
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true));
+    return r;
+  }
+  // x with its non-finite bf16 values cleared; true if there was one.
+  __device__ __forceinline__ bool clear_bad(u32x4& x) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
+      bad |= lo | hi;
+      x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+    }
+    return bad;
+  }
+
+// ln of a softmax's sum from its reference (log2 units) and the sum against it.
+__device__ __forceinline__ float natural(float m, float l) {
+  return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+__device__ __forceinline__ bf16x8_t words(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_bit_cast(bf16x8_t, u32x4{a, b, c, d});
+}
+typedef u32x4 any_u32x4 __attribute__((aligned(2)));  // queries and outputs start at any element
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 any_u32x2 __attribute__((aligned(2)));
+__device__ __forceinline__ void store_bf16x4(uint16_t* to, f32x4 y) {
+  const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
+  const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
+  *reinterpret_cast<any_u32x2*>(to) =
+      u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
+}
+
+// The cached tokens [lo, hi) that new token i of a request sees (hi may be below lo).
+__device__ __forceinline__ int seen_to(const ChunkArgs& a, const Request& q, int i) {
+  return a.causal ? min(q.len, q.len - q.n + i + 1) : q.len;
+}
+__device__ __forceinline__ int seen_from(const ChunkArgs& a, const Request& q, int i) {
+  return a.window ? max(0, q.len - q.n + i + 1 - a.window) : 0;
+}
+
+// What the rows of a workgroup (ROWS of them from row0 on) and one of its groups of 32 see, where
+// the cached tokens are, and this lane's row.
+struct View {
+  const int32_t* table;
+  const uint8_t* pool;
+  int t0, t1;          // this split's tokens [t0, t1)
+  int hi_min, lo_max;  // tokens in [lo_max, hi_min) are seen by every row of the workgroup
+  int w_lo, w_hi;      // and by every row of the group; none of which sees w_end or later ones
+  int w_end;
+  int row_lo, row_hi;  // what this lane's row sees
+  int tok, head;       // its new token and query head (of all heads)
+  bool live, group_live;  // this row, any row of the group exists; one past the end stands in for
+                          // the last
+};
+template <int ROWS>
+__device__ __forceinline__ View view_of(const ChunkArgs& a, const Work& w, int h, int group,
+                                        int col) {
+  View v;
+  const Request& q = w.q;
+  const int n_rows = q.n * a.g, row0 = w.tile * ROWS;
+  const int first = (int)fastdiv(row0, a.div_g);
+  const int last = (int)fastdiv(min(n_rows, row0 + ROWS) - 1, a.div_g);
+  const int lo = seen_from(a, q, first), hi = max(seen_to(a, q, last), 0);
+  v.hi_min = seen_to(a, q, first);
+  v.lo_max = seen_from(a, q, last);
+  v.table = a.table + w.req * a.table_request_stride + h * a.table_head_stride;
+  v.pool = a.pool + w.req * a.request_stride + h * a.head_stride;
+  const int base = lo & ~63, blocks = max(0, hi - base + 63) >> 6;
+  const int c = (blocks + w.splits - 1) / w.splits;
+  v.t0 = base + w.split * c * 64;
+  v.t1 = min(hi, v.t0 + c * 64);
+  const int row_w = row0 + 32 * group, row = min(row_w + col, n_rows - 1);
+  v.group_live = row_w < n_rows;
+  v.live = row_w + col < n_rows;
+  v.tok = (int)fastdiv(row, a.div_g);
+  v.head = h * a.g + row - v.tok * a.g;
+  v.row_hi = seen_to(a, q, v.tok);
+  v.row_lo = seen_from(a, q, v.tok);
+  const int g_first = (int)fastdiv(min(row_w, n_rows - 1), a.div_g);
+  const int g_last = (int)fastdiv(min(row_w + 31, n_rows - 1), a.div_g);
+  v.w_hi = __builtin_amdgcn_readfirstlane(seen_to(a, q, g_first));
+  v.w_lo = __builtin_amdgcn_readfirstlane(seen_from(a, q, g_last));
+  v.w_end = __builtin_amdgcn_readfirstlane(seen_to(a, q, g_last));
+  return v;
+}
+
+// The token of a 32-token group that register i of half 0 of a lane's S^T accumulator holds (half
+// 1: one more).
+__device__ constexpr int score_token(int i) {
+  return 16 * (i >> 3) + 4 * (i & 3) + 2 * ((i >> 2) & 1);
+}
+
+// Softmax weights of 16 N scores (raw products) of this lane's row against its reference, in pairs
+// rounded to bf16; their unrounded sum is returned.
+template <int N>
+__device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (&s)[N],
+                                            float scale, float ref) {
+  const bool wide = __ballot(!(__builtin_fabsf(ref) <= kFused)) != 0;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      float x0 = __builtin_fmaf(s[j][i], scale, -ref);
+      float x1 = __builtin_fmaf(s[j][i + 1], scale, -ref);
+      if (wide) {
+        x0 = over_reference(s[j][i], scale, ref);
+        x1 = over_reference(s[j][i + 1], scale, ref);
+      }
+      const f32x2 p = {__builtin_amdgcn_exp2f(x0), __builtin_amdgcn_exp2f(x1)};
+      sum[i & 2] += p[0];
+      sum[(i & 2) + 1] += p[1];
+      pw[j][i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
+    }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
 
 // ---- grouped-query records -------------------------------------------------------------------
@@ -187,14 +308,6 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
 // each.
 
 using GTile = Tile<32>;  // 32 tokens of 32 pieces: K 0..15, V 16..31
-
-// What a workgroup's rows see, and where its tokens are.
-struct View {
-  const int32_t* table;
-  const uint8_t* pool;
-  int t0, t1;          // this split's tokens [t0, t1)
-  int hi_min, lo_max;  // tokens in [lo_max, hi_min) are seen by every row
-};
 
 // LDS of a workgroup, whichever its path: tiles, bad-token marks, the groups' (max, sum) pairs.
 constexpr int kGroupedMarks = 8 * GTile::BYTES;
@@ -218,27 +331,6 @@ struct Grouped {
     f32x2 sc[RGW];
   };
 
-  // 8 e4m3 values times the power of two s, in bf16.
-  static __device__ __forceinline__ u32x4 widen(uint32_t lo, uint32_t hi, float s) {
-    u32x4 r;
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, false));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, s, true));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, false));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, s, true));
-    return r;
-  }
-  // x with its non-finite bf16 values cleared; true if there was one.
-  static __device__ __forceinline__ bool clear_bad(u32x4& x) {
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool lo = (x[i] & 0x7f80u) == 0x7f80u, hi = (x[i] & 0x7f800000u) == 0x7f800000u;
-      bad |= lo | hi;
-      x[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-    }
-    return bad;
-  }
-
   static __device__ __forceinline__ void run(const ChunkArgs& a, const Work& w, int h,
                                              uint8_t* s_mem) {
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
@@ -248,40 +340,7 @@ struct Grouped {
     // tokens whose V is not finite in a tile that not every row sees: the tile's number + 1
     int* s_bad = reinterpret_cast<int*>(s_mem + kGroupedMarks) + tg * NB * (CT + 1);
 
-    // ---- rows ----
-    const int n_rows = w.q.n * a.g, row0 = w.tile * 32 * RW;
-    auto hi_of = [&](int tok) {
-      return a.causal ? min(w.q.len, w.q.len - w.q.n + tok + 1) : w.q.len;
-    };
-    auto lo_of = [&](int tok) {
-      return a.window ? max(0, w.q.len - w.q.n + tok + 1 - a.window) : 0;
-    };
-    const int tok_first = (int)fastdiv(row0, a.div_g);
-    const int tok_last = (int)fastdiv(min(n_rows, row0 + 32 * RW) - 1, a.div_g);
-    const int lo_wg = lo_of(tok_first), hi_wg = max(hi_of(tok_last), 0);
-    View v;
-    v.hi_min = hi_of(tok_first);
-    v.lo_max = lo_of(tok_last);
-    v.table = a.table + w.req * a.table_request_stride + h * a.table_head_stride;
-    v.pool = a.pool + w.req * a.request_stride + h * a.head_stride;
-    {
-      const int base = lo_wg & ~63, n_blocks = max(0, hi_wg - base + 63) >> 6;
-      const int c = (n_blocks + w.splits - 1) / w.splits;
-      v.t0 = base + w.split * c * 64;
-      v.t1 = min(hi_wg, v.t0 + c * 64);
-    }
-    // this lane's row; one past the end stands in for the last
-    const int row_w = row0 + 32 * hg;
-    const int row = min(row_w + col, n_rows - 1);
-    const bool wave_rows = row_w < n_rows;
-    const int tok = (int)fastdiv(row, a.div_g), head = h * a.g + row - tok * a.g;
-    const int row_hi = hi_of(tok), row_lo = lo_of(tok);
-    // of the wave: tokens in [w_lo, w_hi) are seen by all its rows, none from w_end on by any
-    const int w_hi = __builtin_amdgcn_readfirstlane(
-        hi_of((int)fastdiv(min(row_w, n_rows - 1), a.div_g)));
-    const int w_last = (int)fastdiv(min(row_w + 31, n_rows - 1), a.div_g);
-    const int w_lo = __builtin_amdgcn_readfirstlane(lo_of(w_last));
-    const int w_end = __builtin_amdgcn_readfirstlane(hi_of(w_last));
+    const View v = view_of<32 * RW>(a, w, h, hg, col);
 
     // ---- staging ----
     const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
@@ -365,8 +424,7 @@ struct Grouped {
     // Q^T operand: this lane's row, dims 16 kk + 8 half .. +7
     bf16x8_t qreg[8];
     {
-      typedef u32x4 any_u32x4 __attribute__((aligned(2)));
-      const uint16_t* q = a.q + (int64_t)(w.q.begin + tok) * a.q_stride + (int64_t)head * 128;
+      const uint16_t* q = a.q + (int64_t)(w.q.begin + v.tok) * a.q_stride + (int64_t)v.head * 128;
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk)
         qreg[kk] = __builtin_bit_cast(
@@ -393,7 +451,7 @@ struct Grouped {
         load_entries(it + 2);
       }
       const int base = tile_base(it);
-      if (wave_rows && base < w_end) {
+      if (v.group_live && base < v.w_end) {
         const uint8_t* tile = s_tiles + (it % NB) * TILE;
         f32x16 s[NS];
         const int kr = mla_row(col), ksw = tile_swizzle(kr);
@@ -409,14 +467,14 @@ struct Grouped {
           }
         }
         constexpr uint64_t kFull = CT == 64 ? ~0ull : 0xffffffffull;
-        if (base + CT > w_hi || base < w_lo || (mask_now & kFull) != kFull) {
-          const int hi = row_hi - base - half, lo = row_lo - base - half;
+        if (base + CT > v.w_hi || base < v.w_lo || (mask_now & kFull) != kFull) {
+          const int hi = v.row_hi - base - half, lo = v.row_lo - base - half;
           const uint64_t m = mask_now >> half;
 #pragma unroll
           for (int j = 0; j < NS; ++j)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const int t = 32 * j + 16 * (i >> 3) + 4 * (i & 3) + 2 * ((i >> 2) & 1);
+              const int t = 32 * j + score_token(i);
               const bool seen = t < hi && t >= lo && ((m >> t) & 1);
               s[j][i] = seen ? s[j][i] : -INFINITY;
             }
@@ -438,25 +496,8 @@ struct Grouped {
             for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
         }
         const float ref = m_run == -INFINITY ? 0.f : m_run;
-        const bool wide = __ballot(!(__builtin_fabsf(ref) <= kFused)) != 0;
         uint32_t pw[NS][8];
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < NS; ++j)
-#pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            float x0 = __builtin_fmaf(s[j][i], a.scale_log2, -ref);
-            float x1 = __builtin_fmaf(s[j][i + 1], a.scale_log2, -ref);
-            if (wide) {
-              x0 = over_reference(s[j][i], a.scale_log2, ref);
-              x1 = over_reference(s[j][i + 1], a.scale_log2, ref);
-            }
-            const f32x2 p = {__builtin_amdgcn_exp2f(x0), __builtin_amdgcn_exp2f(x1)};
-            sum[i & 2] += p[0];
-            sum[(i & 2) + 1] += p[1];
-            pw[j][i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
-          }
-        l_run += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        l_run += weights_of<NS>(pw, s, a.scale_log2, ref);
         // V^T operand by transpose reads: in each 16-lane group lane 4s + q addresses row 16 kb +
         // 4s + half (+ 2 for the second read), dims 32 n + 16 (col >> 4) + 4q .. +3; lane t of the
         // group then holds those rows of dim 32 n + 16 (col >> 4) + t, in P's token order.
@@ -466,9 +507,8 @@ struct Grouped {
         for (int j = 0; j < NS; ++j)
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb) {
-            const bf16x8_t p = __builtin_bit_cast(
-                bf16x8_t, u32x4{pw[j][4 * kb], pw[j][4 * kb + 1], pw[j][4 * kb + 2],
-                                pw[j][4 * kb + 3]});
+            const bf16x8_t p =
+                words(pw[j][4 * kb], pw[j][4 * kb + 1], pw[j][4 * kb + 2], pw[j][4 * kb + 3]);
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
               auto vread = [&](int y) {
@@ -492,7 +532,7 @@ struct Grouped {
           for (int t = 0; t < CT; ++t) {
             if (s_bad[(it % NB) * (CT + 1) + 1 + t] != it + 1) continue;
             const int tk = base + t;
-            if (tk >= row_hi || tk < row_lo) continue;
+            if (tk >= v.row_hi || tk < v.row_lo) continue;
             const uint8_t* rec =
                 v.pool + (int64_t)v.table[tk >> a.l.tpr_shift] * a.record_stride;
             const int in = tk & ((1 << a.l.tpr_shift) - 1);
@@ -559,8 +599,7 @@ struct Grouped {
         for (int t = 0; t < TG; ++t)
           r[x] += s_o[((t * RW + hg) * 16 + tg * NQ + x) * 64 + lane] * wt[t];
       }
-      if (row_w + col < n_rows)
-        finish<NQ>(a, w, h, r, tg * NQ, tok, head, hg * 32 + col, m, l, half);
+      if (v.live) finish<NQ>(a, w, v, h, r, tg * NQ, hg * 32 + col, m, l, half);
     } else {
       f32x4 r[16];
 #pragma unroll
@@ -568,14 +607,14 @@ struct Grouped {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           r[4 * n + x] = f32x4{o[n][4 * x], o[n][4 * x + 1], o[n][4 * x + 2], o[n][4 * x + 3]};
-      if (row_w + col < n_rows) finish<16>(a, w, h, r, 0, tok, head, hg * 32 + col, m, l, half);
+      if (v.live) finish<16>(a, w, v, h, r, 0, hg * 32 + col, m, l, half);
     }
   }
 
   // NQ quads of a row's result from quad q0 on (quad 4n + x: dims 32n + 8x + 4 half .. +3).
   template <int NQ>
-  static __device__ __forceinline__ void finish(const ChunkArgs& a, const Work& w, int h,
-                                                const f32x4* r, int q0, int tok, int head,
+  static __device__ __forceinline__ void finish(const ChunkArgs& a, const Work& w,
+                                                const View& v, int h, const f32x4* r, int q0,
                                                 int tile_row, float m, float l, int half) {
     const bool first = q0 == 0 && half == 0;
     if (w.splits > 1) {
@@ -590,23 +629,15 @@ struct Grouped {
       return;
     }
     const float inv = l > 0.f ? 1.f / l : l;
-    uint16_t* out = a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * 128;
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    typedef u32x2 any_u32x2 __attribute__((aligned(2)));
+    uint16_t* out =
+        a.out + (int64_t)(w.q.begin + v.tok) * a.out_stride + (int64_t)v.head * 128;
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
       const int q = q0 + x;
-      const f32x4 y = r[x] * inv;
-      const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
-      const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
-      *reinterpret_cast<any_u32x2*>(out + 32 * (q >> 2) + 8 * (q & 3) + 4 * half) =
-          u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
+      store_bf16x4(out + 32 * (q >> 2) + 8 * (q & 3) + 4 * half, r[x] * inv);
     }
     if (a.lse && first)
-      a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] = natural(m, l);
-  }
-  static __device__ __forceinline__ float natural(float m, float l) {
-    return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+      a.lse[(int64_t)(w.q.begin + v.tok) * (a.kv_heads * a.g) + v.head] = natural(m, l);
   }
 };
 
@@ -615,11 +646,346 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
   __shared__ __align__(1024) uint8_t s_mem[kGroupedLds];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
-  if (!find_work<false>(a, item, w)) return;
-  if (w.waves == 1) Grouped<FP8, 1, 8, 32>::run(a, w, h, s_mem);
-  else if (w.waves == 2) Grouped<FP8, 2, 4, 32>::run(a, w, h, s_mem);
-  else if (w.waves == 4) Grouped<FP8, 4, 2, 64>::run(a, w, h, s_mem);
+  if (!find_work<false, false>(a, item, w)) return;
+  if (w.groups == 1) Grouped<FP8, 1, 8, 32>::run(a, w, h, s_mem);
+  else if (w.groups == 2) Grouped<FP8, 2, 4, 32>::run(a, w, h, s_mem);
+  else if (w.groups == 4) Grouped<FP8, 4, 2, 64>::run(a, w, h, s_mem);
   else Grouped<FP8, 8, 1, 64>::run(a, w, h, s_mem);
+}
+
+// ---- latent records --------------------------------------------------------------------------
+//
+// Eight waves: RG groups of 32 rows, times DS waves that share a group's rows, times TG token
+// groups. A tile is 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the value is
+// the latent part). Of the DS waves of a row group, wave d
+//   adds up the k-steps kk = d mod DS of the scores, which are then summed through LDS,
+//   and keeps the output dims 512 / DS d .. of its rows;
+// so the query and the output of 32 rows, 144 and 256 registers a lane, are spread over DS waves,
+// and a tile is read from LDS once per row group, not once per wave. The softmax is worked out by
+// each of the DS waves.
+
+using LTile = Tile<72>;
+
+template <bool FP8, int RG, int DS, int TG>
+struct Latent {
+  static constexpr int CT = 32;
+  static constexpr int NB = TG == 1 ? 2 : 1;   // tile buffers
+  static constexpr int GW = RG * DS;           // waves of a token group
+  static constexpr int SPLIT = GW / 4;         // waves that share a group of eight rows in staging
+  static constexpr int NQ = 36 / DS;           // k-steps of a wave
+  static constexpr int NO = 16 / DS;           // its output tiles of 32 dims
+  static constexpr int NLD = FP8 ? 4 / SPLIT + 1 : (9 + SPLIT - 1) / SPLIT;  // 16-byte loads
+  static_assert(RG * DS * TG == 8 && (SPLIT == 1 || SPLIT == 2), "shape");
+  // LDS: tiles, partial scores, bad-token marks; at the end the token groups' outputs and (max, sum)
+  static constexpr int SCORES = TG * NB * LTile::BYTES;
+  static constexpr int MARKS = SCORES + 8 * 4096;
+  static constexpr int ML = 8 * NO * 4 * 1024;
+  static constexpr int LDS = std::max(MARKS + TG * NB * (CT + 1) * 4, TG > 1 ? ML + 8 * 32 * 8 : 0);
+
+  static __device__ __forceinline__ void run(const ChunkArgs& a, const Work& w, int h,
+                                             uint8_t* s_mem) {
+    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tg = wave / GW, in_group = wave % GW, rg = in_group / DS, ds = in_group % DS;
+    uint8_t* s_tiles = s_mem + tg * NB * LTile::BYTES;
+    f32x4* s_scores = reinterpret_cast<f32x4*>(s_mem + SCORES) + (tg * GW + rg * DS) * 256;
+    int* s_bad = reinterpret_cast<int*>(s_mem + MARKS) + tg * NB * (CT + 1);
+    const View v = view_of<32 * RG>(a, w, h, rg, col);
+
+    // ---- staging: wave in_group stages rows 8 (in_group / SPLIT) .., part in_group % SPLIT ----
+    const int srg = in_group / SPLIT, spart = in_group % SPLIT;
+    const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
+    auto tile_base = [&](int it) { return v.t0 + (it * TG + tg) * CT; };
+    auto entry = [&](int t) { return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1; };
+    auto ok_entry = [&](int32_t r) { return r >= 0 && r < a.num_records; };
+    int32_t e, ev;  // table entries of this lane's row of the tile to load next, of its token
+    auto load_entries = [&](int it) {
+      const int base = tile_base(it);
+      e = entry(base + 8 * srg + (lane >> 3));
+      ev = entry(base + (lane & (CT - 1)));
+    };
+    u32x4 st[NLD];
+    float st_scale = 1.f;
+    uint32_t vmask = 0;
+    // bf16: segments of 8 pieces: all nine, or 0..3 and 4..8. 8-bit: payload segments 0..3 and the
+    // rotary one, or 0, 1 and 2, 3 with the rotary one.
+    const int seg0 = SPLIT == 1 ? 0 : FP8 ? 2 * spart : 4 * spart;
+    auto issue = [&](int it) {
+      const int t = tile_base(it) + 8 * srg + (lane >> 3);
+      const int in = t & ((1 << a.l.tpr_shift) - 1);
+      vmask = (uint32_t)__ballot(ok_entry(ev));
+      const uint8_t* rec = v.pool + (int64_t)e * a.record_stride;
+      const uint8_t* src = rec + (int64_t)in * a.l.row_bytes + 16 * (lane & 7) + 128 * seg0;
+#pragma unroll
+      for (int x = 0; x < NLD; ++x) st[x] = u32x4{};
+      st_scale = 1.f;
+      if (ok_entry(e)) {
+        if constexpr (FP8) {
+#pragma unroll
+          for (int x = 0; x < NLD - 1; ++x)
+            st[x] = *reinterpret_cast<const u32x4*>(src + 128 * x);
+          if (SPLIT == 1 || spart == 1)
+            st[NLD - 1] = *reinterpret_cast<const u32x4*>(rec + a.l.rope_offset + 128 * in +
+                                                          16 * (lane & 7));
+          st_scale = *reinterpret_cast<const float*>(rec + a.l.scale_offset + 4 * in);
+        } else {
+#pragma unroll
+          for (int x = 0; x < NLD; ++x)
+            if (seg0 + x < (SPLIT == 1 || spart == 1 ? 9 : 4))
+              st[x] = *reinterpret_cast<const u32x4*>(src + 128 * x);
+        }
+      }
+    };
+    auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
+    auto store = [&](int it) {
+      const int r = 8 * srg + (lane >> 3), sw = tile_swizzle(r);
+      uint8_t* dst = s_tiles + (it % NB) * LTile::BYTES + LTile::row(r);
+      const bool part = partial(tile_base(it));
+      bool bad = false;
+      if constexpr (FP8) {
+#pragma unroll
+        for (int x = 0; x < NLD - 1; ++x) {
+          u32x4 p0 = widen(st[x][0], st[x][1], st_scale);
+          u32x4 p1 = widen(st[x][2], st[x][3], st_scale);
+          if (part) {
+            bad |= clear_bad(p0);
+            bad |= clear_bad(p1);
+          }
+          uint8_t* seg = dst + (2 * (seg0 + x) + ((lane & 7) >> 2)) * 1024;
+          const int p = 2 * (lane & 3);
+          *reinterpret_cast<u32x4*>(seg + ((p ^ sw) << 4)) = p0;
+          *reinterpret_cast<u32x4*>(seg + (((p + 1) ^ sw) << 4)) = p1;
+        }
+        if (SPLIT == 1 || spart == 1)
+          *reinterpret_cast<u32x4*>(dst + 8 * 1024 + (((lane & 7) ^ sw) << 4)) = st[NLD - 1];
+      } else {
+#pragma unroll
+        for (int x = 0; x < NLD; ++x) {
+          const int seg = seg0 + x;
+          if (seg < (SPLIT == 1 || spart == 1 ? 9 : 4)) {
+            if (part && seg < 8) bad |= clear_bad(st[x]);
+            *reinterpret_cast<u32x4*>(dst + seg * 1024 + (((lane & 7) ^ sw) << 4)) = st[x];
+          }
+        }
+      }
+      if (part && bad) {
+        s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
+        s_bad[(it % NB) * (CT + 1)] = it + 1;
+      }
+    };
+
+    load_entries(0);
+    for (int i = lane + 64 * in_group; i < NB * (CT + 1); i += 64 * GW) s_bad[i] = 0;
+    // Q^T operand of k-steps kk = DS i + ds: dims 16 kk + 8 half .. +7 of this lane's row
+    bf16x8_t qreg[NQ];
+    {
+      const uint16_t* q = a.q + (int64_t)(w.q.begin + v.tok) * a.q_stride + (int64_t)v.head * 576;
+#pragma unroll
+      for (int i = 0; i < NQ; ++i)
+        qreg[i] = __builtin_bit_cast(
+            bf16x8_t,
+            (u32x4)*reinterpret_cast<const any_u32x4*>(q + 16 * (DS * i + ds) + 8 * half));
+    }
+    f32x16 o[NO];
+#pragma unroll
+    for (int n = 0; n < NO; ++n) o[n] = f32x16{};
+    float m_run = -INFINITY, l_run = 0.f;
+    uint32_t mask_now = 0;
+    if (n_it > 0) {
+      issue(0);
+      load_entries(1);
+      __syncthreads();  // s_bad is clear
+      store(0);
+      mask_now = vmask;
+    }
+
+    for (int it = 0; it < n_it; ++it) {
+      __syncthreads();  // tile `it` is stored; with two buffers, tile it - 1 is read by all
+      if (it + 1 < n_it) {
+        issue(it + 1);
+        load_entries(it + 2);
+      }
+      const int base = tile_base(it);
+      const uint8_t* tile = s_tiles + (it % NB) * LTile::BYTES;
+      const bool busy = v.group_live && base < v.w_end;
+      f32x16 s[1];
+      if (busy) {
+        // K piece 2 kk + half of k-step DS i + ds: for DS 4 segment i, for DS 2 segment i / 2
+        const int kr = mla_row(col), ksw = tile_swizzle(kr);
+        const uint8_t* krow = tile + LTile::row(kr);
+        s[0] = f32x16{};
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) {
+          const int p = DS == 4 ? 2 * ds + half : 4 * (i & 1) + 2 * ds + half;
+          const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
+              krow + (DS == 4 ? i : i / 2) * 1024 + ((p ^ ksw) << 4));
+          s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qreg[i], s[0], 0, 0, 0);
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          s_scores[ds * 256 + x * 64 + lane] =
+              f32x4{s[0][4 * x], s[0][4 * x + 1], s[0][4 * x + 2], s[0][4 * x + 3]};
+      }
+      __syncthreads();  // every wave's part of the scores is there
+      if (busy) {
+        // summed in the same order by every wave, so that they agree on every bit
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          f32x4 y = s_scores[x * 64 + lane];
+#pragma unroll
+          for (int d = 1; d < DS; ++d) y += s_scores[d * 256 + x * 64 + lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[0][4 * x + i] = y[i];
+        }
+        if (base + CT > v.w_hi || base < v.w_lo || mask_now != 0xffffffffu) {
+          const int hi = v.row_hi - base - half, lo = v.row_lo - base - half;
+          const uint32_t m = mask_now >> half;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int t = score_token(i);
+            const bool seen = t < hi && t >= lo && ((m >> t) & 1);
+            s[0][i] = seen ? s[0][i] : -INFINITY;
+          }
+        }
+        float cmax = s[0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, s[0][i]);
+        cmax *= a.scale_log2;
+        if (__ballot(cmax > m_run + kSlack || (m_run == -INFINITY && cmax > -INFINITY))) {
+          const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
+          const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+          m_run = m_new;
+          l_run *= alpha;
+#pragma unroll
+          for (int n = 0; n < NO; ++n)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
+        }
+        uint32_t pw[1][8];
+        l_run += weights_of<1>(pw, s, a.scale_log2, m_run == -INFINITY ? 0.f : m_run);
+        // V^T operand by transpose reads, as in Grouped; dims 32 (NO ds + n) are pieces 4 (NO ds +
+        // n) .., segment (NO ds + n) / 2
+        const int vr = 4 * ((lane & 15) >> 2) + half;
+        const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+          const bf16x8_t p =
+              words(pw[0][4 * kb], pw[0][4 * kb + 1], pw[0][4 * kb + 2], pw[0][4 * kb + 3]);
+#pragma unroll
+          for (int n = 0; n < NO; ++n) {
+            auto vread = [&](int y) {
+              const int r = vr + 2 * y;
+              const uint8_t* at = tile + LTile::row(r) + kb * 2 * LTile::NSEG * 1024 +
+                                  ds * (NO / 2) * 1024 + (n / 2) * 1024 +
+                                  (((vp + 4 * (n & 1)) ^ tile_swizzle(r)) << 4) + 8 * (lane & 1);
+              return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                  (lds_v4i16*)const_cast<uint8_t*>(at));
+            };
+            const bf16x8_t vt = __builtin_bit_cast(
+                bf16x8_t, __builtin_shufflevector(vread(0), vread(1), 0, 1, 2, 3, 4, 5, 6, 7));
+            o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p, o[n], 0, 0, 0);
+          }
+        }
+        // A latent that is not finite, in a tile that only some rows see, was stored as zeros
+        // (zero weights would have made NaN of it). It is key and value at once: what a row that
+        // sees it becomes is NaN.
+        if (partial(base) &&
+            __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
+          const uint32_t bad =
+              (uint32_t)__ballot(s_bad[(it % NB) * (CT + 1) + 1 + (lane & 31)] == it + 1);
+          const int hi = min(v.row_hi - base, 32), lo = max(v.row_lo - base, 0);
+          const uint32_t seen = lo < hi ? (0xffffffffu >> (32 - (hi - lo))) << lo : 0u;
+          if (bad & seen) l_run = NAN;
+        }
+      }
+      if constexpr (NB == 1) __syncthreads();  // the tile is read by all
+      if (it + 1 < n_it) {
+        store(it + 1);
+        mask_now = vmask;
+      }
+    }
+    l_run += __shfl_xor(l_run, 32, 64);
+
+    // ---- results; the token groups' merged through LDS ----
+    float m = m_run, l = l_run;
+    auto quad = [&](int q) {
+      return f32x4{o[q >> 2][4 * (q & 3)], o[q >> 2][4 * (q & 3) + 1], o[q >> 2][4 * (q & 3) + 2],
+                   o[q >> 2][4 * (q & 3) + 3]};
+    };
+    constexpr int QUADS = 4 * NO, MINE = QUADS / TG;
+    f32x4 r[MINE];
+    if constexpr (TG > 1) {
+      float2* s_ml = reinterpret_cast<float2*>(s_mem + ML);
+      f32x4* s_o = reinterpret_cast<f32x4*>(s_mem);
+      __syncthreads();
+#pragma unroll
+      for (int q = 0; q < QUADS; ++q) s_o[(wave * QUADS + q) * 64 + lane] = quad(q);
+      if (half == 0) s_ml[wave * 32 + col] = make_float2(m_run, l_run);
+      __syncthreads();
+      float2 ml[TG];
+      m = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < TG; ++t) {
+        ml[t] = s_ml[(t * GW + in_group) * 32 + col];
+        m = fmaxf(m, ml[t].x);
+      }
+      l = 0.f;
+      float wt[TG];
+#pragma unroll
+      for (int t = 0; t < TG; ++t) {
+        wt[t] = ml[t].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[t].x - m);
+        l += ml[t].y * wt[t];
+      }
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) {
+        r[x] = f32x4{};
+#pragma unroll
+        for (int t = 0; t < TG; ++t)
+          r[x] += s_o[((t * GW + in_group) * QUADS + tg * MINE + x) * 64 + lane] * wt[t];
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < MINE; ++x) r[x] = quad(x);
+    }
+    if (!v.live) return;
+    const bool first = ds == 0 && tg == 0 && half == 0;
+    // quad q of the wave: dims 32 (NO ds + q / 4) + 8 (q % 4) + 4 half .. +3
+    auto dim = [&](int x) {
+      const int q = tg * MINE + x;
+      return 32 * (NO * ds + (q >> 2)) + 8 * (q & 3) + 4 * half;
+    };
+    if (w.splits > 1) {
+      const int64_t pr =
+          h * a.head_part_rows + w.part_row + w.split * 32 * RG + rg * 32 + col;
+#pragma unroll
+      for (int x = 0; x < MINE; ++x)
+        *reinterpret_cast<f32x4*>(a.part_o + pr * 512 + dim(x)) = r[x];
+      if (first) a.part_ml[pr] = make_float2(m, l);
+      return;
+    }
+    const float inv = l > 0.f ? 1.f / l : l;
+    uint16_t* out =
+        a.out + (int64_t)(w.q.begin + v.tok) * a.out_stride + (int64_t)v.head * 512;
+#pragma unroll
+    for (int x = 0; x < MINE; ++x) store_bf16x4(out + dim(x), r[x] * inv);
+    if (a.lse && first)
+      a.lse[(int64_t)(w.q.begin + v.tok) * (a.kv_heads * a.g) + v.head] = natural(m, l);
+  }
+};
+
+template <bool FP8>
+__global__ __launch_bounds__(512, 2) void chunk_latent_kernel(ChunkArgs a) {
+  using L1 = Latent<FP8, 1, 4, 2>;
+  using L2 = Latent<FP8, 2, 4, 1>;
+  using L4 = Latent<FP8, 4, 2, 1>;
+  constexpr int LDS = std::max(std::max(L1::LDS, L2::LDS), L4::LDS);
+  __shared__ __align__(1024) uint8_t s_mem[LDS];
+  const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
+  Work w;
+  if (!find_work<true, false>(a, item, w)) return;
+  if (w.groups == 1) L1::run(a, w, h, s_mem);
+  else if (w.groups == 2) L2::run(a, w, h, s_mem);
+  else L4::run(a, w, h, s_mem);
 }
 
 // Merge of the splits' partial results of a row tile: 256 threads, SG groups of 32 lanes per row,
@@ -630,9 +996,9 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
   __shared__ f32x4 s_o[8][NX][32];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
-  if (!find_work<true>(a, item, w) || w.splits == 1) return;
+  if (!find_work<(DV == 512), true>(a, item, w) || w.splits == 1) return;
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sg = grp % SG;
-  const int bm = 32 * w.waves, tile_row = blockIdx.y * ROWS + grp / SG;
+  const int bm = 32 * w.groups, tile_row = blockIdx.y * ROWS + grp / SG;
   const int row = w.tile * bm + tile_row;
   const bool live = tile_row < bm && row < w.q.n * a.g;
   const int64_t base = h * a.head_part_rows + w.part_row + tile_row;
@@ -672,103 +1038,10 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
   const int tok = (int)fastdiv(row, a.div_g), head = h * a.g + row - tok * a.g;
   const float inv = l > 0.f ? 1.f / l : l;
   uint16_t* out = a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * DV;
-  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-  typedef u32x2 any_u32x2 __attribute__((aligned(2)));
 #pragma unroll
-  for (int x = 0; x < NX; ++x) {
-    const f32x4 y = r[x] * inv;
-    const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
-    const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
-    *reinterpret_cast<any_u32x2*>(out + 128 * x + 4 * lane) =
-        u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
-  }
+  for (int x = 0; x < NX; ++x) store_bf16x4(out + 128 * x + 4 * lane, r[x] * inv);
   if (a.lse && lane == 0)
-    a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] =
-        l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
-}
-
-__device__ inline uint16_t f32_to_bf16(float x) {
-  return __builtin_bit_cast(uint16_t, (__bf16)x);
-}
-
-template <bool LATENT, bool FP8>
-__global__ __launch_bounds__(64) void chunk_rows_kernel(ChunkArgs a) {
-  constexpr int NQ = LATENT ? 9 : 2, NV = LATENT ? 8 : 2;
-  const int H = a.kv_heads * a.g, lane = threadIdx.x;
-  const int tok = blockIdx.x / H, e = blockIdx.x - tok * H, h = e / a.g;
-  int req = -1, begin = 0, end = 0;
-  if (a.start) {
-    for (int r = 0; r < a.requests; ++r) {
-      begin = min(max(a.start[r], 0), a.total);
-      end = min(max(a.start[r + 1], begin), a.total);
-      if (tok >= begin && tok < end) {
-        req = r;
-        break;
-      }
-    }
-  } else if (tok < a.requests * a.max_chunk) {
-    req = tok / a.max_chunk;
-    begin = req * a.max_chunk;
-    end = begin + a.max_chunk;
-  }
-  if (req < 0) return;
-  const int len = a.kv_len ? min(max(a.kv_len[req], 0), a.max_tokens) : a.max_tokens;
-  const int pos = len - (end - begin) + (tok - begin);
-  const int hi = a.causal ? min(len, pos + 1) : len;
-  const int lo = a.window ? max(0, pos - a.window + 1) : 0;
-  const uint16_t* q = a.q + tok * a.q_stride + (int64_t)e * (LATENT ? 576 : 128);
-  float qv[NQ], acc[NV], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < NQ; ++i) qv[i] = bf16_to_f32(q[lane + 64 * i]);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) acc[i] = 0.f;
-  const int32_t* table = a.table + req * a.table_request_stride + h * a.table_head_stride;
-  for (int j = lo; j < hi; ++j) {
-    const int32_t r = table[j >> a.l.tpr_shift];
-    if (r < 0 || r >= a.num_records) continue;
-    const uint8_t* rec = a.pool + req * a.request_stride + h * a.head_stride + r * a.record_stride;
-    const int t = j & ((1 << a.l.tpr_shift) - 1);
-    const uint8_t* row = rec + (int64_t)t * a.l.row_bytes;
-    float kv[NQ], vv[NV];
-    if constexpr (!FP8) {
-      const uint16_t* x = reinterpret_cast<const uint16_t*>(row);
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) kv[i] = bf16_to_f32(x[lane + 64 * i]);
-#pragma unroll
-      for (int i = 0; i < NV; ++i) vv[i] = LATENT ? kv[i] : bf16_to_f32(x[128 + lane + 64 * i]);
-    } else {
-      const float* sc = reinterpret_cast<const float*>(rec + a.l.scale_offset);
-      const float sk = sc[LATENT ? t : 2 * t];
-#pragma unroll
-      for (int i = 0; i < (LATENT ? 8 : 2); ++i)
-        kv[i] = __builtin_amdgcn_cvt_f32_fp8(row[lane + 64 * i], 0) * sk;
-      if constexpr (LATENT)
-        kv[8] = bf16_to_f32(
-            reinterpret_cast<const uint16_t*>(rec + a.l.rope_offset + t * 128)[lane]);
-#pragma unroll
-      for (int i = 0; i < NV; ++i)
-        vv[i] = LATENT ? kv[i]
-                       : __builtin_amdgcn_cvt_f32_fp8(row[128 + lane + 64 * i], 0) * sc[2 * t + 1];
-    }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) s += qv[i] * kv[i];
-#pragma unroll
-    for (int x = 32; x >= 1; x >>= 1) s += __shfl_xor(s, x, 64);
-    s *= a.scale_log2;
-    const float m_new = fmaxf(m, s);
-    const float alpha = exp2f(m - m_new), p = exp2f(s - m_new);
-    l = l * alpha + p;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) acc[i] = acc[i] * alpha + p * vv[i];
-    m = m_new;
-  }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  uint16_t* o = a.out + tok * a.out_stride + (int64_t)e * (LATENT ? 512 : 128);
-#pragma unroll
-  for (int i = 0; i < NV; ++i) o[lane + 64 * i] = f32_to_bf16(acc[i] * inv);
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)tok * H + e] = l > 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] = natural(m, l);
 }
 
 // ---- host: the call's plan ----------------------------------------------------------------
@@ -786,14 +1059,15 @@ constexpr int kTargetWorkgroups = 512;
 ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& c) {
   ChunkPlan p{};
   p.d_v = kv.layout == HISPARSE_KV_GROUPED ? 128 : 512;
-  if (kv.layout != HISPARSE_KV_GROUPED) return p;
+  const bool latent = kv.layout == HISPARSE_KV_LATENT;
   const int64_t chunk = std::min<int64_t>(c.max_chunk, std::max(c.total_tokens, 1));
   const int64_t max_rows = chunk * c.q_heads;
-  const int64_t bm = 32 * row_waves((int)std::min<int64_t>(max_rows, 1 << 20));
+  const int64_t bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent);
   const int64_t tokens = (int64_t)c.max_records * kv.tokens_per_record;
-  // every request has a last row tile that may not be full; the others are of 256 rows
+  // every request has a last row tile that may not be full; the others are of the most rows
   p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
-  p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / 256 + c.num_requests,
+  p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / (latent ? 128 : 256) +
+                                  c.num_requests,
                               (int64_t)c.num_requests * p.uni_tiles);
   const int64_t span =
       c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
@@ -920,22 +1194,23 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const StreamDevice device(s);
   const bool fp8 = kv->type == HISPARSE_KV_FP8;
+  const dim3 grid((unsigned)(p.items * c->kv_heads)), block(512);
+  const dim3 merge((unsigned)(p.tiles * c->kv_heads),
+                   p.max_splits <= 4 ? p.merge_rows / 8 : p.merge_rows);
   if (kv->layout == HISPARSE_KV_GROUPED) {
-    const dim3 grid((unsigned)(p.items * c->kv_heads));
-    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
-    if (p.workspace_bytes > 0) {
-      const unsigned x = (unsigned)(p.tiles * c->kv_heads);
-      if (p.max_splits <= 4)
-        hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), dim3(x, p.merge_rows / 8), dim3(256), 0,
-                           s, a);
-      else
-        hipLaunchKernelGGL((chunk_merge_kernel<128, 8>), dim3(x, p.merge_rows), dim3(256), 0, s, a);
-    }
+    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, block, 0, s, a);
+    if (p.max_splits > 4)
+      hipLaunchKernelGGL((chunk_merge_kernel<128, 8>), merge, dim3(256), 0, s, a);
+    else if (p.max_splits > 1)
+      hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), merge, dim3(256), 0, s, a);
   } else {
-    const dim3 grid((unsigned)(c->total_tokens * c->kv_heads * c->q_heads));
-    if (fp8) hipLaunchKernelGGL((chunk_rows_kernel<true, true>), grid, dim3(64), 0, s, a);
-    else hipLaunchKernelGGL((chunk_rows_kernel<true, false>), grid, dim3(64), 0, s, a);
+    if (fp8) hipLaunchKernelGGL(chunk_latent_kernel<true>, grid, block, 0, s, a);
+    else hipLaunchKernelGGL(chunk_latent_kernel<false>, grid, block, 0, s, a);
+    if (p.max_splits > 4)
+      hipLaunchKernelGGL((chunk_merge_kernel<512, 8>), merge, dim3(256), 0, s, a);
+    else if (p.max_splits > 1)
+      hipLaunchKernelGGL((chunk_merge_kernel<512, 1>), merge, dim3(256), 0, s, a);
   }
   return hipGetLastError() == hipSuccess ? HISPARSE_OK : HISPARSE_ERR_HIP;
 }
