@@ -564,7 +564,8 @@ typedef struct {
   int32_t record_bytes;       /* multiple of 16, at least hisparse_kv_record_bytes, at most 8 MiB;
                                  for bf16 each token's share of it a multiple of 16 as well */
   int64_t num_records;        /* 1 .. 2^31 - 1: indices outside [0, num_records) are padding */
-  int64_t record_stride;      /* bytes, multiples of 16, >= 0; record_stride >= record_bytes */
+  int64_t record_stride;      /* bytes, multiples of 16, >= 0; record_stride at least record_bytes
+                                 and below 2^31 */
   int64_t head_stride;
   int64_t request_stride;
 } hisparse_kv_desc_t;
@@ -618,8 +619,8 @@ typedef struct {
   int32_t kv_heads;            /* kv heads (units) of a request, >= 1; at most 2^20 of all requests */
   int32_t q_heads;             /* query heads on each kv head: 1 .. 256 */
   int32_t total_tokens;        /* rows of d_q and d_out: new tokens of all requests, or more */
-  int32_t max_chunk;           /* new tokens of the longest request, >= 1; with d_chunk_start a hint
-                                  that only picks the plan */
+  int32_t max_chunk;           /* the most new tokens of a request, >= 1; a longer chunk is held to
+                                  its first max_chunk */
   int32_t max_records;         /* entries of a record table row: the longest request's records;
                                   max_records * tokens_per_record at most 2^30 */
   int64_t q_token_stride;      /* elements from one new token's heads to the next one's, >= 0 */

@@ -162,19 +162,7 @@ __device__ __forceinline__ void mfma_qk(f32x16& acc, const u32x4& k, const bf16x
 // four different 32-byte slot pairs.
 __device__ inline int tile_row(int m) { return 4 * (m & 3) + (m >> 2); }
 
-// Direct global->LDS load of one block, segment SEG of row group rg: `src` is this lane's row (row
-// 8 rg + lane / 8) already advanced by the lane's 16-byte piece. The load's immediate offset
-// moves both addresses.
-template <int P, int SEG>
-__device__ __forceinline__ void stage_block(uint8_t* tile, int rg, const uint8_t* src) {
-  __builtin_amdgcn_global_load_lds(
-      src, (lds_void*)(tile + (rg * Tile<P>::NSEG + SEG) * 1024 - SEG * 128), 16, SEG * 128, 0);
-}
-template <int P>
-__device__ __forceinline__ void stage_rows(uint8_t* tile, int rg, const uint8_t* src) {
-  static_for<Tile<P>::NSEG>([&](auto seg) { stage_block<P, seg>(tile, rg, src); });
-}
-// The same by way of registers, for rows at any address: a direct-to-LDS load has to be aligned.
+// stage_rows by way of registers, for rows at any address: a direct-to-LDS load has to be aligned.
 template <int P>
 __device__ __forceinline__ void copy_rows(uint8_t* tile, int rg, const uint8_t* src) {
   typedef u32x4 any_u32x4 __attribute__((aligned(2)));
@@ -183,11 +171,6 @@ __device__ __forceinline__ void copy_rows(uint8_t* tile, int rg, const uint8_t* 
   for (int seg = 0; seg < Tile<P>::NSEG; ++seg)
     dst[seg * 64] = *reinterpret_cast<const any_u32x4*>(src + seg * 128);
 }
-// The 16-byte piece (times 16) that a lane fetches for its row of row group rg.
-__device__ inline int stage_piece(int lane, int rg) {
-  return ((lane & 7) ^ tile_swizzle(8 * rg + (lane >> 3))) << 4;
-}
-
 // The records of a split: where its tokens' indices are and how a token finds its bytes.
 struct SplitRows {
   const int32_t* idx;     // the split's record indices in memory

@@ -82,6 +82,10 @@ template <int N>
 __device__ __forceinline__ void lgkm_wait2(u32x4& a, u32x4& b) {
   asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(N));
 }
+template <int N>
+__device__ __forceinline__ void lgkm_wait1(u32x4& a) {
+  asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(N));
+}
 
 // Wait until at most N direct-to-LDS loads of this wave are outstanding and its LDS writes are
 // done, then synchronise the workgroup. (A workgroup fence would also drain the younger
@@ -119,6 +123,23 @@ struct Tile {
   __device__ static int row(int r) { return (r >> 3) * (NSEG * 1024) + (r & 7) * 128; }
 };
 __device__ inline int tile_swizzle(int r) { return (r >> 1) & 7; }
+
+// Direct global->LDS load of one block, segment SEG of row group rg: `src` is this lane's row (row
+// 8 rg + lane / 8) already advanced by the lane's 16-byte piece. The load's immediate offset
+// moves both addresses.
+template <int P, int SEG>
+__device__ __forceinline__ void stage_block(uint8_t* tile, int rg, const uint8_t* src) {
+  __builtin_amdgcn_global_load_lds(
+      src, (lds_void*)(tile + (rg * Tile<P>::NSEG + SEG) * 1024 - SEG * 128), 16, SEG * 128, 0);
+}
+template <int P>
+__device__ __forceinline__ void stage_rows(uint8_t* tile, int rg, const uint8_t* src) {
+  static_for<Tile<P>::NSEG>([&](auto seg) { stage_block<P, seg>(tile, rg, src); });
+}
+// The 16-byte piece (times 16) that a lane fetches for its row of row group rg.
+__device__ inline int stage_piece(int lane, int rg) {
+  return ((lane & 7) ^ tile_swizzle(8 * rg + (lane >> 3))) << 4;
+}
 
 // Logical row r of a 32-token MFMA tile -> LDS tile row (token) for the latent-attention kernel.
 // With r = 16a + 8b + 4h + s the row is 16a + 4s + 2b + h: the P operand of a lane (k-step a,

@@ -14,9 +14,12 @@ namespace hisparse {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
-// Exponentials are taken against a running reference that moves only when a row's scores outgrow it
-// by more than this (powers of two): exact softmax arithmetic with another reference point.
-constexpr float kSlack = 8.0f;
+// Exponentials are taken against a reference per row, the largest score of the first tile that it
+// sees, which moves only when a tile's weights add up to more than this: exact softmax arithmetic
+// with another reference point, and no search for the largest score in the other tiles. (Weights
+// up to 2^64 and their sums over 2^30 tokens stay inside the float range; the score that the
+// reference was taken from weighs 1, so that a row's sum is at least that.)
+constexpr float kWeightLimit = 18446744073709551616.f;
 // Up to this reference a weight comes from one fused multiply-add; beyond it the product is rounded
 // first, as the reference was, or a weight could leave the float range.
 constexpr float kFused = 16777216.f;
@@ -193,6 +196,11 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     return bad;
   }
 
+// x if it is an infinity or NaN, else 0 (in bit operations, for the reason given at mask_scores).
+__device__ __forceinline__ float if_not_finite(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return __uint_as_float(b & (uint32_t)((int32_t)((b & 0x7fffffffu) + 0x00800000u) >> 31));
+}
 // ln of a softmax's sum from its reference (log2 units) and the sum against it.
 __device__ __forceinline__ float natural(float m, float l) {
   return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -270,29 +278,82 @@ __device__ constexpr int score_token(int i) {
   return 16 * (i >> 3) + 4 * (i & 3) + 2 * ((i >> 2) & 1);
 }
 
-// Softmax weights of 16 N scores (raw products) of this lane's row against its reference, in pairs
-// rounded to bf16; their unrounded sum is returned.
+// Bits of the tokens base .. base + 31 that lie in [lo, hi) and in `exist`, moved down by `half`: bit
+// score_token(i) is register i's.
+__device__ __forceinline__ uint32_t seen_bits(uint32_t exist, int lo, int hi, int base, int half) {
+  lo = max(lo - base, 0);
+  hi = min(hi - base, 32);
+  const uint32_t range = lo < hi ? (0xffffffffu >> (32 - hi + lo)) << lo : 0u;
+  return (range & exist) >> half;
+}
+// A score whose token is not seen weighs nothing. (Bit operations on the score itself: compares
+// would hold a pair of scalar registers for each of 16 lane masks.)
+__device__ __forceinline__ void mask_scores(f32x16& s, uint32_t seen) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const uint32_t m = (uint32_t)((int32_t)(seen << (31 - score_token(i))) >> 31);
+    s[i] = __uint_as_float((__float_as_uint(s[i]) & m) | (0xff800000u & ~m));
+  }
+}
+// Softmax weights of 16 N scores (raw products) of this lane's row against a reference, in pairs
+// rounded to bf16; returns their unrounded sum.
 template <int N>
 __device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (&s)[N],
                                             float scale, float ref) {
-  const bool wide = __ballot(!(__builtin_fabsf(ref) <= kFused)) != 0;
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-      float x0 = __builtin_fmaf(s[j][i], scale, -ref);
-      float x1 = __builtin_fmaf(s[j][i + 1], scale, -ref);
-      if (wide) {
-        x0 = over_reference(s[j][i], scale, ref);
-        x1 = over_reference(s[j][i + 1], scale, ref);
-      }
-      const f32x2 p = {__builtin_amdgcn_exp2f(x0), __builtin_amdgcn_exp2f(x1)};
+      const f32x2 p = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i], scale, -ref)),
+                       __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i + 1], scale, -ref))};
       sum[i & 2] += p[0];
       sum[(i & 2) + 1] += p[1];
       pw[j][i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
     }
   return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+// The rare cases: rows without a reference, rows that outgrew theirs (both get the largest of these
+// scores, sum and output following), and references whose products would not stay in range
+// unrounded.
+template <int N, int NO>
+__device__ __forceinline__ float weights_moved(uint32_t (&pw)[N][8], f32x16 (&s)[N], float scale,
+                                               float& m_run, float& l_run, f32x16 (&o)[NO]) {
+  float cmax = s[0][0];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) cmax = fmaxf(cmax, s[j][i]);
+  cmax *= scale;
+  const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
+  // without a reference, sum and output are zero
+  const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
+  m_run = m_new;
+  l_run *= alpha;
+#pragma unroll
+  for (int n = 0; n < NO; ++n)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
+  const float ref = m_new == -INFINITY ? 0.f : m_new;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[j][i] = over_reference(s[j][i], scale, ref);
+  return weights_of<N>(pw, s, 1.f, 0.f);
+}
+// The weights of a row's next 16 N scores; its sum, and where need be its reference and output,
+// follow.
+template <int N, int NO>
+__device__ __forceinline__ void next_weights(uint32_t (&pw)[N][8], f32x16 (&s)[N], float scale,
+                                             float& m_run, float& l_run, f32x16 (&o)[NO]) {
+  float sum = 0.f;
+  bool rare = __ballot(!(__builtin_fabsf(m_run) <= kFused)) != 0;  // -inf: none yet
+  if (__builtin_expect(!rare, 1)) {
+    sum = weights_of<N>(pw, s, scale, m_run);
+    rare = __ballot(!(sum <= kWeightLimit)) != 0;
+  }
+  if (__builtin_expect(rare, 0)) sum = weights_moved<N, NO>(pw, s, scale, m_run, l_run, o);
+  l_run += sum;
 }
 
 // ---- grouped-query records -------------------------------------------------------------------
@@ -307,6 +368,9 @@ __device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (
 // order of mla_row are its P operands, and the row's reference, sum and limits are one register
 // each.
 
+// Tokens that do not exist are read from here.
+__device__ __attribute__((aligned(16))) uint8_t g_zero_row[1152];
+
 using GTile = Tile<32>;  // 32 tokens of 32 pieces: K 0..15, V 16..31
 
 // LDS of a workgroup, whichever its path: tiles, bad-token marks, the groups' (max, sum) pairs.
@@ -316,7 +380,7 @@ constexpr int kGroupedLds = kGroupedMl + 8 * 32 * 8;
 
 template <bool FP8, int RW, int TG, int CT>
 struct Grouped {
-  static constexpr int NB = RW == 1 ? 1 : 2;  // tile buffers (one wave alone needs one)
+  static constexpr int NB = RW == 8 ? 3 : RW == 1 ? 1 : 2;  // tile buffers
   static constexpr int NS = CT / 32;
   static constexpr int TILE = NS * GTile::BYTES;
   static constexpr int RGW = CT / 8 / RW;  // groups of eight rows that a wave stages
@@ -325,6 +389,9 @@ struct Grouped {
   static_assert(LDS_TILES <= kGroupedMarks && TG * NB * (CT + 1) * 4 <= kGroupedMl - kGroupedMarks,
                 "LDS");
   static_assert(RW * TG == 8 && CT % (8 * RW) == 0 && CT <= 64, "shape");
+
+  // 16-bit tiles of the widest path go to LDS directly
+  static constexpr bool DIRECT = RW == 8 && !FP8;
 
   struct Staged {
     u32x4 x[RGW][NLD];
@@ -345,28 +412,25 @@ struct Grouped {
     // ---- staging ----
     const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
     auto tile_base = [&](int it) { return v.t0 + (it * TG + tg) * CT; };
-    int32_t e[RGW], ev;  // table entries of the tile to load next, and of its token `lane`
-    auto entry = [&](int t) {
-      return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1;
-    };
+    int32_t e[RGW];  // table entries of this lane's rows of the tile to load next
+    int32_t ev;      // and of token `lane` of the tile whose scores come next
+    auto entry = [&](int t) { return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1; };
     auto load_entries = [&](int it) {
       const int base = tile_base(it);
 #pragma unroll
       for (int i = 0; i < RGW; ++i) e[i] = entry(base + 8 * (hg * RGW + i) + (lane >> 3));
-      ev = entry(base + (lane & (CT - 1)));
     };
+    auto mask_entry = [&](int it) { return entry(tile_base(it) + (lane & (CT - 1))); };
     Staged st;
-    uint64_t vmask = 0;  // of the staged tile: bit t, token t exists
     auto ok_entry = [&](int32_t r) { return r >= 0 && r < a.num_records; };
     auto issue = [&](int it) {
       const int base = tile_base(it);
-      vmask = __ballot(ok_entry(ev));
 #pragma unroll
       for (int i = 0; i < RGW; ++i) {
         const int t = base + 8 * (hg * RGW + i) + (lane >> 3);
         const int in = t & ((1 << a.l.tpr_shift) - 1);
-        const uint8_t* rec = v.pool + (int64_t)e[i] * a.record_stride;
-        const uint8_t* src = rec + in * a.l.row_bytes + 16 * (lane & 7);
+        const uint8_t* rec = v.pool + (uint64_t)(uint32_t)e[i] * (uint32_t)a.record_stride;
+        const uint8_t* src = rec + __umul24(in, a.l.row_bytes) + 16 * (lane & 7);
         if (ok_entry(e[i])) {
 #pragma unroll
           for (int x = 0; x < NLD; ++x)
@@ -381,6 +445,35 @@ struct Grouped {
       }
     };
     auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
+    auto mark_bad = [&](int it, int r) {
+      s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
+      s_bad[(it % NB) * (CT + 1)] = it + 1;
+    };
+    auto direct = [&](int it) {
+      static_assert(!DIRECT || RGW == 1, "a wave stages eight rows");
+      const int t = tile_base(it) + 8 * hg + (lane >> 3);
+      const int in = t & ((1 << a.l.tpr_shift) - 1);
+      const uint8_t* row = v.pool + (uint64_t)(uint32_t)e[0] * (uint32_t)a.record_stride +
+                           __umul24(in, a.l.row_bytes);
+      stage_rows<32>(s_tiles + (it % NB) * TILE + (hg >> 2) * GTile::BYTES, hg & 3,
+                     (ok_entry(e[0]) ? row : g_zero_row) + stage_piece(lane, hg));
+    };
+    // this wave's rows of a tile that was stored directly
+    auto scrub = [&](int it) {
+      const int r = 8 * hg + (lane >> 3);
+      bool bad = false;
+#pragma unroll
+      for (int x = 2; x < 4; ++x) {
+        u32x4* at = reinterpret_cast<u32x4*>(s_tiles + (it % NB) * TILE + (r >> 5) * GTile::BYTES +
+                                             GTile::row(r & 31) + x * 1024) + (lane & 7);
+        u32x4 p = *at;
+        if (clear_bad(p)) {
+          bad = true;
+          *at = p;
+        }
+      }
+      if (bad) mark_bad(it, r);
+    };
     auto store = [&](int it) {
       uint8_t* tile = s_tiles + (it % NB) * TILE;
       const bool part = partial(tile_base(it));
@@ -412,14 +505,12 @@ struct Grouped {
             *reinterpret_cast<u32x4*>(dst + x * 1024 + (((lane & 7) ^ sw) << 4)) = p;
           }
         }
-        if (part && bad) {
-          s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
-          s_bad[(it % NB) * (CT + 1)] = it + 1;
-        }
+        if (part && bad) mark_bad(it, r);
       }
     };
 
     load_entries(0);
+    ev = mask_entry(0);
     for (int i = lane + 64 * hg; i < NB * (CT + 1); i += 64 * RW) s_bad[i] = 0;
     // Q^T operand: this lane's row, dims 16 kk + 8 half .. +7
     bf16x8_t qreg[8];
@@ -434,129 +525,207 @@ struct Grouped {
 #pragma unroll
     for (int n = 0; n < 4; ++n) o[n] = f32x16{};
     float m_run = -INFINITY, l_run = 0.f;
-    uint64_t mask_now = 0;
-    if (n_it > 0) {
-      issue(0);
-      load_entries(1);
-      if (RW > 1 || TG > 1) __syncthreads();  // s_bad is clear
-      store(0);
-      mask_now = vmask;
-    }
 
-    for (int it = 0; it < n_it; ++it) {
-      if constexpr (RW > 1) __syncthreads();  // tile `it` is stored, tile it - 1 read by all
-      else __builtin_amdgcn_wave_barrier();
-      if (it + 1 < n_it) {
-        issue(it + 1);
-        load_entries(it + 2);
-      }
+    // ---- one tile's steps ----
+    auto busy = [&](int it) { return v.group_live && tile_base(it) < v.w_end; };
+    // S^T of a tile: K reads KD k-steps ahead of the MFMAs (see lds_read_b128)
+    auto scores = [&](int it, f32x16 (&s)[NS]) {
+      const int kr = mla_row(col), sw = tile_swizzle(kr);
+      const uint32_t krow = lds_addr(s_tiles + (it % NB) * TILE + GTile::row(kr));
+      uint32_t ka[4];  // piece 2 kk + half of k-steps kk, kk + 4
+#pragma unroll
+      for (int i = 0; i < 4; ++i) ka[i] = krow + (((2 * i + half) ^ sw) << 4);
+      constexpr int N = 8 * NS, KD = 8;  // read x: k-step x / NS of tokens 32 (x % NS) ..
+      u32x4 kb[KD];
+      auto kread = [&](auto x) {
+        constexpr int kk = x / NS, j = x % NS;
+        kb[x % KD] = lds_read_b128<j * GTile::BYTES + (kk / 4) * 1024>(ka[kk & 3]);
+      };
+      static_for<KD>(kread);
+      static_for<N>([&](auto x) {
+        constexpr int later = N - 1 - x < KD - 1 ? N - 1 - x : KD - 1;
+        constexpr int kk = x / NS, j = x % NS;
+        lgkm_wait1<later>(kb[x % KD]);
+        s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, kb[x % KD]),
+                                                      qreg[kk], kk == 0 ? f32x16{} : s[j], 0, 0,
+                                                      0);
+        if constexpr (x + KD < N) kread(std::integral_constant<int, x + KD>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    auto softmax = [&](int it, f32x16 (&s)[NS], uint64_t exist, uint32_t (&pw)[NS][8]) {
       const int base = tile_base(it);
-      if (v.group_live && base < v.w_end) {
-        const uint8_t* tile = s_tiles + (it % NB) * TILE;
-        f32x16 s[NS];
-        const int kr = mla_row(col), ksw = tile_swizzle(kr);
-#pragma unroll
-        for (int j = 0; j < NS; ++j) {
-          s[j] = f32x16{};
-          const uint8_t* krow = tile + j * GTile::BYTES + GTile::row(kr);
-#pragma unroll
-          for (int kk = 0; kk < 8; ++kk) {
-            const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
-                krow + (kk / 4) * 1024 + ((((2 * kk + half) & 7) ^ ksw) << 4));
-            s[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qreg[kk], s[j], 0, 0, 0);
-          }
-        }
-        constexpr uint64_t kFull = CT == 64 ? ~0ull : 0xffffffffull;
-        if (base + CT > v.w_hi || base < v.w_lo || (mask_now & kFull) != kFull) {
-          const int hi = v.row_hi - base - half, lo = v.row_lo - base - half;
-          const uint64_t m = mask_now >> half;
-#pragma unroll
-          for (int j = 0; j < NS; ++j)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const int t = 32 * j + score_token(i);
-              const bool seen = t < hi && t >= lo && ((m >> t) & 1);
-              s[j][i] = seen ? s[j][i] : -INFINITY;
-            }
-        }
-        float cmax = s[0][0];
+      constexpr uint64_t kFull = CT == 64 ? ~0ull : 0xffffffffull;
+      if (base + CT > v.w_hi || base < v.w_lo || (exist & kFull) != kFull) {
 #pragma unroll
         for (int j = 0; j < NS; ++j)
+          mask_scores(s[j], seen_bits((uint32_t)(exist >> (32 * j)), v.row_lo, v.row_hi,
+                                      base + 32 * j, half));
+      }
+      next_weights<NS, 4>(pw, s, a.scale_log2, m_run, l_run, o);
+    };
+    // O^T += V^T P^T. V by transpose reads: in each 16-lane group lane 4s + q addresses row 16 kb +
+    // 4s + half (+ 2 for the second read), dims 32 n + 16 (col >> 4) + 4q .. +3; lane t of the
+    // group then holds those rows of dim 32 n + 16 (col >> 4) + t, in P's token order.
+    auto pv = [&](int it, const uint32_t (&pw)[NS][8]) {
+      const int vr = 4 * ((lane & 15) >> 2) + half;
+      const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
+      const uint8_t* tile = s_tiles + (it % NB) * TILE;
+      uint32_t va[2][2];  // [n & 1][first / second read]
 #pragma unroll
-          for (int i = 0; i < 16; ++i) cmax = fmaxf(cmax, s[j][i]);
-        cmax *= a.scale_log2;
-        if (__ballot(cmax > m_run + kSlack || (m_run == -INFINITY && cmax > -INFINITY))) {
-          const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
-          const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-          m_run = m_new;
-          l_run *= alpha;
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          va[n][y] = lds_addr(tile + GTile::row(vr + 2 * y) + 8 * (lane & 1) +
+                              (((vp + 4 * n) ^ tile_swizzle(vr + 2 * y)) << 4));
+      constexpr int N = 8 * NS, VD = 6;  // MFMA x: tokens 16 (x / 4) .., dims 32 (x % 4) ..
+      v4i16 lo[VD], hi[VD];
+      auto vread = [&](auto x) {
+        constexpr int j = x / 8, kb = x / 4 % 2, n = x % 4;
+        constexpr int OFF = j * GTile::BYTES + kb * 2 * GTile::NSEG * 1024 + (2 + n / 2) * 1024;
+        lo[x % VD] = lds_read_tr16_b64<OFF>(va[n & 1][0]);
+        hi[x % VD] = lds_read_tr16_b64<OFF>(va[n & 1][1]);
+      };
+      static_for<VD>(vread);
+      static_for<N>([&](auto x) {
+        constexpr int later = N - 1 - x < VD - 1 ? N - 1 - x : VD - 1;
+        constexpr int j = x / 8, kb = x / 4 % 2, n = x % 4;
+        lgkm_wait2<2 * later>(lo[x % VD], hi[x % VD]);
+        const bf16x8_t vt = __builtin_bit_cast(
+            bf16x8_t, __builtin_shufflevector(lo[x % VD], hi[x % VD], 0, 1, 2, 3, 4, 5, 6, 7));
+        o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            vt, words(pw[j][4 * kb], pw[j][4 * kb + 1], pw[j][4 * kb + 2], pw[j][4 * kb + 3]),
+            o[n], 0, 0, 0);
+        if constexpr (x + VD < N) vread(std::integral_constant<int, x + VD>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      // Infinities and NaN in V of a tile that only some rows see were stored as zeros (zero
+      // weights would have made NaN of them): they go to the rows that see them here.
+      const int base = tile_base(it);
+      if (partial(base) &&
+          __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
+        for (int t = 0; t < CT; ++t) {
+          if (s_bad[(it % NB) * (CT + 1) + 1 + t] != it + 1) continue;
+          const int tk = base + t;
+          if (tk >= v.row_hi || tk < v.row_lo) continue;
+          const uint8_t* rec = v.pool + (int64_t)v.table[tk >> a.l.tpr_shift] * a.record_stride;
+          const int in = tk & ((1 << a.l.tpr_shift) - 1);
+          const uint8_t* vrow = rec + (int64_t)in * a.l.row_bytes + (FP8 ? 128 : 256);
+          float sc = 1.f;
+          if constexpr (FP8)
+            sc = reinterpret_cast<const float*>(rec + a.l.scale_offset)[2 * in + 1];
 #pragma unroll
           for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
-        }
-        const float ref = m_run == -INFINITY ? 0.f : m_run;
-        uint32_t pw[NS][8];
-        l_run += weights_of<NS>(pw, s, a.scale_log2, ref);
-        // V^T operand by transpose reads: in each 16-lane group lane 4s + q addresses row 16 kb +
-        // 4s + half (+ 2 for the second read), dims 32 n + 16 (col >> 4) + 4q .. +3; lane t of the
-        // group then holds those rows of dim 32 n + 16 (col >> 4) + t, in P's token order.
-        const int vr = 4 * ((lane & 15) >> 2) + half;
-        const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
-#pragma unroll
-        for (int j = 0; j < NS; ++j)
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb) {
-            const bf16x8_t p =
-                words(pw[j][4 * kb], pw[j][4 * kb + 1], pw[j][4 * kb + 2], pw[j][4 * kb + 3]);
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-              auto vread = [&](int y) {
-                const int r = vr + 2 * y;  // + 16 kb: two row groups further
-                const uint8_t* at = tile + j * GTile::BYTES + GTile::row(r) + kb * 2 * 4096 +
-                                    (2 + n / 2) * 1024 +
-                                    (((vp + 4 * (n & 1)) ^ tile_swizzle(r)) << 4) + 8 * (lane & 1);
-                return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (lds_v4i16*)const_cast<uint8_t*>(at));
-              };
-              const bf16x8_t vt = __builtin_bit_cast(
-                  bf16x8_t,
-                  __builtin_shufflevector(vread(0), vread(1), 0, 1, 2, 3, 4, 5, 6, 7));
-              o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p, o[n], 0, 0, 0);
+            for (int i = 0; i < 16; ++i) {
+              const int d = 32 * n + 8 * (i >> 2) + 4 * half + (i & 3);
+              float x;
+              if constexpr (FP8) x = __builtin_amdgcn_cvt_f32_fp8(vrow[d], 0) * sc;
+              else x = bf16_to_f32(reinterpret_cast<const uint16_t*>(vrow)[d]);
+              o[n][i] += if_not_finite(x);
+              if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // few loads at a time
             }
-          }
-        // Infinities and NaN in V of a tile that only some rows see were stored as zeros (zero
-        // weights would have made NaN of them): they go to the rows that see them here.
-        if (partial(base) &&
-            __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
-          for (int t = 0; t < CT; ++t) {
-            if (s_bad[(it % NB) * (CT + 1) + 1 + t] != it + 1) continue;
-            const int tk = base + t;
-            if (tk >= v.row_hi || tk < v.row_lo) continue;
-            const uint8_t* rec =
-                v.pool + (int64_t)v.table[tk >> a.l.tpr_shift] * a.record_stride;
-            const int in = tk & ((1 << a.l.tpr_shift) - 1);
-            const uint8_t* vrow = rec + (int64_t)in * a.l.row_bytes + (FP8 ? 128 : 256);
-            float sc = 1.f;
-            if constexpr (FP8)
-              sc = reinterpret_cast<const float*>(rec + a.l.scale_offset)[2 * in + 1];
-#pragma unroll
-            for (int n = 0; n < 4; ++n)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                const int d = 32 * n + 8 * (i >> 2) + 4 * half + (i & 3);
-                float x;
-                if constexpr (FP8) x = __builtin_amdgcn_cvt_f32_fp8(vrow[d], 0) * sc;
-                else x = bf16_to_f32(reinterpret_cast<const uint16_t*>(vrow)[d]);
-                if (!(__builtin_fabsf(x) <= 3.3895314e38f)) o[n][i] += x;
-              }
-          }
         }
       }
-      if (it + 1 < n_it) {
-        if constexpr (RW == 1) __builtin_amdgcn_wave_barrier();
-        store(it + 1);
-        mask_now = vmask;
+    };
+    f32x16 s[NS];
+    uint32_t pw[NS][8];
+
+    if constexpr (RW == 8) {
+      // The two waves of a SIMD (w and w + 4) take turns: while one's MFMAs run (V of tile i - 1,
+      // scores of tile i) the other works out its softmax and stages, a barrier apart. Waves 4..7
+      // are half a tile behind, so they stage a tile further ahead. Tile t is read until the
+      // second MFMA phase of t + 1; three buffers.
+      // By way of registers, tile t is stored in the softmax phase before its first reader's
+      // MFMAs. Directly, it is sent for in the slot in which its buffer comes free: by waves 0..3
+      // as their MFMA phase begins, by 4..7 a softmax phase earlier.
+      const int lead = wave >= 4 ? 2 : 1;
+      if (n_it > 0) {
+        if constexpr (DIRECT) {
+          direct(0);
+          load_entries(1);
+          if (lead == 2) {
+            if (n_it > 1) direct(1);
+            load_entries(2);
+          }
+          wait_loads_and_barrier<0>();
+          // the query too: a wait for it inside the loop would drain the tiles in flight
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk) asm volatile("" : "+v"(qreg[kk]));
+          if (lead == 2 && partial(tile_base(0))) scrub(0);
+        } else {
+          issue(0);
+          load_entries(1);
+          lds_barrier();  // s_bad is clear
+          store(0);
+          if (lead == 2 && n_it > 1) {
+            issue(1);
+            load_entries(2);
+            store(1);
+          }
+          if (lead < n_it) issue(lead);
+          load_entries(lead + 1);
+          lds_barrier();  // tile 0 is stored
+        }
+        if (lead == 2) lds_barrier();
+        for (int i = 0; i <= n_it; ++i) {
+          if (DIRECT && lead == 1) {
+            if (i + 1 < n_it) direct(i + 1);
+            load_entries(i + 2);
+          }
+          if (i > 0 && busy(i - 1)) pv(i - 1, pw);
+          if (i < n_it && busy(i)) scores(i, s);
+          if (DIRECT && lead == 2) wait_loads_and_barrier<0>();  // tile i + 1 is here
+          else lds_barrier();
+          if (i < n_it) {
+            const uint64_t exist = __ballot(ok_entry(ev));
+            if constexpr (DIRECT) {
+              if (lead == 2) {
+                if (i + 2 < n_it) direct(i + 2);
+                load_entries(i + 3);
+              }
+              const int t = i + lead - 1;
+              if (t < n_it && partial(tile_base(t))) scrub(t);
+            }
+            ev = mask_entry(i + 1);
+            if (busy(i)) softmax(i, s, exist, pw);
+            if constexpr (!DIRECT) {
+              if (i + lead < n_it) {
+                store(i + lead);
+                if (i + lead + 1 < n_it) issue(i + lead + 1);
+                load_entries(i + lead + 2);
+              }
+            }
+          }
+          if (DIRECT && lead == 1) wait_loads_and_barrier<0>();
+          else lds_barrier();
+        }
+        if (lead == 1) lds_barrier();
+      }
+    } else {
+      if (n_it > 0) {
+        issue(0);
+        load_entries(1);
+        lds_barrier();  // s_bad is clear
+        store(0);
+      }
+      for (int it = 0; it < n_it; ++it) {
+        // tile `it` is stored, tile it - 1 read by all (one wave alone: in its own order)
+        if constexpr (RW > 1) lds_barrier();
+        else asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const uint64_t exist = __ballot(ok_entry(ev));
+        ev = mask_entry(it + 1);
+        if (it + 1 < n_it) {
+          issue(it + 1);
+          load_entries(it + 2);
+        }
+        if (busy(it)) {
+          scores(it, s);
+          softmax(it, s, exist, pw);
+          pv(it, pw);
+        }
+        asm volatile("" ::: "memory");
+        if (it + 1 < n_it) store(it + 1);
       }
     }
     l_run += __shfl_xor(l_run, 32, 64);
@@ -714,8 +883,8 @@ struct Latent {
       const int t = tile_base(it) + 8 * srg + (lane >> 3);
       const int in = t & ((1 << a.l.tpr_shift) - 1);
       vmask = (uint32_t)__ballot(ok_entry(ev));
-      const uint8_t* rec = v.pool + (int64_t)e * a.record_stride;
-      const uint8_t* src = rec + (int64_t)in * a.l.row_bytes + 16 * (lane & 7) + 128 * seg0;
+      const uint8_t* rec = v.pool + (uint64_t)(uint32_t)e * (uint32_t)a.record_stride;
+      const uint8_t* src = rec + __umul24(in, a.l.row_bytes) + 16 * (lane & 7) + 128 * seg0;
 #pragma unroll
       for (int x = 0; x < NLD; ++x) st[x] = u32x4{};
       st_scale = 1.f;
@@ -838,31 +1007,10 @@ struct Latent {
           for (int i = 0; i < 4; ++i) s[0][4 * x + i] = y[i];
         }
         if (base + CT > v.w_hi || base < v.w_lo || mask_now != 0xffffffffu) {
-          const int hi = v.row_hi - base - half, lo = v.row_lo - base - half;
-          const uint32_t m = mask_now >> half;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int t = score_token(i);
-            const bool seen = t < hi && t >= lo && ((m >> t) & 1);
-            s[0][i] = seen ? s[0][i] : -INFINITY;
-          }
-        }
-        float cmax = s[0][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) cmax = fmaxf(cmax, s[0][i]);
-        cmax *= a.scale_log2;
-        if (__ballot(cmax > m_run + kSlack || (m_run == -INFINITY && cmax > -INFINITY))) {
-          const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
-          const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
-          m_run = m_new;
-          l_run *= alpha;
-#pragma unroll
-          for (int n = 0; n < NO; ++n)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
+          mask_scores(s[0], seen_bits(mask_now, v.row_lo, v.row_hi, base, half));
         }
         uint32_t pw[1][8];
-        l_run += weights_of<1>(pw, s, a.scale_log2, m_run == -INFINITY ? 0.f : m_run);
+        next_weights<1, NO>(pw, s, a.scale_log2, m_run, l_run, o);
         // V^T operand by transpose reads, as in Grouped; dims 32 (NO ds + n) are pieces 4 (NO ds +
         // n) .., segment (NO ds + n) / 2
         const int vr = 4 * ((lane & 15) >> 2) + half;

@@ -255,11 +255,10 @@ hisparse_status_t hisparse_validate_kv(const hisparse_kv_desc_t* d) {
   if (d->type == HISPARSE_KV_BF16 && d->record_bytes % (16 * d->tokens_per_record) != 0)
     return HISPARSE_ERR_INVALID_ARG;
   if (d->num_records < 1 || d->num_records > 0x7FFFFFFFLL) return HISPARSE_ERR_INVALID_ARG;
-  if (d->record_stride < d->record_bytes || d->record_stride % 16 != 0 || d->head_stride < 0 ||
+  if (d->record_stride < d->record_bytes || d->record_stride > INT32_MAX ||
+      d->record_stride % 16 != 0 || d->head_stride < 0 ||
       d->head_stride % 16 != 0 || d->request_stride < 0 || d->request_stride % 16 != 0)
     return HISPARSE_ERR_INVALID_ARG;
-  // offsets stay inside 64 bits
-  if ((double)d->num_records * d->record_stride > 4.0e18) return HISPARSE_ERR_INVALID_ARG;
   return HISPARSE_OK;
 }
 
