@@ -143,19 +143,6 @@ __device__ inline float add_weights(uint32_t w, float sum) {
   const bf16x2_t ones = {(__bf16)1.0f, (__bf16)1.0f};
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, w), ones, sum, false);
 }
-// S^T += K . Q^T for one k-step once the K rows' read (with at most N later LDS reads) is in;
-// the first step of a chain (FIRST) starts from zero. The s_nop covers the wait states after a
-// just-written operand that the compiler does not see through the assembly.
-template <int N, bool FIRST>
-__device__ __forceinline__ void mfma_qk(f32x16& acc, const u32x4& k, const bf16x8_t& q) {
-  if constexpr (FIRST)
-    asm volatile("s_waitcnt lgkmcnt(%3)\n\ts_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0"
-                 : "=&v"(acc) : "v"(k), "v"(q), "n"(N));
-  else
-    asm volatile("s_waitcnt lgkmcnt(%3)\n\ts_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
-                 : "+v"(acc) : "v"(k), "v"(q), "n"(N));
-}
-
 // Row order of a 16-token group inside the MFMA tiles: operand row m reads token
 // tile_row(m) = 4 (m & 3) + (m >> 2). A lane's S^T accumulator then holds tokens tile_row(4g + j)
 // (+16), and the four rows of a PV transpose read are 4 apart, which the swizzle spreads over

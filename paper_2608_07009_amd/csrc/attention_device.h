@@ -87,6 +87,19 @@ __device__ __forceinline__ void lgkm_wait1(u32x4& a) {
   asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(N));
 }
 
+// S^T += K . Q^T for one k-step once the K rows' read (with at most N later LDS reads) is in;
+// the first step of a chain (FIRST) starts from zero. The s_nop covers the wait states after a
+// just-written operand that the compiler does not see through the assembly.
+template <int N, bool FIRST>
+__device__ __forceinline__ void mfma_qk(f32x16& acc, const u32x4& k, const bf16x8_t& q) {
+  if constexpr (FIRST)
+    asm volatile("s_waitcnt lgkmcnt(%3)\n\ts_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0"
+                 : "=&v"(acc) : "v"(k), "v"(q), "n"(N));
+  else
+    asm volatile("s_waitcnt lgkmcnt(%3)\n\ts_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0"
+                 : "+v"(acc) : "v"(k), "v"(q), "n"(N));
+}
+
 // Wait until at most N direct-to-LDS loads of this wave are outstanding and its LDS writes are
 // done, then synchronise the workgroup. (A workgroup fence would also drain the younger
 // prefetches, which is exactly what the pipeline must not do.)

@@ -313,19 +313,35 @@ __device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (
     }
   return (sum[0] + sum[1]) + (sum[2] + sum[3]);
 }
+// The largest of a row's 16 N scores on its two lanes, times the scale.
+template <int N>
+__device__ __forceinline__ float largest(const f32x16 (&s)[N], float scale) {
+  float c = s[0][0];
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) c = fmaxf(c, s[j][i]);
+  c *= scale;
+  return fmaxf(c, __shfl_xor(c, 32, 64));
+}
+// Weights against a reference whose products would not stay in range unrounded, or none (-inf).
+template <int N>
+__device__ __forceinline__ float weights_rounded(uint32_t (&pw)[N][8], f32x16 (&s)[N],
+                                                 float scale, float ref) {
+  if (ref == -INFINITY) ref = 0.f;
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[j][i] = over_reference(s[j][i], scale, ref);
+  return weights_of<N>(pw, s, 1.f, 0.f);
+}
 // The rare cases: rows without a reference, rows that outgrew theirs (both get the largest of these
 // scores, sum and output following), and references whose products would not stay in range
 // unrounded.
 template <int N, int NO>
 __device__ __forceinline__ float weights_moved(uint32_t (&pw)[N][8], f32x16 (&s)[N], float scale,
                                                float& m_run, float& l_run, f32x16 (&o)[NO]) {
-  float cmax = s[0][0];
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) cmax = fmaxf(cmax, s[j][i]);
-  cmax *= scale;
-  const float m_new = fmaxf(m_run, fmaxf(cmax, __shfl_xor(cmax, 32, 64)));
+  const float m_new = fmaxf(m_run, largest<N>(s, scale));
   // without a reference, sum and output are zero
   const float alpha = m_run == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - m_new);
   m_run = m_new;
@@ -334,12 +350,7 @@ __device__ __forceinline__ float weights_moved(uint32_t (&pw)[N][8], f32x16 (&s)
   for (int n = 0; n < NO; ++n)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[n][i] *= alpha;
-  const float ref = m_new == -INFINITY ? 0.f : m_new;
-#pragma unroll
-  for (int j = 0; j < N; ++j)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[j][i] = over_reference(s[j][i], scale, ref);
-  return weights_of<N>(pw, s, 1.f, 0.f);
+  return weights_rounded<N>(pw, s, scale, m_new);
 }
 // The weights of a row's next 16 N scores; its sum, and where need be its reference and output,
 // follow.
@@ -824,127 +835,120 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
 
 // ---- latent records --------------------------------------------------------------------------
 //
-// Eight waves: RG groups of 32 rows, times DS waves that share a group's rows, times TG token
-// groups. A tile is 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the value is
-// the latent part). Of the DS waves of a row group, wave d
+// Four waves, one per SIMD with all of its registers: RG groups of 32 rows, times DS waves that share
+// a group's rows. A tile is 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the
+// value is the latent part). Of the DS waves of a row group, wave d
 //   adds up the k-steps kk = d mod DS of the scores, which are then summed through LDS,
-//   and keeps the output dims 512 / DS d .. of its rows;
-// so the query and the output of 32 rows, 144 and 256 registers a lane, are spread over DS waves,
-// and a tile is read from LDS once per row group, not once per wave. The softmax is worked out by
-// each of the DS waves.
+//   and keeps the output dims 512 / DS d .. of its rows,
+// so that few rows still spread over four waves. The output (256 / DS registers a lane) lives in
+// accumulation registers; the score MFMAs are assembly so that theirs do not (see mfma_qk).
+// Nothing but MFMAs touches the output: a row's reference stays the largest score of the first tile
+// that it sees. If some row's weights outgrow the range (kWeightLimit), the workgroup goes over its
+// tokens twice more: for every row's largest score, then for the result against those.
+// 16-bit tiles are stored by direct loads NB - 1 tiles ahead, 8-bit ones widened by way of registers
+// one tile ahead; either is done in the shadow of the score MFMAs.
 
 using LTile = Tile<72>;
 
-template <bool FP8, int RG, int DS, int TG>
+template <bool FP8, int RG, int DS>
 struct Latent {
   static constexpr int CT = 32;
-  static constexpr int NB = TG == 1 ? 2 : 1;   // tile buffers
-  static constexpr int GW = RG * DS;           // waves of a token group
-  static constexpr int SPLIT = GW / 4;         // waves that share a group of eight rows in staging
+  static constexpr int NB = FP8 ? 2 : 3;       // tile buffers
   static constexpr int NQ = 36 / DS;           // k-steps of a wave
   static constexpr int NO = 16 / DS;           // its output tiles of 32 dims
-  static constexpr int NLD = FP8 ? 4 / SPLIT + 1 : (9 + SPLIT - 1) / SPLIT;  // 16-byte loads
-  static_assert(RG * DS * TG == 8 && (SPLIT == 1 || SPLIT == 2), "shape");
-  // LDS: tiles, partial scores, bad-token marks; at the end the token groups' outputs and (max, sum)
-  static constexpr int SCORES = TG * NB * LTile::BYTES;
-  static constexpr int MARKS = SCORES + 8 * 4096;
-  static constexpr int ML = 8 * NO * 4 * 1024;
-  static constexpr int LDS = std::max(MARKS + TG * NB * (CT + 1) * 4, TG > 1 ? ML + 8 * 32 * 8 : 0);
+  static constexpr int NBASE = 4 / DS;         // its K operand addresses
+  static_assert(RG * DS == 4, "shape");
+  static constexpr int SCORES = NB * LTile::BYTES;  // LDS offsets
+  static constexpr int MARKS = SCORES + (DS > 1 ? 4 * 4096 : 0);
+  static constexpr int LDS = MARKS + NB * (CT + 1) * 4 + 4;
 
   static __device__ __forceinline__ void run(const ChunkArgs& a, const Work& w, int h,
                                              uint8_t* s_mem) {
     const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tg = wave / GW, in_group = wave % GW, rg = in_group / DS, ds = in_group % DS;
-    uint8_t* s_tiles = s_mem + tg * NB * LTile::BYTES;
-    f32x4* s_scores = reinterpret_cast<f32x4*>(s_mem + SCORES) + (tg * GW + rg * DS) * 256;
-    int* s_bad = reinterpret_cast<int*>(s_mem + MARKS) + tg * NB * (CT + 1);
+    const int rg = wave / DS, ds = wave % DS;
+    f32x4* s_scores = reinterpret_cast<f32x4*>(s_mem + SCORES) + rg * DS * 256;
+    int* s_bad = reinterpret_cast<int*>(s_mem + MARKS);
     const View v = view_of<32 * RG>(a, w, h, rg, col);
+    const int n_it = max(0, v.t1 - v.t0 + CT - 1) / CT;
+    auto tile_base = [&](int it) { return v.t0 + it * CT; };
+    auto tile_at = [&](int it) { return s_mem + (it % NB) * LTile::BYTES; };
+    auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
 
-    // ---- staging: wave in_group stages rows 8 (in_group / SPLIT) .., part in_group % SPLIT ----
-    const int srg = in_group / SPLIT, spart = in_group % SPLIT;
-    const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
-    auto tile_base = [&](int it) { return v.t0 + (it * TG + tg) * CT; };
+    // ---- staging: a wave stages eight rows of a tile ----
     auto entry = [&](int t) { return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1; };
     auto ok_entry = [&](int32_t r) { return r >= 0 && r < a.num_records; };
-    int32_t e, ev;  // table entries of this lane's row of the tile to load next, of its token
-    auto load_entries = [&](int it) {
-      const int base = tile_base(it);
-      e = entry(base + 8 * srg + (lane >> 3));
-      ev = entry(base + (lane & (CT - 1)));
-    };
-    u32x4 st[NLD];
+    int32_t e;   // table entry of this lane's row of the tile to load next
+    int32_t ev;  // and of token `lane` of the tile whose scores come next
+    auto load_entry = [&](int it) { e = entry(tile_base(it) + 8 * wave + (lane >> 3)); };
+    auto mask_entry = [&](int it) { return entry(tile_base(it) + col); };
+    const uint8_t* src = nullptr;  // this lane's row of the next tile (direct), its record (8-bit)
+    u32x4 st[5];
     float st_scale = 1.f;
-    uint32_t vmask = 0;
-    // bf16: segments of 8 pieces: all nine, or 0..3 and 4..8. 8-bit: payload segments 0..3 and the
-    // rotary one, or 0, 1 and 2, 3 with the rotary one.
-    const int seg0 = SPLIT == 1 ? 0 : FP8 ? 2 * spart : 4 * spart;
-    auto issue = [&](int it) {
-      const int t = tile_base(it) + 8 * srg + (lane >> 3);
-      const int in = t & ((1 << a.l.tpr_shift) - 1);
-      vmask = (uint32_t)__ballot(ok_entry(ev));
-      const uint8_t* rec = v.pool + (uint64_t)(uint32_t)e * (uint32_t)a.record_stride;
-      const uint8_t* src = rec + __umul24(in, a.l.row_bytes) + 16 * (lane & 7) + 128 * seg0;
-#pragma unroll
-      for (int x = 0; x < NLD; ++x) st[x] = u32x4{};
-      st_scale = 1.f;
-      if (ok_entry(e)) {
-        if constexpr (FP8) {
-#pragma unroll
-          for (int x = 0; x < NLD - 1; ++x)
-            st[x] = *reinterpret_cast<const u32x4*>(src + 128 * x);
-          if (SPLIT == 1 || spart == 1)
-            st[NLD - 1] = *reinterpret_cast<const u32x4*>(rec + a.l.rope_offset + 128 * in +
-                                                          16 * (lane & 7));
-          st_scale = *reinterpret_cast<const float*>(rec + a.l.scale_offset + 4 * in);
-        } else {
-#pragma unroll
-          for (int x = 0; x < NLD; ++x)
-            if (seg0 + x < (SPLIT == 1 || spart == 1 ? 9 : 4))
-              st[x] = *reinterpret_cast<const u32x4*>(src + 128 * x);
-        }
-      }
+    auto mark_bad = [&](int it, int r) {
+      s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
+      s_bad[(it % NB) * (CT + 1)] = it + 1;
     };
-    auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
-    auto store = [&](int it) {
-      const int r = 8 * srg + (lane >> 3), sw = tile_swizzle(r);
-      uint8_t* dst = s_tiles + (it % NB) * LTile::BYTES + LTile::row(r);
-      const bool part = partial(tile_base(it));
-      bool bad = false;
-      if constexpr (FP8) {
+    auto in_record = [&](int it) {
+      return (tile_base(it) + 8 * wave + (lane >> 3)) & ((1 << a.l.tpr_shift) - 1);
+    };
+    auto record = [&]() {
+      return v.pool + (uint64_t)(uint32_t)e * (uint32_t)a.record_stride;
+    };
+    auto find_row = [&](int it) {
+      src = (ok_entry(e) ? record() + __umul24(in_record(it), a.l.row_bytes) : g_zero_row) +
+            stage_piece(lane, wave);
+    };
+    auto direct = [&](auto seg, int it) { stage_block<72, seg>(tile_at(it), wave, src); };
+    auto load8 = [&](int it) {
+      const int in = in_record(it);
+      const uint8_t* rec = record();
+      if (ok_entry(e)) {
 #pragma unroll
-        for (int x = 0; x < NLD - 1; ++x) {
-          u32x4 p0 = widen(st[x][0], st[x][1], st_scale);
-          u32x4 p1 = widen(st[x][2], st[x][3], st_scale);
-          if (part) {
-            bad |= clear_bad(p0);
-            bad |= clear_bad(p1);
-          }
-          uint8_t* seg = dst + (2 * (seg0 + x) + ((lane & 7) >> 2)) * 1024;
-          const int p = 2 * (lane & 3);
-          *reinterpret_cast<u32x4*>(seg + ((p ^ sw) << 4)) = p0;
-          *reinterpret_cast<u32x4*>(seg + (((p + 1) ^ sw) << 4)) = p1;
-        }
-        if (SPLIT == 1 || spart == 1)
-          *reinterpret_cast<u32x4*>(dst + 8 * 1024 + (((lane & 7) ^ sw) << 4)) = st[NLD - 1];
+        for (int x = 0; x < 4; ++x)
+          st[x] = *reinterpret_cast<const u32x4*>(rec + 512 * in + 128 * x + 16 * (lane & 7));
+        st[4] = *reinterpret_cast<const u32x4*>(rec + a.l.rope_offset + 128 * in +
+                                                16 * (lane & 7));
+        st_scale = *reinterpret_cast<const float*>(rec + a.l.scale_offset + 4 * in);
       } else {
 #pragma unroll
-        for (int x = 0; x < NLD; ++x) {
-          const int seg = seg0 + x;
-          if (seg < (SPLIT == 1 || spart == 1 ? 9 : 4)) {
-            if (part && seg < 8) bad |= clear_bad(st[x]);
-            *reinterpret_cast<u32x4*>(dst + seg * 1024 + (((lane & 7) ^ sw) << 4)) = st[x];
-          }
-        }
-      }
-      if (part && bad) {
-        s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
-        s_bad[(it % NB) * (CT + 1)] = it + 1;
+        for (int x = 0; x < 5; ++x) st[x] = u32x4{};
+        st_scale = 1.f;
       }
     };
+    // piece 0..7: eight latent dims of this lane's row, 8: its rotary dims
+    auto store8 = [&](auto piece, int it) {
+      const int r = 8 * wave + (lane >> 3), sw = tile_swizzle(r);
+      uint8_t* dst = tile_at(it) + LTile::row(r);
+      if constexpr (piece == 8) {
+        *reinterpret_cast<u32x4*>(dst + 8 * 1024 + (((lane & 7) ^ sw) << 4)) = st[4];
+      } else {
+        constexpr int x = piece / 2, y = piece % 2;
+        u32x4 p = widen(st[x][2 * y], st[x][2 * y + 1], st_scale);
+        if (partial(tile_base(it)) && clear_bad(p)) mark_bad(it, r);
+        *reinterpret_cast<u32x4*>(dst + (2 * x + ((lane & 7) >> 2)) * 1024 +
+                                  (((2 * (lane & 3) + y) ^ sw) << 4)) = p;
+      }
+    };
+    // this wave's rows of a tile that was stored directly
+    auto scrub = [&](int it) {
+      const int r = 8 * wave + (lane >> 3);
+      bool bad = false;
+      for (int x = 0; x < 8; ++x) {
+        u32x4* at = reinterpret_cast<u32x4*>(tile_at(it) + LTile::row(r) + x * 1024) + (lane & 7);
+        u32x4 p = *at;
+        if (clear_bad(p)) {
+          bad = true;
+          *at = p;
+        }
+      }
+      if (bad) mark_bad(it, r);
+    };
 
-    load_entries(0);
-    for (int i = lane + 64 * in_group; i < NB * (CT + 1); i += 64 * GW) s_bad[i] = 0;
+    load_entry(0);
+    ev = mask_entry(0);
+    for (int i = threadIdx.x; i < NB * (CT + 1) + 1; i += 256) s_bad[i] = 0;
+    int* s_outgrown = s_bad + NB * (CT + 1);
     // Q^T operand of k-steps kk = DS i + ds: dims 16 kk + 8 half .. +7 of this lane's row
     bf16x8_t qreg[NQ];
     {
@@ -955,48 +959,80 @@ struct Latent {
             bf16x8_t,
             (u32x4)*reinterpret_cast<const any_u32x4*>(q + 16 * (DS * i + ds) + 8 * half));
     }
-    f32x16 o[NO];
-#pragma unroll
-    for (int n = 0; n < NO; ++n) o[n] = f32x16{};
-    float m_run = -INFINITY, l_run = 0.f;
-    uint32_t mask_now = 0;
-    if (n_it > 0) {
-      issue(0);
-      load_entries(1);
-      __syncthreads();  // s_bad is clear
-      store(0);
-      mask_now = vmask;
-    }
-
-    for (int it = 0; it < n_it; ++it) {
-      __syncthreads();  // tile `it` is stored; with two buffers, tile it - 1 is read by all
-      if (it + 1 < n_it) {
-        issue(it + 1);
-        load_entries(it + 2);
-      }
-      const int base = tile_base(it);
-      const uint8_t* tile = s_tiles + (it % NB) * LTile::BYTES;
-      const bool busy = v.group_live && base < v.w_end;
-      f32x16 s[1];
-      if (busy) {
-        // K piece 2 kk + half of k-step DS i + ds: for DS 4 segment i, for DS 2 segment i / 2
-        const int kr = mla_row(col), ksw = tile_swizzle(kr);
-        const uint8_t* krow = tile + LTile::row(kr);
-        s[0] = f32x16{};
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-          const int p = DS == 4 ? 2 * ds + half : 4 * (i & 1) + 2 * ds + half;
-          const bf16x8_t k = *reinterpret_cast<const bf16x8_t*>(
-              krow + (DS == 4 ? i : i / 2) * 1024 + ((p ^ ksw) << 4));
-          s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, qreg[i], s[0], 0, 0, 0);
+    // the first tiles on their way, from the entries of tile 0 on
+    auto begin = [&]() {
+      if constexpr (FP8) {
+        load8(0);
+        load_entry(1);
+        lds_barrier();  // s_bad is clear
+        static_for<9>([&](auto p) { store8(p, 0); });
+        if (n_it > 1) load8(1);
+        load_entry(2);
+      } else {
+        find_row(0);
+        static_for<9>([&](auto p) { direct(p, 0); });
+        load_entry(1);
+        if (n_it > 1) {
+          find_row(1);
+          static_for<9>([&](auto p) { direct(p, 1); });
         }
+        load_entry(2);
+        lds_barrier();  // s_bad is clear
+      }
+    };
+    // Scores of tile `it` for every row of the wave (a row that sees none of it, or does not exist,
+    // has them masked later or never stored), the next tile's staging in the MFMAs' shadow.
+    auto scores = [&](int it, f32x16& sum, uint32_t& exist) {
+      // tile `it` is stored, and tile it - 1 read, by every wave
+      if constexpr (!FP8) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (partial(tile_base(it))) scrub(it);
+      }
+      lds_barrier();
+      exist = (uint32_t)__ballot(ok_entry(ev));
+      ev = mask_entry(it + 1);
+      const int ahead = FP8 ? it + 1 : it + 2;  // the tile to store next
+      const bool more = ahead < n_it;
+      if constexpr (!FP8) {
+        if (more) find_row(ahead);
+      }
+      const int kr = mla_row(col), sw = tile_swizzle(kr);
+      const uint32_t krow = lds_addr(tile_at(it) + LTile::row(kr));
+      uint32_t ka[NBASE];  // piece 2 kk + half of k-steps kk = DS i + ds, i mod NBASE
+#pragma unroll
+      for (int i = 0; i < NBASE; ++i) ka[i] = krow + (((2 * (DS * i + ds) + half) ^ sw) << 4);
+      constexpr int KD = 4, EVERY = 4 / DS;
+      u32x4 kb[KD];
+      auto kread = [&](auto i) {
+        kb[i % KD] = lds_read_b128<(i / NBASE) * 1024>(ka[i % NBASE]);
+      };
+      f32x16 even, odd;  // two chains of MFMAs
+      static_for<KD>(kread);
+      static_for<NQ>([&](auto i) {
+        constexpr int later = NQ - 1 - i < KD - 1 ? NQ - 1 - i : KD - 1;
+        mfma_qk<later, (i < 2)>((i & 1) ? odd : even, kb[i % KD], qreg[i]);
+        if constexpr (i % EVERY == 0) {
+          constexpr std::integral_constant<int, i / EVERY> piece{};
+          if (more) {
+            if constexpr (FP8) store8(piece, ahead);
+            else direct(piece, ahead);
+          }
+        }
+        if constexpr (i + KD < NQ) kread(std::integral_constant<int, i + KD>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" : "+v"(even), "+v"(odd));
+      sum = even + odd;
+      if constexpr (FP8) {
+        if (it + 2 < n_it) load8(it + 2);
+      }
+      load_entry(it + 3);
+      if constexpr (DS > 1) {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           s_scores[ds * 256 + x * 64 + lane] =
-              f32x4{s[0][4 * x], s[0][4 * x + 1], s[0][4 * x + 2], s[0][4 * x + 3]};
-      }
-      __syncthreads();  // every wave's part of the scores is there
-      if (busy) {
+              f32x4{sum[4 * x], sum[4 * x + 1], sum[4 * x + 2], sum[4 * x + 3]};
+        lds_barrier();  // every wave's part of the scores is there
         // summed in the same order by every wave, so that they agree on every bit
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -1004,128 +1040,152 @@ struct Latent {
 #pragma unroll
           for (int d = 1; d < DS; ++d) y += s_scores[d * 256 + x * 64 + lane];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[0][4 * x + i] = y[i];
+          for (int i = 0; i < 4; ++i) sum[4 * x + i] = y[i];
         }
-        if (base + CT > v.w_hi || base < v.w_lo || mask_now != 0xffffffffu) {
-          mask_scores(s[0], seen_bits(mask_now, v.row_lo, v.row_hi, base, half));
-        }
-        uint32_t pw[1][8];
-        next_weights<1, NO>(pw, s, a.scale_log2, m_run, l_run, o);
+      }
+      const int base = tile_base(it);
+      if (base + CT > v.w_hi || base < v.w_lo || exist != 0xffffffffu)
+        mask_scores(sum, seen_bits(exist, v.row_lo, v.row_hi, base, half));
+    };
+
+    f32x16 o[NO];
+    float m_run = -INFINITY, l_run = 0.f;
+    if (n_it > 0) {
+      begin();
+      // a wait for the query inside the loop would drain the tiles in flight
+#pragma unroll
+      for (int i = 0; i < NQ; ++i) asm volatile("" : "+v"(qreg[i]));
+    }
+    for (int attempt = 0;; ++attempt) {
+#pragma unroll
+      for (int n = 0; n < NO; ++n) {
+        o[n] = f32x16{};
+        asm volatile("" : "+a"(o[n]));
+      }
+      l_run = 0.f;
+      for (int it = 0; it < n_it; ++it) {
+        f32x16 s[1];
+        uint32_t exist;
+        scores(it, s[0], exist);
         // V^T operand by transpose reads, as in Grouped; dims 32 (NO ds + n) are pieces 4 (NO ds +
         // n) .., segment (NO ds + n) / 2
         const int vr = 4 * ((lane & 15) >> 2) + half;
         const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
+        uint32_t va[2][2];  // [n & 1][first / second read]
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-          const bf16x8_t p =
-              words(pw[0][4 * kb], pw[0][4 * kb + 1], pw[0][4 * kb + 2], pw[0][4 * kb + 3]);
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
-          for (int n = 0; n < NO; ++n) {
-            auto vread = [&](int y) {
-              const int r = vr + 2 * y;
-              const uint8_t* at = tile + LTile::row(r) + kb * 2 * LTile::NSEG * 1024 +
-                                  ds * (NO / 2) * 1024 + (n / 2) * 1024 +
-                                  (((vp + 4 * (n & 1)) ^ tile_swizzle(r)) << 4) + 8 * (lane & 1);
-              return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (lds_v4i16*)const_cast<uint8_t*>(at));
-            };
-            const bf16x8_t vt = __builtin_bit_cast(
-                bf16x8_t, __builtin_shufflevector(vread(0), vread(1), 0, 1, 2, 3, 4, 5, 6, 7));
-            o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vt, p, o[n], 0, 0, 0);
-          }
+          for (int y = 0; y < 2; ++y)
+            va[n][y] = lds_addr(tile_at(it) + LTile::row(vr + 2 * y) + 8 * (lane & 1) +
+                                ds * (NO / 2) * 1024 +
+                                (((vp + 4 * n) ^ tile_swizzle(vr + 2 * y)) << 4));
+        constexpr int N = 2 * NO, VD = 4;  // MFMA x: tokens 16 (x / NO) .., dims 32 (x % NO) ..
+        v4i16 lo[VD], hi[VD];
+        auto vread = [&](auto x) {
+          constexpr int OFF = (x / NO) * 2 * LTile::NSEG * 1024 + (x % NO) / 2 * 1024;
+          lo[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][0]);
+          hi[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][1]);
+        };
+        static_for<VD>(vread);  // in flight while the weights are worked out
+        uint32_t pw[1][8];
+        if (__builtin_expect(__ballot(!(__builtin_fabsf(m_run) <= kFused)) != 0, 0)) {
+          if (m_run == -INFINITY) m_run = largest<1>(s, a.scale_log2);
+          l_run += weights_rounded<1>(pw, s, a.scale_log2, m_run);
+        } else {
+          l_run += weights_of<1>(pw, s, a.scale_log2, m_run);
         }
+        static_for<N>([&](auto x) {
+          constexpr int later = N - 1 - x < VD - 1 ? N - 1 - x : VD - 1;
+          constexpr int kb = x / NO, n = x % NO;
+          lgkm_wait2<2 * later>(lo[x % VD], hi[x % VD]);
+          const bf16x8_t vt = __builtin_bit_cast(
+              bf16x8_t, __builtin_shufflevector(lo[x % VD], hi[x % VD], 0, 1, 2, 3, 4, 5, 6, 7));
+          o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              vt, words(pw[0][4 * kb], pw[0][4 * kb + 1], pw[0][4 * kb + 2], pw[0][4 * kb + 3]),
+              o[n], 0, 0, 0);
+          if constexpr (x + VD < N) vread(std::integral_constant<int, x + VD>{});
+          __builtin_amdgcn_sched_barrier(0);
+        });
         // A latent that is not finite, in a tile that only some rows see, was stored as zeros
         // (zero weights would have made NaN of it). It is key and value at once: what a row that
         // sees it becomes is NaN.
+        const int base = tile_base(it);
         if (partial(base) &&
             __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
           const uint32_t bad =
               (uint32_t)__ballot(s_bad[(it % NB) * (CT + 1) + 1 + (lane & 31)] == it + 1);
-          const int hi = min(v.row_hi - base, 32), lo = max(v.row_lo - base, 0);
-          const uint32_t seen = lo < hi ? (0xffffffffu >> (32 - (hi - lo))) << lo : 0u;
-          if (bad & seen) l_run = NAN;
+          if (bad & seen_bits(0xffffffffu, v.row_lo, v.row_hi, base, 0)) l_run = NAN;
         }
       }
-      if constexpr (NB == 1) __syncthreads();  // the tile is read by all
-      if (it + 1 < n_it) {
-        store(it + 1);
-        mask_now = vmask;
+      if (attempt == 1) break;
+      // some row's weights outgrew its reference? (A sum that is NaN is no reason: it stays so.)
+      if (__ballot(l_run > kWeightLimit) && lane == 0) *s_outgrown = 1;
+      lds_barrier();
+      if (__builtin_expect(__builtin_amdgcn_readfirstlane(*s_outgrown) == 0, 1)) break;
+      load_entry(0);
+      ev = mask_entry(0);
+      begin();
+      m_run = -INFINITY;
+      for (int it = 0; it < n_it; ++it) {
+        f32x16 s[1];
+        uint32_t exist;
+        scores(it, s[0], exist);
+        m_run = fmaxf(m_run, largest<1>(s, a.scale_log2));
       }
+      lds_barrier();  // the last tiles are read
+      load_entry(0);
+      ev = mask_entry(0);
+      begin();
     }
     l_run += __shfl_xor(l_run, 32, 64);
 
-    // ---- results; the token groups' merged through LDS ----
-    float m = m_run, l = l_run;
-    auto quad = [&](int q) {
-      return f32x4{o[q >> 2][4 * (q & 3)], o[q >> 2][4 * (q & 3) + 1], o[q >> 2][4 * (q & 3) + 2],
-                   o[q >> 2][4 * (q & 3) + 3]};
+    // ---- results: the accumulators are read one by one (arithmetic on them would move all of them
+    // to vector registers); the wait states after the last MFMA are given here ----
+    asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
+    auto quad = [&](int n, int x) {
+      f32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(o[n][4 * x + i]));
+        r[i] = y;
+      }
+      return r;
     };
-    constexpr int QUADS = 4 * NO, MINE = QUADS / TG;
-    f32x4 r[MINE];
-    if constexpr (TG > 1) {
-      float2* s_ml = reinterpret_cast<float2*>(s_mem + ML);
-      f32x4* s_o = reinterpret_cast<f32x4*>(s_mem);
-      __syncthreads();
-#pragma unroll
-      for (int q = 0; q < QUADS; ++q) s_o[(wave * QUADS + q) * 64 + lane] = quad(q);
-      if (half == 0) s_ml[wave * 32 + col] = make_float2(m_run, l_run);
-      __syncthreads();
-      float2 ml[TG];
-      m = -INFINITY;
-#pragma unroll
-      for (int t = 0; t < TG; ++t) {
-        ml[t] = s_ml[(t * GW + in_group) * 32 + col];
-        m = fmaxf(m, ml[t].x);
-      }
-      l = 0.f;
-      float wt[TG];
-#pragma unroll
-      for (int t = 0; t < TG; ++t) {
-        wt[t] = ml[t].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[t].x - m);
-        l += ml[t].y * wt[t];
-      }
-#pragma unroll
-      for (int x = 0; x < MINE; ++x) {
-        r[x] = f32x4{};
-#pragma unroll
-        for (int t = 0; t < TG; ++t)
-          r[x] += s_o[((t * GW + in_group) * QUADS + tg * MINE + x) * 64 + lane] * wt[t];
-      }
-    } else {
-#pragma unroll
-      for (int x = 0; x < MINE; ++x) r[x] = quad(x);
-    }
     if (!v.live) return;
-    const bool first = ds == 0 && tg == 0 && half == 0;
-    // quad q of the wave: dims 32 (NO ds + q / 4) + 8 (q % 4) + 4 half .. +3
-    auto dim = [&](int x) {
-      const int q = tg * MINE + x;
-      return 32 * (NO * ds + (q >> 2)) + 8 * (q & 3) + 4 * half;
-    };
+    const float m = m_run, l = l_run;
+    const bool first = ds == 0 && half == 0;
+    // quad x of tile n: dims 32 (NO ds + n) + 8 x + 4 half .. +3
+    const int dim0 = 32 * NO * ds + 4 * half;
     if (w.splits > 1) {
       const int64_t pr =
           h * a.head_part_rows + w.part_row + w.split * 32 * RG + rg * 32 + col;
+      float* po = a.part_o + pr * 512 + dim0;
 #pragma unroll
-      for (int x = 0; x < MINE; ++x)
-        *reinterpret_cast<f32x4*>(a.part_o + pr * 512 + dim(x)) = r[x];
+      for (int n = 0; n < NO; ++n)
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<f32x4*>(po + 32 * n + 8 * x) = quad(n, x);
       if (first) a.part_ml[pr] = make_float2(m, l);
       return;
     }
     const float inv = l > 0.f ? 1.f / l : l;
     uint16_t* out =
-        a.out + (int64_t)(w.q.begin + v.tok) * a.out_stride + (int64_t)v.head * 512;
+        a.out + (int64_t)(w.q.begin + v.tok) * a.out_stride + (int64_t)v.head * 512 + dim0;
 #pragma unroll
-    for (int x = 0; x < MINE; ++x) store_bf16x4(out + dim(x), r[x] * inv);
+    for (int n = 0; n < NO; ++n)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) store_bf16x4(out + 32 * n + 8 * x, quad(n, x) * inv);
     if (a.lse && first)
       a.lse[(int64_t)(w.q.begin + v.tok) * (a.kv_heads * a.g) + v.head] = natural(m, l);
   }
 };
 
 template <bool FP8>
-__global__ __launch_bounds__(512, 2) void chunk_latent_kernel(ChunkArgs a) {
-  using L1 = Latent<FP8, 1, 4, 2>;
-  using L2 = Latent<FP8, 2, 4, 1>;
-  using L4 = Latent<FP8, 4, 2, 1>;
+__global__ __launch_bounds__(256, 1) void chunk_latent_kernel(ChunkArgs a) {
+  using L1 = Latent<FP8, 1, 4>;
+  using L2 = Latent<FP8, 2, 2>;
+  using L4 = Latent<FP8, 4, 1>;
   constexpr int LDS = std::max(std::max(L1::LDS, L2::LDS), L4::LDS);
   __shared__ __align__(1024) uint8_t s_mem[LDS];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
@@ -1342,19 +1402,19 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const StreamDevice device(s);
   const bool fp8 = kv->type == HISPARSE_KV_FP8;
-  const dim3 grid((unsigned)(p.items * c->kv_heads)), block(512);
+  const dim3 grid((unsigned)(p.items * c->kv_heads));
   const dim3 merge((unsigned)(p.tiles * c->kv_heads),
                    p.max_splits <= 4 ? p.merge_rows / 8 : p.merge_rows);
   if (kv->layout == HISPARSE_KV_GROUPED) {
-    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, block, 0, s, a);
+    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
     if (p.max_splits > 4)
       hipLaunchKernelGGL((chunk_merge_kernel<128, 8>), merge, dim3(256), 0, s, a);
     else if (p.max_splits > 1)
       hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), merge, dim3(256), 0, s, a);
   } else {
-    if (fp8) hipLaunchKernelGGL(chunk_latent_kernel<true>, grid, block, 0, s, a);
-    else hipLaunchKernelGGL(chunk_latent_kernel<false>, grid, block, 0, s, a);
+    if (fp8) hipLaunchKernelGGL(chunk_latent_kernel<true>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(chunk_latent_kernel<false>, grid, dim3(256), 0, s, a);
     if (p.max_splits > 4)
       hipLaunchKernelGGL((chunk_merge_kernel<512, 8>), merge, dim3(256), 0, s, a);
     else if (p.max_splits > 1)
