@@ -32,7 +32,7 @@ struct ChunkArgs {
   const uint16_t* q;
   uint16_t* out;
   float* lse;
-  float* part_o;    // [part rows][d_v]: unnormalised outputs of splits
+  float* part_o;    // unnormalised outputs of splits, 32 rows at a time (see part_quad)
   float2* part_ml;  // [part rows] (reference in log2 units, sum)
   int64_t record_stride, head_stride, request_stride;
   int64_t q_stride, out_stride, table_request_stride, table_head_stride;
@@ -216,6 +216,14 @@ __device__ __forceinline__ void store_bf16x4(uint16_t* to, f32x4 y) {
   const bf16x2_t b1 = __builtin_convertvector(f32x2{y[2], y[3]}, bf16x2_t);
   *reinterpret_cast<any_u32x2*>(to) =
       u32x2{__builtin_bit_cast(uint32_t, b0), __builtin_bit_cast(uint32_t, b1)};
+}
+
+// Partial results are stored as the accumulators hold them, so that every lane writes 16 contiguous
+// bytes of a wave's 1024: per 32 rows, quad 4n + x (dims 32n + 8x ..), lane (row lane & 31), dims +
+// 4 (lane / 32) .. +3. (Row by row a store touched 32 rows, 32 bytes of each.)
+__device__ __forceinline__ float* part_quad(float* part_o, int64_t part_row, int d_v, int quad,
+                                            int lane) {
+  return part_o + part_row * d_v + (quad * 64 + lane) * 4;
 }
 
 // The cached tokens [lo, hi) that new token i of a request sees (hi may be below lo).
@@ -798,14 +806,11 @@ struct Grouped {
                                                 int tile_row, float m, float l, int half) {
     const bool first = q0 == 0 && half == 0;
     if (w.splits > 1) {
-      const int64_t pr = h * a.head_part_rows + w.part_row + w.split * 32 * RW + tile_row;
+      const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RW + (tile_row >> 5)) * 32;
 #pragma unroll
-      for (int x = 0; x < NQ; ++x) {
-        const int q = q0 + x;
-        *reinterpret_cast<f32x4*>(a.part_o + pr * 128 + 32 * (q >> 2) + 8 * (q & 3) + 4 * half) =
-            r[x];
-      }
-      if (first) a.part_ml[pr] = make_float2(m, l);
+      for (int x = 0; x < NQ; ++x)
+        *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 128, q0 + x, threadIdx.x & 63)) = r[x];
+      if (first) a.part_ml[pr + (tile_row & 31)] = make_float2(m, l);
       return;
     }
     const float inv = l > 0.f ? 1.f / l : l;
@@ -1158,15 +1163,14 @@ struct Latent {
     // quad x of tile n: dims 32 (NO ds + n) + 8 x + 4 half .. +3
     const int dim0 = 32 * NO * ds + 4 * half;
     if (w.splits > 1) {
-      const int64_t pr =
-          h * a.head_part_rows + w.part_row + w.split * 32 * RG + rg * 32 + col;
-      float* po = a.part_o + pr * 512 + dim0;
+      const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
 #pragma unroll
       for (int n = 0; n < NO; ++n)
 #pragma unroll
         for (int x = 0; x < 4; ++x)
-          *reinterpret_cast<f32x4*>(po + 32 * n + 8 * x) = quad(n, x);
-      if (first) a.part_ml[pr] = make_float2(m, l);
+          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, 4 * (NO * ds + n) + x, lane)) =
+              quad(n, x);
+      if (first) a.part_ml[pr + col] = make_float2(m, l);
       return;
     }
     const float inv = l > 0.f ? 1.f / l : l;
@@ -1196,60 +1200,84 @@ __global__ __launch_bounds__(256, 1) void chunk_latent_kernel(ChunkArgs a) {
   else L4::run(a, w, h, s_mem);
 }
 
-// Merge of the splits' partial results of a row tile: 256 threads, SG groups of 32 lanes per row,
-// each over every SG-th split; the groups' sums joined through LDS in their order.
+// Merge of the splits' partial results of 32 rows and 128 dims: SG sets of four waves, each with
+// every SG-th split, wave x of a set with quads 4x .. 4x + 3; the sets' sums are joined in LDS in
+// their order, and rows written out whole from there.
 template <int DV, int SG>
-__global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
-  constexpr int ROWS = 8 / SG, NX = DV / 128;
-  __shared__ f32x4 s_o[8][NX][32];
+__global__ __launch_bounds__(256 * SG) void chunk_merge_kernel(ChunkArgs a) {
+  constexpr int NT = 256 * SG;
+  __shared__ float s_w[kMaxSplits][32];  // a split's weight in each row's result
+  __shared__ float s_m[32], s_l[32], s_red[SG * 8][32];
+  __shared__ f32x4 s_o[SG][16][64];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
   if (!find_work<(DV == 512), true>(a, item, w) || w.splits == 1) return;
-  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5, sg = grp % SG;
-  const int bm = 32 * w.groups, tile_row = blockIdx.y * ROWS + grp / SG;
-  const int row = w.tile * bm + tile_row;
-  const bool live = tile_row < bm && row < w.q.n * a.g;
-  const int64_t base = h * a.head_part_rows + w.part_row + tile_row;
-  float m = -INFINITY, l = 0.f;
-  f32x4 r[NX];
+  const int group = blockIdx.y / (DV / 128), block = blockIdx.y % (DV / 128);
+  const int n_rows = w.q.n * a.g, row0 = (w.tile * w.groups + group) * 32;
+  if (group >= w.groups || row0 >= n_rows) return;
+  const int live = min(32, n_rows - row0);
+  // rows pr + s * step .. + 31 hold split s
+  const int64_t pr = h * a.head_part_rows + w.part_row + group * 32, step = w.groups * 32;
+  const int t = threadIdx.x, lane = t & 63, row = t & 31, part = t >> 5;
+  float m = -INFINITY;
+  if (row < live)
+    for (int s = part; s < w.splits; s += SG * 8) m = fmaxf(m, a.part_ml[pr + s * step + row].x);
+  s_red[part][row] = m;
+  __syncthreads();
+  if (part == 0) {
 #pragma unroll
-  for (int x = 0; x < NX; ++x) r[x] = f32x4{};
-  if (live) {
-    for (int s = lane; s < w.splits; s += 32) m = fmaxf(m, a.part_ml[base + (int64_t)s * bm].x);
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-#pragma unroll 4
-    for (int s = sg; s < w.splits; s += SG) {
-      const int64_t pr = base + (int64_t)s * bm;
-      const float2 ml = a.part_ml[pr];
+    for (int i = 1; i < SG * 8; ++i) m = fmaxf(m, s_red[i][row]);
+    s_m[row] = m;
+  }
+  __syncthreads();
+  m = s_m[row];
+  float l = 0.f;
+  if (row < live)
+    for (int s = part; s < w.splits; s += SG * 8) {
+      const float2 ml = a.part_ml[pr + s * step + row];
+      // a split that sees nothing has reference -inf, and sum and output 0
       const float wt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - m);
+      s_w[s][row] = wt;
       l += ml.y * wt;
+    }
+  s_red[part][row] = l;
+  __syncthreads();
+  if (part == 0) {
+    l = 0.f;
 #pragma unroll
-      for (int x = 0; x < NX; ++x)
-        r[x] += *reinterpret_cast<const f32x4*>(a.part_o + pr * DV + 128 * x + 4 * lane) * wt;
+    for (int i = 0; i < SG * 8; ++i) l += s_red[i][row];
+    s_l[row] = l;
+  }
+  const int set = t >> 8, q0 = (t >> 6 & 3) * 4;
+  f32x4 r[4] = {};
+  if (row < live) {
+#pragma unroll 4
+    for (int s = set; s < w.splits; s += SG) {
+      const float wt = s_w[s][row];
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        r[x] += *reinterpret_cast<const f32x4*>(
+                    part_quad(a.part_o, pr + s * step, DV, block * 16 + q0 + x, lane)) * wt;
     }
   }
-  if constexpr (SG > 1) {
-    __shared__ float s_l[8];
 #pragma unroll
-    for (int x = 0; x < NX; ++x) s_o[grp][x][lane] = r[x];
-    if (lane == 0) s_l[grp] = l;
-    __syncthreads();
-    if (sg != 0) return;
-    for (int t = 1; t < SG; ++t) {
-      l += s_l[grp + t];
+  for (int x = 0; x < 4; ++x) s_o[set][q0 + x][lane] = r[x];
+  __syncthreads();
+  // a row's 128 dims by 32 threads, four dims each: dims 4c .. are quad c / 2, half c & 1
+  for (int y = t >> 5; y < live; y += NT / 32) {
+    const int c = t & 31, at = (c & 1) * 32 + y;
+    f32x4 o = s_o[0][c >> 1][at];
 #pragma unroll
-      for (int x = 0; x < NX; ++x) r[x] += s_o[grp + t][x][lane];
-    }
+    for (int i = 1; i < SG; ++i) o += s_o[i][c >> 1][at];
+    l = s_l[y];
+    const float inv = l > 0.f ? 1.f / l : l;
+    const int tok = (int)fastdiv(row0 + y, a.div_g), head = h * a.g + row0 + y - tok * a.g;
+    store_bf16x4(a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * DV +
+                     block * 128 + 4 * c,
+                 o * inv);
+    if (a.lse && c == 0 && block == 0)
+      a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] = natural(s_m[y], l);
   }
-  if (!live) return;
-  const int tok = (int)fastdiv(row, a.div_g), head = h * a.g + row - tok * a.g;
-  const float inv = l > 0.f ? 1.f / l : l;
-  uint16_t* out = a.out + (int64_t)(w.q.begin + tok) * a.out_stride + (int64_t)head * DV;
-#pragma unroll
-  for (int x = 0; x < NX; ++x) store_bf16x4(out + 128 * x + 4 * lane, r[x] * inv);
-  if (a.lse && lane == 0)
-    a.lse[(int64_t)(w.q.begin + tok) * (a.kv_heads * a.g) + head] = natural(m, l);
 }
 
 // ---- host: the call's plan ----------------------------------------------------------------
@@ -1257,7 +1285,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
 struct ChunkPlan {
   int64_t tiles, items;  // at most so many row tiles, (tile, split)s of a kv head
   int64_t part_rows;     // rows of partial results, all kv heads
-  int32_t d_v, target, uni_tiles, uni_splits, max_splits, merge_rows;
+  int32_t d_v, target, uni_tiles, uni_splits, max_splits;
+  int32_t groups;        // of 32 rows of the largest row tile
   size_t workspace_bytes;
 };
 
@@ -1299,7 +1328,7 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     p.items = std::max(p.items, (int64_t)c.num_requests * p.uni_tiles * p.uni_splits);
   }
   if (p.max_splits > 1) {
-    p.merge_rows = (int32_t)bm;
+    p.groups = (int32_t)(bm / 32);
     p.part_rows = p.items * bm * c.kv_heads;
     p.workspace_bytes = (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2));
   }
@@ -1403,22 +1432,26 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   const StreamDevice device(s);
   const bool fp8 = kv->type == HISPARSE_KV_FP8;
   const dim3 grid((unsigned)(p.items * c->kv_heads));
-  const dim3 merge((unsigned)(p.tiles * c->kv_heads),
-                   p.max_splits <= 4 ? p.merge_rows / 8 : p.merge_rows);
-  if (kv->layout == HISPARSE_KV_GROUPED) {
-    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
-    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
-    if (p.max_splits > 4)
-      hipLaunchKernelGGL((chunk_merge_kernel<128, 8>), merge, dim3(256), 0, s, a);
-    else if (p.max_splits > 1)
-      hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), merge, dim3(256), 0, s, a);
-  } else {
+  const bool latent = kv->layout == HISPARSE_KV_LATENT;
+  if (latent) {
     if (fp8) hipLaunchKernelGGL(chunk_latent_kernel<true>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(chunk_latent_kernel<false>, grid, dim3(256), 0, s, a);
-    if (p.max_splits > 4)
-      hipLaunchKernelGGL((chunk_merge_kernel<512, 8>), merge, dim3(256), 0, s, a);
-    else if (p.max_splits > 1)
+  } else {
+    if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
+    else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
+  }
+  if (p.max_splits > 1) {
+    // few workgroups with many splits each: four times the threads
+    const dim3 merge((unsigned)(p.tiles * c->kv_heads), p.groups * (latent ? 4 : 1));
+    const bool deep = p.max_splits > 8 && (int64_t)merge.x * merge.y <= kTargetWorkgroups;
+    if (latent && deep)
+      hipLaunchKernelGGL((chunk_merge_kernel<512, 4>), merge, dim3(1024), 0, s, a);
+    else if (latent)
       hipLaunchKernelGGL((chunk_merge_kernel<512, 1>), merge, dim3(256), 0, s, a);
+    else if (deep)
+      hipLaunchKernelGGL((chunk_merge_kernel<128, 4>), merge, dim3(1024), 0, s, a);
+    else
+      hipLaunchKernelGGL((chunk_merge_kernel<128, 1>), merge, dim3(256), 0, s, a);
   }
   return hipGetLastError() == hipSuccess ? HISPARSE_OK : HISPARSE_ERR_HIP;
 }
