@@ -64,6 +64,16 @@ __device__ __forceinline__ v4i16 lds_read_tr16_b64(uint32_t addr) {
   asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
   return v;
 }
+// The same for bytes: in each group of 16 lanes, lane 2s + q addresses 8 bytes, columns 8q .., of row
+// s; lane t then holds column t of the eight rows.
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+template <int OFF>
+__device__ __forceinline__ u32x2 lds_read_tr8_b64(uint32_t addr) {
+  static_assert(OFF >= 0 && OFF < 65536, "immediate offset");
+  u32x2 v;
+  asm volatile("ds_read_b64_tr_b8 %0, %1 offset:%2" : "=v"(v) : "v"(addr), "n"(OFF));
+  return v;
+}
 // f(0), f(1), ..., f(N - 1) with the index as a compile-time constant (immediate offsets).
 template <int N, int I = 0, class F>
 __device__ __forceinline__ void static_for(F&& f) {
@@ -82,8 +92,8 @@ template <int N>
 __device__ __forceinline__ void lgkm_wait2(u32x4& a, u32x4& b) {
   asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(N));
 }
-template <int N>
-__device__ __forceinline__ void lgkm_wait1(u32x4& a) {
+template <int N, class T>
+__device__ __forceinline__ void lgkm_wait1(T& a) {
   asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(N));
 }
 
@@ -136,6 +146,11 @@ struct Tile {
   __device__ static int row(int r) { return (r >> 3) * (NSEG * 1024) + (r & 7) * 128; }
 };
 __device__ inline int tile_swizzle(int r) { return (r >> 1) & 7; }
+
+// Direct global->LDS load of 4 bytes per lane, to `lds` + 4 times the lane.
+__device__ __forceinline__ void load_lds4(const uint8_t* src, uint8_t* lds) {
+  __builtin_amdgcn_global_load_lds(src, (lds_void*)lds, 4, 0, 0);
+}
 
 // Direct global->LDS load of one block, segment SEG of row group rg: `src` is this lane's row (row
 // 8 rg + lane / 8) already advanced by the lane's 16-byte piece. The load's immediate offset

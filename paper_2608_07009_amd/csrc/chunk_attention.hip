@@ -24,7 +24,9 @@ constexpr float kWeightLimit = 18446744073709551616.f;
 // first, as the reference was, or a weight could leave the float range.
 constexpr float kFused = 16777216.f;
 constexpr int kMaxSplits = 128;  // parts of one request's cached tokens
-constexpr int kMinSplitTokens = 256;
+// The least tokens of a split: a workgroup's two rounds of two tiles (latent records), its eight
+// tiles (grouped-query ones).
+__device__ __host__ constexpr int min_split(bool latent) { return latent ? 128 : 256; }
 
 struct ChunkArgs {
   const uint8_t* pool;
@@ -39,7 +41,8 @@ struct ChunkArgs {
   int64_t num_records, head_part_rows;
   KvLayout l;
   int32_t requests, kv_heads, g, total, max_chunk, max_tokens, window, causal;
-  int32_t target;               // workgroups that splitting aims at (0: no splits)
+  int32_t split;                // the cached tokens may be split
+  int32_t target;               // workgroups that splitting aims at (0: none)
   int32_t num_splits;           // asked for (0: chosen)
   int32_t uni_tiles, uni_splits;  // of every request, where they are alike (start and kv_len null)
   FastDiv div_g;
@@ -48,11 +51,14 @@ struct ChunkArgs {
 
 // ---- which piece of the call a workgroup does ------------------------------------------------
 
-// Rows (new token, query head of the kv head) of one workgroup: groups of 32, as many as the
-// request's rows fill, up to eight (grouped-query records) or four (latent ones). What waves are
-// left over take other tokens or other dims.
-__device__ __host__ inline int row_groups(int rows, bool latent) {
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : (rows <= 128 || latent) ? 4 : 8;
+// Rows (new token, query head of the kv head) of one workgroup, in groups of 32; what waves are left
+// over take other tokens. Grouped-query records: as many groups as the request's rows fill, up to
+// eight. Latent ones: four, or two where the cached tokens are split: a split's partial results are
+// 2 KB a row, written and read again, and a workgroup of half the rows covers twice the tokens (32
+// requests of 128 heads over 2048 8-bit tokens: 59 us with four, of which 28 partial results).
+__device__ __host__ inline int row_groups(int rows, bool latent, bool split) {
+  if (latent) return rows <= 64 || split ? 2 : 4;
+  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
 }
 
 struct Request {
@@ -100,7 +106,7 @@ template <bool LATENT, bool MERGE>
 __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w) {
   const int lane = threadIdx.x & 63;
   if (!a.start && !a.kv_len) {
-    const int bm = 32 * row_groups(a.max_chunk * a.g, LATENT);
+    const int bm = 32 * row_groups(a.max_chunk * a.g, LATENT, a.split);
     const int per = MERGE ? a.uni_tiles : a.uni_tiles * a.uni_splits;
     w.req = item / per;
     if (w.req >= a.requests) return false;
@@ -116,7 +122,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
   }
   auto tiles_of = [&](const Request& q, int& groups) {
     const int rows = q.n * a.g;
-    groups = row_groups(rows, LATENT);
+    groups = row_groups(rows, LATENT, a.split);
     return (rows + 32 * groups - 1) / (32 * groups);
   };
   auto span_of = [&](const Request& q) {
@@ -137,7 +143,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     }
     // a little more than their share, so that there are no more items than the host allows for
     const float p = sum * (float)a.kv_heads * (64.01f / (float)a.target) + 1.f;
-    part = (int)fminf(fmaxf(p, (float)kMinSplitTokens), 1.5e9f);
+    part = (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1.5e9f);
   }
   int items = 0;
   int64_t rows = 0;
@@ -201,6 +207,17 @@ __device__ __forceinline__ float if_not_finite(float x) {
   const uint32_t b = __float_as_uint(x);
   return __uint_as_float(b & (uint32_t)((int32_t)((b & 0x7fffffffu) + 0x00800000u) >> 31));
 }
+// The same for e4m3 values (NaN is 0x7f, with either sign; there are no infinities).
+__device__ __forceinline__ bool clear_bad8(u32x4& x) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = ((x[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+    any |= b;
+    x[i] &= ~((b >> 7) * 0xffu);
+  }
+  return any != 0;
+}
 // ln of a softmax's sum from its reference (log2 units) and the sum against it.
 __device__ __forceinline__ float natural(float m, float l) {
   return l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
@@ -209,7 +226,6 @@ __device__ __forceinline__ bf16x8_t words(uint32_t a, uint32_t b, uint32_t c, ui
   return __builtin_bit_cast(bf16x8_t, u32x4{a, b, c, d});
 }
 typedef u32x4 any_u32x4 __attribute__((aligned(2)));  // queries and outputs start at any element
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 any_u32x2 __attribute__((aligned(2)));
 __device__ __forceinline__ void store_bf16x4(uint16_t* to, f32x4 y) {
   const bf16x2_t b0 = __builtin_convertvector(f32x2{y[0], y[1]}, bf16x2_t);
@@ -304,19 +320,24 @@ __device__ __forceinline__ void mask_scores(f32x16& s, uint32_t seen) {
   }
 }
 // Softmax weights of 16 N scores (raw products) of this lane's row against a reference, in pairs
-// rounded to bf16; returns their unrounded sum.
+// rounded to bf16 (times their tokens' value scales, if given); returns their unrounded sum.
 template <int N>
 __device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (&s)[N],
-                                            float scale, float ref) {
+                                            float scale, float ref,
+                                            const u32x4* value_scale = nullptr) {
   float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
-      const f32x2 p = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i], scale, -ref)),
-                       __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i + 1], scale, -ref))};
+      f32x2 p = {__builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i], scale, -ref)),
+                 __builtin_amdgcn_exp2f(__builtin_fmaf(s[j][i + 1], scale, -ref))};
       sum[i & 2] += p[0];
       sum[(i & 2) + 1] += p[1];
+      if (value_scale) {
+        p[0] *= __uint_as_float(value_scale[4 * j + (i >> 2)][i & 3]);
+        p[1] *= __uint_as_float(value_scale[4 * j + (i >> 2)][(i & 3) + 1]);
+      }
       pw[j][i >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
     }
   return (sum[0] + sum[1]) + (sum[2] + sum[3]);
@@ -335,13 +356,14 @@ __device__ __forceinline__ float largest(const f32x16 (&s)[N], float scale) {
 // Weights against a reference whose products would not stay in range unrounded, or none (-inf).
 template <int N>
 __device__ __forceinline__ float weights_rounded(uint32_t (&pw)[N][8], f32x16 (&s)[N],
-                                                 float scale, float ref) {
+                                                 float scale, float ref,
+                                                 const u32x4* value_scale = nullptr) {
   if (ref == -INFINITY) ref = 0.f;
 #pragma unroll
   for (int j = 0; j < N; ++j)
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[j][i] = over_reference(s[j][i], scale, ref);
-  return weights_of<N>(pw, s, 1.f, 0.f);
+  return weights_of<N>(pw, s, 1.f, 0.f, value_scale);
 }
 // The rare cases: rows without a reference, rows that outgrew theirs (both get the largest of these
 // scores, sum and output following), and references whose products would not stay in range
@@ -840,306 +862,450 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
 
 // ---- latent records --------------------------------------------------------------------------
 //
-// Four waves, one per SIMD with all of its registers: RG groups of 32 rows, times DS waves that share
-// a group's rows. A tile is 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the
-// value is the latent part). Of the DS waves of a row group, wave d
-//   adds up the k-steps kk = d mod DS of the scores, which are then summed through LDS,
-//   and keeps the output dims 512 / DS d .. of its rows,
-// so that few rows still spread over four waves. The output (256 / DS registers a lane) lives in
-// accumulation registers; the score MFMAs are assembly so that theirs do not (see mfma_qk).
-// Nothing but MFMAs touches the output: a row's reference stays the largest score of the first tile
-// that it sees. If some row's weights outgrow the range (kWeightLimit), the workgroup goes over its
-// tokens twice more: for every row's largest score, then for the result against those.
-// 16-bit tiles are stored by direct loads NB - 1 tiles ahead, 8-bit ones widened by way of registers
-// one tile ahead; either is done in the shadow of the score MFMAs.
+// Four waves, one per SIMD with all of its registers, in TG token groups of RG row waves: 128 rows on
+// one tile, or 64 rows (a second row wave without rows only stages) on two tiles at once. A tile is
+// 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the value is the latent part).
+// A wave keeps its 32 rows' query (144 registers a lane) and output (256 accumulators; the score
+// MFMAs are assembly so that theirs are not, see mfma_qk). Nothing but MFMAs touches the output: a
+// row's reference stays the largest score of the first tile that it sees. If some row's weights
+// outgrow the range (kWeightLimit), the workgroup goes over its tokens twice more: for every row's
+// largest score, then for the result against those.
+// Tiles are stored by direct loads NB - 1 tiles ahead, sent in the shadow of the score MFMAs. 8-bit
+// tiles stay so in LDS (half the traffic) and are widened by the wave that reads an operand, exactly:
+// e4m3 fits bf16. Their scales join where they cost least: the latent part of a score is multiplied
+// by its token's (the rotary part, a chain of MFMAs of its own, is not), and so is the weight that
+// goes with the token's value.
 
-using LTile = Tile<72>;
+using LTile = Tile<72>;  // 16-bit rows
+using PTile = Tile<32>;  // 8-bit latent rows of 512 bytes
+using RTile = Tile<8>;   // and their rotary dims
 
-template <bool FP8, int RG, int DS>
+template <bool FP8, int TG>
 struct Latent {
   static constexpr int CT = 32;
-  static constexpr int NB = FP8 ? 2 : 3;       // tile buffers
-  static constexpr int NQ = 36 / DS;           // k-steps of a wave
-  static constexpr int NO = 16 / DS;           // its output tiles of 32 dims
-  static constexpr int NBASE = 4 / DS;         // its K operand addresses
-  static_assert(RG * DS == 4, "shape");
-  static constexpr int SCORES = NB * LTile::BYTES;  // LDS offsets
-  static constexpr int MARKS = SCORES + (DS > 1 ? 4 * 4096 : 0);
-  static constexpr int LDS = MARKS + NB * (CT + 1) * 4 + 4;
+  static constexpr int RG = 4 / TG;            // row waves of a token group
+  static constexpr int NB = (FP8 ? 6 : 4) / TG;  // tile buffers of a token group
+  static constexpr int AHEAD = NB - 1;         // tiles between a load and its tile's scores
+  // direct loads of a wave per tile: TG groups of eight rows; 8-bit, and the scales
+  static constexpr int LOADS = FP8 ? 5 * TG + 1 : 9 * TG;
+  static constexpr int TILE = FP8 ? PTile::BYTES + RTile::BYTES + RG * 256 : LTile::BYTES;
+  // LDS: tiles (8-bit: latent rows, rotary dims, a copy of the 32 scales per wave), under which the
+  // query passes first and the token groups' outputs last; table entries of WINDOW tokens;
+  // bad-token marks; the token groups' (reference, sum) pairs
+  static constexpr int WINDOW = 512;
+  static constexpr int ENTRIES = std::max(TG * NB * TILE, 4 * LTile::BYTES);
+  static constexpr int MARKS = ENTRIES + WINDOW * 4;
+  static constexpr int N_MARKS = TG * NB * (CT + 1) + 1;  // the last: a row outgrew its reference
+  static constexpr int ML = (MARKS + N_MARKS * 4 + 15) / 16 * 16;
+  static constexpr int LDS = ML + 4 * 32 * 8;
+  static_assert((AHEAD + 1) * TG * CT <= 256 && LDS <= 160 * 1024, "window and LDS");
 
   static __device__ __forceinline__ void run(const ChunkArgs& a, const Work& w, int h,
                                              uint8_t* s_mem) {
-    const int lane = threadIdx.x & 63, half = lane >> 5, col = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rg = wave / DS, ds = wave % DS;
-    f32x4* s_scores = reinterpret_cast<f32x4*>(s_mem + SCORES) + rg * DS * 256;
-    int* s_bad = reinterpret_cast<int*>(s_mem + MARKS);
-    const View v = view_of<32 * RG>(a, w, h, rg, col);
-    const int n_it = max(0, v.t1 - v.t0 + CT - 1) / CT;
-    auto tile_base = [&](int it) { return v.t0 + it * CT; };
-    auto tile_at = [&](int it) { return s_mem + (it % NB) * LTile::BYTES; };
+    const int tg = TG == 1 ? 0 : wave / RG, rg = TG == 1 ? wave : wave % RG;
+    // What the loop derives from the lane is worked out anew in every tile: kept, it would spill,
+    // and a reload waits for the direct loads in flight.
+    auto lane_now = []() {
+      int x = threadIdx.x & 63;
+      asm volatile("" : "+v"(x));
+      return x;
+    };
+    int32_t* s_entry = reinterpret_cast<int32_t*>(s_mem + ENTRIES);
+    int* s_marks = reinterpret_cast<int*>(s_mem + MARKS);
+    int* s_outgrown = s_marks + N_MARKS - 1;
+    const View v = view_of<32 * RG>(a, w, h, rg, threadIdx.x & 31);
+    const int n_it = max(0, v.t1 - v.t0 + TG * CT - 1) / (TG * CT);
+    auto first_token = [&](int it) { return (it * TG + tg) * CT; };  // from t0 on
+    auto tile_base = [&](int it) { return v.t0 + first_token(it); };
+    auto tile_at = [&](int it) { return s_mem + (tg * NB + it % NB) * TILE; };
+    auto scales_at = [&](int it) { return tile_at(it) + PTile::BYTES + RTile::BYTES + rg * 256; };
+    // a tile's marks: its number + 1 if a token has some, then per token the same
+    auto marks_at = [&](int it) { return s_marks + (tg * NB + it % NB) * (CT + 1); };
     auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
 
-    // ---- staging: a wave stages eight rows of a tile ----
-    auto entry = [&](int t) { return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1; };
-    auto ok_entry = [&](int32_t r) { return r >= 0 && r < a.num_records; };
-    int32_t e;   // table entry of this lane's row of the tile to load next
-    int32_t ev;  // and of token `lane` of the tile whose scores come next
-    auto load_entry = [&](int it) { e = entry(tile_base(it) + 8 * wave + (lane >> 3)); };
-    auto mask_entry = [&](int it) { return entry(tile_base(it) + col); };
-    const uint8_t* src = nullptr;  // this lane's row of the next tile (direct), its record (8-bit)
-    u32x4 st[5];
-    float st_scale = 1.f;
-    auto mark_bad = [&](int it, int r) {
-      s_bad[(it % NB) * (CT + 1) + 1 + r] = it + 1;
-      s_bad[(it % NB) * (CT + 1)] = it + 1;
+    // ---- table entries, checked (-1: no token), of WINDOW tokens from the current 256 on, so that
+    // nothing in the loop waits for a load younger than the tiles' ----
+    int32_t e_next;  // this thread's entry of the 256 tokens after the window
+    auto load_entries = [&](int block) {
+      const int t = v.t0 + block * 256 + (int)threadIdx.x;
+      e_next = t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1;
     };
-    auto in_record = [&](int it) {
-      return (tile_base(it) + 8 * wave + (lane >> 3)) & ((1 << a.l.tpr_shift) - 1);
+    auto store_entries = [&](int block) {
+      s_entry[(block & 1) * 256 + threadIdx.x] =
+          e_next >= 0 && e_next < a.num_records ? e_next : -1;
     };
-    auto record = [&]() {
-      return v.pool + (uint64_t)(uint32_t)e * (uint32_t)a.record_stride;
-    };
-    auto find_row = [&](int it) {
-      src = (ok_entry(e) ? record() + __umul24(in_record(it), a.l.row_bytes) : g_zero_row) +
-            stage_piece(lane, wave);
-    };
-    auto direct = [&](auto seg, int it) { stage_block<72, seg>(tile_at(it), wave, src); };
-    auto load8 = [&](int it) {
-      const int in = in_record(it);
-      const uint8_t* rec = record();
-      if (ok_entry(e)) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-          st[x] = *reinterpret_cast<const u32x4*>(rec + 512 * in + 128 * x + 16 * (lane & 7));
-        st[4] = *reinterpret_cast<const u32x4*>(rec + a.l.rope_offset + 128 * in +
-                                                16 * (lane & 7));
-        st_scale = *reinterpret_cast<const float*>(rec + a.l.scale_offset + 4 * in);
-      } else {
-#pragma unroll
-        for (int x = 0; x < 5; ++x) st[x] = u32x4{};
-        st_scale = 1.f;
-      }
-    };
-    // piece 0..7: eight latent dims of this lane's row, 8: its rotary dims
-    auto store8 = [&](auto piece, int it) {
-      const int r = 8 * wave + (lane >> 3), sw = tile_swizzle(r);
-      uint8_t* dst = tile_at(it) + LTile::row(r);
-      if constexpr (piece == 8) {
-        *reinterpret_cast<u32x4*>(dst + 8 * 1024 + (((lane & 7) ^ sw) << 4)) = st[4];
-      } else {
-        constexpr int x = piece / 2, y = piece % 2;
-        u32x4 p = widen(st[x][2 * y], st[x][2 * y + 1], st_scale);
-        if (partial(tile_base(it)) && clear_bad(p)) mark_bad(it, r);
-        *reinterpret_cast<u32x4*>(dst + (2 * x + ((lane & 7) >> 2)) * 1024 +
-                                  (((2 * (lane & 3) + y) ^ sw) << 4)) = p;
-      }
-    };
-    // this wave's rows of a tile that was stored directly
-    auto scrub = [&](int it) {
-      const int r = 8 * wave + (lane >> 3);
-      bool bad = false;
-      for (int x = 0; x < 8; ++x) {
-        u32x4* at = reinterpret_cast<u32x4*>(tile_at(it) + LTile::row(r) + x * 1024) + (lane & 7);
-        u32x4 p = *at;
-        if (clear_bad(p)) {
-          bad = true;
-          *at = p;
-        }
-      }
-      if (bad) mark_bad(it, r);
+    // the entries of this lane's rows of tile `ahead`, of token lane & 31 of tile `it`, and, 8-bit,
+    // of the token of `ahead` whose scale this lane fetches: scales lie in the order of the scores
+    int32_t e[TG], ev, es;
+    auto scale_token = [](int lane) { return score_token(lane & 15) + ((lane >> 4) & 1); };
+    auto read_entries = [&](int ahead, int it) {
+      const int lane = lane_now();
+      auto at = [&](int t) { return lds_addr(s_entry + (t & (WINDOW - 1))); };
+      const int t = first_token(ahead);
+      const uint32_t p = at(t + 8 * TG * rg + (lane >> 3)), q = at(first_token(it) + (lane & 31));
+      const uint32_t r = FP8 ? at(t + scale_token(lane)) : q;
+      asm volatile(
+          "ds_read_b32 %0, %3\n\tds_read_b32 %1, %4\n\tds_read_b32 %2, %5\n\t"
+          "s_waitcnt lgkmcnt(0)"
+          : "=&v"(e[0]), "=&v"(ev), "=&v"(es)
+          : "v"(p), "v"(q), "v"(r)
+          : "memory");
+      if constexpr (TG == 2)
+        asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(e[1])
+                     : "v"(at(t + 16 * rg + 8 + (lane >> 3)))
+                     : "memory");
     };
 
-    load_entry(0);
-    ev = mask_entry(0);
-    for (int i = threadIdx.x; i < NB * (CT + 1) + 1; i += 256) s_bad[i] = 0;
-    int* s_outgrown = s_bad + NB * (CT + 1);
-    // Q^T operand of k-steps kk = DS i + ds: dims 16 kk + 8 half .. +7 of this lane's row
-    bf16x8_t qreg[NQ];
-    {
-      const uint16_t* q = a.q + (int64_t)(w.q.begin + v.tok) * a.q_stride + (int64_t)v.head * 576;
-#pragma unroll
-      for (int i = 0; i < NQ; ++i)
-        qreg[i] = __builtin_bit_cast(
-            bf16x8_t,
-            (u32x4)*reinterpret_cast<const any_u32x4*>(q + 16 * (DS * i + ds) + 8 * half));
-    }
-    // the first tiles on their way, from the entries of tile 0 on
-    auto begin = [&]() {
-      if constexpr (FP8) {
-        load8(0);
-        load_entry(1);
-        lds_barrier();  // s_bad is clear
-        static_for<9>([&](auto p) { store8(p, 0); });
-        if (n_it > 1) load8(1);
-        load_entry(2);
+    // ---- staging: a wave stages TG groups of eight rows of its token group's tiles ----
+    auto record = [&](int32_t r) {
+      return v.pool + (uint64_t)(uint32_t)r * (uint32_t)a.record_stride;
+    };
+    const uint8_t* src;  // this lane's row (or its rotary dims) of the group at hand
+    auto find_row = [&](int32_t r, int it, int group, bool rope) {
+      const int lane = lane_now();
+      const int in = (tile_base(it) + 8 * group + (lane >> 3)) & ((1 << a.l.tpr_shift) - 1);
+      const int at = rope ? a.l.rope_offset + 128 * in : (int)__umul24(in, a.l.row_bytes);
+      src = (r >= 0 ? record(r) + at : g_zero_row) + stage_piece(lane, group);
+    };
+    // load x of tile `it`: the segments of a group's rows, then the next group's; 8-bit: segment 4 is
+    // the rotary dims, the last load the scales
+    auto direct = [&](auto x, int it) {
+      constexpr int SEGS = FP8 ? 5 : 9, y = x / SEGS, seg = x % SEGS;
+      const int group = TG * rg + y;
+      if constexpr (x < SEGS * TG && (seg == 0 || (FP8 && seg == 4)))
+        find_row(e[y], it, group, seg == 4 && FP8);
+      if constexpr (x == SEGS * TG) {
+        const int lane = lane_now();
+        const int in = (tile_base(it) + scale_token(lane)) & ((1 << a.l.tpr_shift) - 1);
+        load_lds4(es >= 0 ? record(es) + a.l.scale_offset + 4 * in : g_zero_row, scales_at(it));
+      } else if constexpr (!FP8) {
+        stage_block<72, seg>(tile_at(it), group, src);
+      } else if constexpr (seg < 4) {
+        stage_block<32, seg>(tile_at(it), group, src);
       } else {
-        find_row(0);
-        static_for<9>([&](auto p) { direct(p, 0); });
-        load_entry(1);
-        if (n_it > 1) {
-          find_row(1);
-          static_for<9>([&](auto p) { direct(p, 1); });
-        }
-        load_entry(2);
-        lds_barrier();  // s_bad is clear
+        stage_block<8, 0>(tile_at(it) + PTile::BYTES, group, src);
       }
     };
-    // Scores of tile `it` for every row of the wave (a row that sees none of it, or does not exist,
-    // has them masked later or never stored), the next tile's staging in the MFMAs' shadow.
-    auto scores = [&](int it, f32x16& sum, uint32_t& exist) {
-      // tile `it` is stored, and tile it - 1 read, by every wave
-      if constexpr (!FP8) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (partial(tile_base(it))) scrub(it);
-      }
-      lds_barrier();
-      exist = (uint32_t)__ballot(ok_entry(ev));
-      ev = mask_entry(it + 1);
-      const int ahead = FP8 ? it + 1 : it + 2;  // the tile to store next
-      const bool more = ahead < n_it;
-      if constexpr (!FP8) {
-        if (more) find_row(ahead);
-      }
-      const int kr = mla_row(col), sw = tile_swizzle(kr);
-      const uint32_t krow = lds_addr(tile_at(it) + LTile::row(kr));
-      uint32_t ka[NBASE];  // piece 2 kk + half of k-steps kk = DS i + ds, i mod NBASE
-#pragma unroll
-      for (int i = 0; i < NBASE; ++i) ka[i] = krow + (((2 * (DS * i + ds) + half) ^ sw) << 4);
-      constexpr int KD = 4, EVERY = 4 / DS;
-      u32x4 kb[KD];
-      auto kread = [&](auto i) {
-        kb[i % KD] = lds_read_b128<(i / NBASE) * 1024>(ka[i % NBASE]);
-      };
-      f32x16 even, odd;  // two chains of MFMAs
-      static_for<KD>(kread);
-      static_for<NQ>([&](auto i) {
-        constexpr int later = NQ - 1 - i < KD - 1 ? NQ - 1 - i : KD - 1;
-        mfma_qk<later, (i < 2)>((i & 1) ? odd : even, kb[i % KD], qreg[i]);
-        if constexpr (i % EVERY == 0) {
-          constexpr std::integral_constant<int, i / EVERY> piece{};
-          if (more) {
-            if constexpr (FP8) store8(piece, ahead);
-            else direct(piece, ahead);
+    // What is not finite in this wave's rows of a tile, and in its copy of the scales, is cleared.
+    auto scrub = [&](int it) {
+      const int lane = lane_now();
+      int* marks = marks_at(it);
+      for (int y = 0; y < TG; ++y) {
+        const int r = 8 * (TG * rg + y) + (lane >> 3);
+        bool bad = false;
+        for (int x = 0; x < (FP8 ? 4 : 8); ++x) {
+          u32x4* at = reinterpret_cast<u32x4*>(
+                          tile_at(it) + (FP8 ? PTile::row(r) : LTile::row(r)) + x * 1024) +
+                      (lane & 7);
+          u32x4 p = *at;
+          if (FP8 ? clear_bad8(p) : clear_bad(p)) {
+            bad = true;
+            *at = p;
           }
         }
-        if constexpr (i + KD < NQ) kread(std::integral_constant<int, i + KD>{});
-        __builtin_amdgcn_sched_barrier(0);
-      });
-      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" : "+v"(even), "+v"(odd));
-      sum = even + odd;
-      if constexpr (FP8) {
-        if (it + 2 < n_it) load8(it + 2);
+        if (bad) marks[0] = marks[1 + r] = it + 1;
       }
-      load_entry(it + 3);
-      if constexpr (DS > 1) {
+      if constexpr (FP8) {
+        float* at = reinterpret_cast<float*>(scales_at(it)) + (lane & 31);
+        if (!(__builtin_fabsf(*at) <= 3.4028235e38f)) {
+          marks[0] = marks[1 + scale_token(lane & 31)] = it + 1;
+          *at = 0.f;
+        }
+      }
+    };
+    // A wait leaves the direct loads of `younger` later tiles in flight.
+    auto wait_tiles = [&](int younger) {
+      static_for<AHEAD>([&](auto x) {
+        if (younger == x) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(x * LOADS) : "memory");
+      });
+    };
+    auto begin = [&]() {  // the first tiles on their way, e_next holding the first entries
+      store_entries(0);
+      load_entries(1);
+      lds_barrier();
+      store_entries(1);  // read after the loop's barriers
+      load_entries(2);
+      for (int t = 0; t < min(AHEAD, n_it); ++t) {
+        read_entries(t, t);
+        static_for<LOADS>([&](auto x) { direct(x, t); });
+      }
+    };
+    // The start of an iteration: tile `it` is stored, and tile it - 1 read, by every wave. `exist`:
+    // its tokens.
+    auto next_tile = [&](int it) {
+      wait_tiles(min(n_it - 1 - it, AHEAD - 1));
+      if (partial(tile_base(it))) scrub(it);
+      lds_barrier();
+      // the window moves on by 256 tokens
+      constexpr int EVERY = 256 / (TG * CT);
+      if (it % EVERY == 0 && it > 0) {
+        store_entries(it / EVERY + 1);
+        load_entries(it / EVERY + 2);
+      }
+      read_entries(it + AHEAD, it);
+      return (uint32_t)__ballot(ev >= 0);
+    };
+
+    load_entries(0);
+    for (int i = threadIdx.x; i < N_MARKS; i += 256) s_marks[i] = 0;
+    if (!v.group_live) {  // no rows: stages only
+      lds_barrier();      // the query's (below)
+      for (int attempt = 0;; ++attempt) {
+        begin();
+        for (int it = 0; it < n_it; ++it) {
+          next_tile(it);
+          if (it + AHEAD < n_it) static_for<LOADS>([&](auto x) { direct(x, it + AHEAD); });
+        }
+        lds_barrier();
+        if (attempt == 2 || (attempt == 0 && *s_outgrown == 0)) break;
+        load_entries(0);
+      }
+      if constexpr (TG > 1) lds_barrier();
+      return;
+    }
+
+    // ---- Q^T operands, by way of LDS (read in operand order, each load would touch 64 rows): the 32
+    // rows of the wave as one tile of its own, then from k-step kk dims 16 kk + 8 half .. +7; 8-bit:
+    // two k-steps from each 32 dims, 16 half + 0 .. 7 and 8 .. 15 of them, as K's pieces lie ----
+    bf16x8_t qreg[36];
+    {
+      uint8_t* tile = s_mem + wave * LTile::BYTES;
+      const int lane = lane_now();
+      const uint16_t* q = a.q + (int64_t)w.q.begin * a.q_stride + (int64_t)h * a.g * 576;
+      const int row0 = (w.tile * RG + rg) * 32, last = w.q.n * a.g - 1;
+      const bool aligned = (((uintptr_t)q | (uintptr_t)(a.q_stride * 2)) & 15) == 0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          s_scores[ds * 256 + x * 64 + lane] =
-              f32x4{sum[4 * x], sum[4 * x + 1], sum[4 * x + 2], sum[4 * x + 3]};
-        lds_barrier();  // every wave's part of the scores is there
-        // summed in the same order by every wave, so that they agree on every bit
+      for (int y = 0; y < 4; ++y) {
+        const int row = min(row0 + 8 * y + (lane >> 3), last);
+        const int tok = (int)fastdiv(row, a.div_g);
+        const uint8_t* from = reinterpret_cast<const uint8_t*>(q + tok * a.q_stride +
+                                                               (row - tok * a.g) * 576) +
+                              stage_piece(lane, y);
+        if (aligned) {
+          stage_rows<72>(tile, y, from);
+        } else {
+          u32x4* to = reinterpret_cast<u32x4*>(tile + y * LTile::NSEG * 1024) + lane;
+#pragma unroll
+          for (int seg = 0; seg < 9; ++seg)
+            to[seg * 64] = *reinterpret_cast<const any_u32x4*>(from + seg * 128);
+        }
+      }
+      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+      const int half = lane >> 5, col = lane & 31, sw = tile_swizzle(col);
+      const uint32_t at = lds_addr(tile + LTile::row(col));
+      static_for<9>([&](auto i) {  // four reads and their wait in one block
+        uint32_t p[4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          f32x4 y = s_scores[x * 64 + lane];
-#pragma unroll
-          for (int d = 1; d < DS; ++d) y += s_scores[d * 256 + x * 64 + lane];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sum[4 * x + i] = y[i];
+          const int piece = FP8 && i < 8 ? 4 * (x >> 1) + 2 * half + (x & 1) : 2 * x + half;
+          p[x] = at + ((piece ^ sw) << 4);
         }
+        u32x4 r0, r1, r2, r3;
+        asm volatile(
+            "ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%8\n\t"
+            "ds_read_b128 %2, %6 offset:%8\n\tds_read_b128 %3, %7 offset:%8\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(r0), "=&v"(r1), "=&v"(r2), "=&v"(r3)
+            : "v"(p[0]), "v"(p[1]), "v"(p[2]), "v"(p[3]), "n"(i * 1024)
+            : "memory");
+        qreg[4 * i] = __builtin_bit_cast(bf16x8_t, r0);
+        qreg[4 * i + 1] = __builtin_bit_cast(bf16x8_t, r1);
+        qreg[4 * i + 2] = __builtin_bit_cast(bf16x8_t, r2);
+        qreg[4 * i + 3] = __builtin_bit_cast(bf16x8_t, r3);
+      });
+      lds_barrier();  // every wave has its query: the tiles may come
+    }
+
+    // The scales of this lane's 16 scores.
+    auto read_scales = [&](int it, u32x4 (&sc)[4]) {
+      const uint32_t at = lds_addr(scales_at(it)) + 64 * (lane_now() >> 5);
+      asm volatile(
+          "ds_read_b128 %0, %4\n\tds_read_b128 %1, %4 offset:16\n\tds_read_b128 %2, %4 offset:32\n\t"
+          "ds_read_b128 %3, %4 offset:48\n\ts_waitcnt lgkmcnt(0)"
+          : "=&v"(sc[0]), "=&v"(sc[1]), "=&v"(sc[2]), "=&v"(sc[3])
+          : "v"(at));
+    };
+    // Scores of tile `it`, those of tokens that a row does not see -inf, and the next tiles' loads in
+    // the MFMAs' shadow.
+    auto scores = [&](int it, f32x16& sum, u32x4 (&sc)[4]) {
+      const uint32_t exist = next_tile(it);
+      const int ahead = it + AHEAD;
+      const bool more = ahead < n_it;
+      const int lane = lane_now(), half = lane >> 5;
+      const int kr = mla_row(lane & 31), sw = tile_swizzle(kr);
+      const uint32_t krow = lds_addr(tile_at(it)) + (FP8 ? PTile::row(kr) : LTile::row(kr));
+      uint32_t ka[4];  // pieces 2 x + half of a segment
+#pragma unroll
+      for (int x = 0; x < 4; ++x) ka[x] = krow + (((2 * x + half) ^ sw) << 4);
+      f32x16 even, odd;  // two chains of MFMAs; 8-bit: the latent and the rotary part
+      constexpr int NR = FP8 ? 20 : 36, KD = FP8 ? 3 : 4;  // reads, of which in flight
+      u32x4 kb[KD];
+      // 8-bit: 16 reads of two k-steps each, then the rotary four
+      const uint32_t rope = lds_addr(tile_at(it) + PTile::BYTES) + RTile::row(kr) - krow;
+      auto kread = [&](auto x) {
+        if constexpr (FP8 && x >= 16) kb[x % KD] = lds_read_b128<0>(ka[x & 3] + rope);
+        else kb[x % KD] = lds_read_b128<(x / 4) * 1024>(ka[x & 3]);
+      };
+      static_for<KD>(kread);
+      static_for<NR>([&](auto x) {
+        constexpr int later = NR - 1 - x < KD - 1 ? NR - 1 - x : KD - 1;
+        if constexpr (!FP8) {
+          mfma_qk<later, (x < 2)>((x & 1) ? odd : even, kb[x % KD], qreg[x]);
+        } else if constexpr (x < 16) {
+          lgkm_wait1<later>(kb[x % KD]);
+          const u32x4 k = kb[x % KD];
+          mfma_qk<15, (x == 0)>(even, widen(k[0], k[1], 1.f), qreg[2 * x]);
+          mfma_qk<15, false>(even, widen(k[2], k[3], 1.f), qreg[2 * x + 1]);
+        } else {
+          mfma_qk<later, (x == 16)>(odd, kb[x % KD], qreg[16 + x]);
+        }
+        // the next tile's loads, spread over the reads
+        constexpr int from = x * LOADS / NR, to = (x + 1) * LOADS / NR;
+        if constexpr (from < to) {
+          if (more)
+            static_for<to - from>([&](auto y) {
+              direct(std::integral_constant<int, from + y>{}, ahead);
+            });
+        }
+        if constexpr (x + KD < NR) kread(std::integral_constant<int, x + KD>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (FP8) read_scales(it, sc);
+      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" : "+v"(even), "+v"(odd));
+      if constexpr (FP8) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          sum[i] = __builtin_fmaf(even[i], __uint_as_float(sc[i >> 2][i & 3]), odd[i]);
+      } else {
+        sum = even + odd;
       }
       const int base = tile_base(it);
       if (base + CT > v.w_hi || base < v.w_lo || exist != 0xffffffffu)
-        mask_scores(sum, seen_bits(exist, v.row_lo, v.row_hi, base, half));
+        mask_scores(sum, seen_bits(exist, v.row_lo, v.row_hi, base, lane_now() >> 5));
     };
 
-    f32x16 o[NO];
+    // Accumulator tile n holds dims 32 n .. of token group 0's output and dims 32 ((n + 8) % 16) ..
+    // of group 1's, so that at the end each group finishes its tiles 0..7 and leaves the other group
+    // tiles 8..15 with the same code (registers cannot be chosen at run time).
+    f32x16 o[16];
     float m_run = -INFINITY, l_run = 0.f;
-    if (n_it > 0) {
-      begin();
-      // a wait for the query inside the loop would drain the tiles in flight
-#pragma unroll
-      for (int i = 0; i < NQ; ++i) asm volatile("" : "+v"(qreg[i]));
-    }
+    begin();
     for (int attempt = 0;; ++attempt) {
 #pragma unroll
-      for (int n = 0; n < NO; ++n) {
+      for (int n = 0; n < 16; ++n) {
         o[n] = f32x16{};
         asm volatile("" : "+a"(o[n]));
       }
       l_run = 0.f;
       for (int it = 0; it < n_it; ++it) {
         f32x16 s[1];
-        uint32_t exist;
-        scores(it, s[0], exist);
-        // V^T operand by transpose reads, as in Grouped; dims 32 (NO ds + n) are pieces 4 (NO ds +
-        // n) .., segment (NO ds + n) / 2
-        const int vr = 4 * ((lane & 15) >> 2) + half;
-        const int vp = 2 * (col >> 4) + ((lane & 3) >> 1);
-        uint32_t va[2][2];  // [n & 1][first / second read]
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int y = 0; y < 2; ++y)
-            va[n][y] = lds_addr(tile_at(it) + LTile::row(vr + 2 * y) + 8 * (lane & 1) +
-                                ds * (NO / 2) * 1024 +
-                                (((vp + 4 * n) ^ tile_swizzle(vr + 2 * y)) << 4));
-        constexpr int N = 2 * NO, VD = 4;  // MFMA x: tokens 16 (x / NO) .., dims 32 (x % NO) ..
-        v4i16 lo[VD], hi[VD];
-        auto vread = [&](auto x) {
-          constexpr int OFF = (x / NO) * 2 * LTile::NSEG * 1024 + (x % NO) / 2 * 1024;
-          lo[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][0]);
-          hi[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][1]);
-        };
-        static_for<VD>(vread);  // in flight while the weights are worked out
+        u32x4 sc[4];
+        scores(it, s[0], sc);
+        const int lane = lane_now();
+        constexpr int VD = 4;  // MFMA x: tokens 16 (x / 16) .., accumulator tile x % 16
         uint32_t pw[1][8];
-        if (__builtin_expect(__ballot(!(__builtin_fabsf(m_run) <= kFused)) != 0, 0)) {
-          if (m_run == -INFINITY) m_run = largest<1>(s, a.scale_log2);
-          l_run += weights_rounded<1>(pw, s, a.scale_log2, m_run);
-        } else {
-          l_run += weights_of<1>(pw, s, a.scale_log2, m_run);
-        }
-        static_for<N>([&](auto x) {
-          constexpr int later = N - 1 - x < VD - 1 ? N - 1 - x : VD - 1;
-          constexpr int kb = x / NO, n = x % NO;
-          lgkm_wait2<2 * later>(lo[x % VD], hi[x % VD]);
-          const bf16x8_t vt = __builtin_bit_cast(
-              bf16x8_t, __builtin_shufflevector(lo[x % VD], hi[x % VD], 0, 1, 2, 3, 4, 5, 6, 7));
+        auto weights = [&]() {
+          if (__builtin_expect(__ballot(!(__builtin_fabsf(m_run) <= kFused)) != 0, 0)) {
+            if (m_run == -INFINITY) m_run = largest<1>(s, a.scale_log2);
+            l_run += weights_rounded<1>(pw, s, a.scale_log2, m_run, FP8 ? sc : nullptr);
+          } else {
+            l_run += weights_of<1>(pw, s, a.scale_log2, m_run, FP8 ? sc : nullptr);
+          }
+        };
+        auto multiply = [&](auto x, const bf16x8_t& vt) {
+          constexpr int kb = x / 16, n = x % 16;
           o[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
               vt, words(pw[0][4 * kb], pw[0][4 * kb + 1], pw[0][4 * kb + 2], pw[0][4 * kb + 3]),
               o[n], 0, 0, 0);
-          if constexpr (x + VD < N) vread(std::integral_constant<int, x + VD>{});
-          __builtin_amdgcn_sched_barrier(0);
-        });
+        };
+        if constexpr (FP8) {
+          // V^T operand by byte transposes: in each 16-lane group, lane 2s + q addresses 8 bytes of
+          // the token that is s-th in P's order, 16 kb + 4 (s & 3) + 2 (s >> 2) + half; dims 32 n +
+          // 16 (lane / 16 & 1) are piece 2n + (lane / 16 & 1)
+          const int sr = (lane & 15) >> 1, vr = 4 * (sr & 3) + 2 * (sr >> 2) + (lane >> 5);
+          const int vp = (lane >> 4) & 1;
+          uint32_t va[4];  // n & 3
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+            va[n] = lds_addr(tile_at(it) + PTile::row(vr) + 8 * (lane & 1) +
+                             (((2 * n + vp) ^ tile_swizzle(vr)) << 4));
+          u32x2 vb[VD];
+          const uint32_t turn = tg * 2048;
+          auto vread = [&](auto x) {
+            constexpr int OFF = (x / 16) * 2 * PTile::NSEG * 1024 + (x % 16) / 4 * 1024;
+            vb[x % VD] =
+                lds_read_tr8_b64<OFF>(x % 16 < 8 ? va[x & 3] + turn : va[x & 3] - turn);
+          };
+          static_for<VD>(vread);  // in flight while the weights are worked out
+          weights();
+          static_for<32>([&](auto x) {
+            constexpr int later = 31 - x < VD - 1 ? 31 - x : VD - 1;
+            lgkm_wait1<later>(vb[x % VD]);
+            const u32x4 vt = widen(vb[x % VD][0], vb[x % VD][1], 1.f);
+            if constexpr (x + VD < 32) vread(std::integral_constant<int, x + VD>{});
+            multiply(x, __builtin_bit_cast(bf16x8_t, vt));
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        } else {
+          // V^T operand by transpose reads, as in Grouped; dims 32 n .. are pieces 4 n .., segment
+          // n / 2
+          const int vr = 4 * ((lane & 15) >> 2) + (lane >> 5);
+          const int vp = 2 * ((lane & 31) >> 4) + ((lane & 3) >> 1);
+          uint32_t va[2][2];  // [n & 1][first / second read]
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+              va[n][y] = lds_addr(tile_at(it) + LTile::row(vr + 2 * y) + 8 * (lane & 1) +
+                                  (((vp + 4 * n) ^ tile_swizzle(vr + 2 * y)) << 4));
+          v4i16 lo[VD], hi[VD];
+          const uint32_t turn = tg * 4096;
+          auto vread = [&](auto x) {
+            constexpr int OFF = (x / 16) * 2 * LTile::NSEG * 1024 + (x % 16) / 2 * 1024;
+            const uint32_t t = x % 16 < 8 ? turn : 0u - turn;
+            lo[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][0] + t);
+            hi[x % VD] = lds_read_tr16_b64<OFF>(va[x & 1][1] + t);
+          };
+          static_for<VD>(vread);
+          weights();
+          static_for<32>([&](auto x) {
+            constexpr int later = 31 - x < VD - 1 ? 31 - x : VD - 1;
+            lgkm_wait2<2 * later>(lo[x % VD], hi[x % VD]);
+            multiply(x, __builtin_bit_cast(bf16x8_t,
+                                           __builtin_shufflevector(lo[x % VD], hi[x % VD], 0, 1, 2,
+                                                                   3, 4, 5, 6, 7)));
+            if constexpr (x + VD < 32) vread(std::integral_constant<int, x + VD>{});
+            __builtin_amdgcn_sched_barrier(0);
+          });
+        }
         // A latent that is not finite, in a tile that only some rows see, was stored as zeros
         // (zero weights would have made NaN of it). It is key and value at once: what a row that
         // sees it becomes is NaN.
         const int base = tile_base(it);
-        if (partial(base) &&
-            __builtin_amdgcn_readfirstlane(s_bad[(it % NB) * (CT + 1)]) == it + 1) {
-          const uint32_t bad =
-              (uint32_t)__ballot(s_bad[(it % NB) * (CT + 1) + 1 + (lane & 31)] == it + 1);
+        const int* marks = marks_at(it);
+        if (partial(base) && __builtin_amdgcn_readfirstlane(marks[0]) == it + 1) {
+          const uint32_t bad = (uint32_t)__ballot(marks[1 + (threadIdx.x & 31)] == it + 1);
           if (bad & seen_bits(0xffffffffu, v.row_lo, v.row_hi, base, 0)) l_run = NAN;
         }
       }
-      if (attempt == 1) break;
       // some row's weights outgrew its reference? (A sum that is NaN is no reason: it stays so.)
-      if (__ballot(l_run > kWeightLimit) && lane == 0) *s_outgrown = 1;
-      lds_barrier();
-      if (__builtin_expect(__builtin_amdgcn_readfirstlane(*s_outgrown) == 0, 1)) break;
-      load_entry(0);
-      ev = mask_entry(0);
+      if (attempt == 0 && __ballot(l_run > kWeightLimit) && (threadIdx.x & 63) == 0)
+        *s_outgrown = 1;
+      lds_barrier();  // every wave is past its tiles
+      if (attempt == 1 || __builtin_amdgcn_readfirstlane(*s_outgrown) == 0) break;
+      load_entries(0);
       begin();
       m_run = -INFINITY;
       for (int it = 0; it < n_it; ++it) {
         f32x16 s[1];
-        uint32_t exist;
-        scores(it, s[0], exist);
+        u32x4 sc[4];
+        scores(it, s[0], sc);
         m_run = fmaxf(m_run, largest<1>(s, a.scale_log2));
       }
       lds_barrier();  // the last tiles are read
-      load_entry(0);
-      ev = mask_entry(0);
+      load_entries(0);
       begin();
     }
     l_run += __shfl_xor(l_run, 32, 64);
@@ -1157,47 +1323,60 @@ struct Latent {
       }
       return r;
     };
-    if (!v.live) return;
-    const float m = m_run, l = l_run;
-    const bool first = ds == 0 && half == 0;
-    // quad x of tile n: dims 32 (NO ds + n) + 8 x + 4 half .. +3
-    const int dim0 = 32 * NO * ds + 4 * half;
-    if (w.splits > 1) {
-      const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
+    const int lane = lane_now(), half = lane >> 5, col = lane & 31;
+    float m = m_run, l = l_run, mine = 1.f, other = 0.f;
+    f32x4* s_o = reinterpret_cast<f32x4*>(s_mem);  // [wave][8 tiles][4 quads][64 lanes]
+    if constexpr (TG > 1) {
+      float2* s_ml = reinterpret_cast<float2*>(s_mem + ML);
 #pragma unroll
-      for (int n = 0; n < NO; ++n)
+      for (int n = 0; n < 8; ++n)
 #pragma unroll
-        for (int x = 0; x < 4; ++x)
-          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, 4 * (NO * ds + n) + x, lane)) =
-              quad(n, x);
-      if (first) a.part_ml[pr + col] = make_float2(m, l);
-      return;
+        for (int x = 0; x < 4; ++x) s_o[(wave * 32 + 4 * n + x) * 64 + lane] = quad(8 + n, x);
+      if (half == 0) s_ml[wave * 32 + col] = make_float2(m_run, l_run);
+      lds_barrier();
+      const float2 g = s_ml[(wave ^ RG) * 32 + col];
+      m = fmaxf(m_run, g.x);
+      mine = m_run == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run - m);
+      other = g.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(g.x - m);
+      // in the groups' order, so that both halves of a row have one sum
+      l = tg == 0 ? l_run * mine + g.y * other : g.y * other + l_run * mine;
     }
+    const View u = view_of<32 * RG>(a, w, h, rg, col);  // again, rather than kept
     const float inv = l > 0.f ? 1.f / l : l;
+    const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
     uint16_t* out =
-        a.out + (int64_t)(w.q.begin + v.tok) * a.out_stride + (int64_t)v.head * 512 + dim0;
+        a.out + (int64_t)(w.q.begin + u.tok) * a.out_stride + (int64_t)u.head * 512 + 4 * half;
+    static_for<16 / TG>([&](auto n) {
+      const int tile = (n + 8 * tg) & 15;  // its dims
 #pragma unroll
-    for (int n = 0; n < NO; ++n)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) store_bf16x4(out + 32 * n + 8 * x, quad(n, x) * inv);
-    if (a.lse && first)
-      a.lse[(int64_t)(w.q.begin + v.tok) * (a.kv_heads * a.g) + v.head] = natural(m, l);
+      for (int x = 0; x < 4; ++x) {
+        f32x4 r = quad(n, x);
+        if constexpr (TG > 1) {
+          const f32x4 y = s_o[((wave ^ RG) * 32 + 4 * n + x) * 64 + lane];
+          r = tg == 0 ? r * mine + y * other : y * other + r * mine;
+        }
+        if (w.splits > 1)
+          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, 4 * tile + x, lane)) = r;
+        else if (u.live)
+          store_bf16x4(out + 32 * tile + 8 * x, r * inv);
+      }
+    });
+    if (u.live && tg == 0 && half == 0) {
+      if (w.splits > 1) a.part_ml[pr + col] = make_float2(m, l);
+      else if (a.lse)
+        a.lse[(int64_t)(w.q.begin + u.tok) * (a.kv_heads * a.g) + u.head] = natural(m, l);
+    }
   }
 };
 
 template <bool FP8>
 __global__ __launch_bounds__(256, 1) void chunk_latent_kernel(ChunkArgs a) {
-  using L1 = Latent<FP8, 1, 4>;
-  using L2 = Latent<FP8, 2, 2>;
-  using L4 = Latent<FP8, 4, 1>;
-  constexpr int LDS = std::max(std::max(L1::LDS, L2::LDS), L4::LDS);
-  __shared__ __align__(1024) uint8_t s_mem[LDS];
+  __shared__ __align__(1024) uint8_t s_mem[std::max(Latent<FP8, 1>::LDS, Latent<FP8, 2>::LDS)];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
   if (!find_work<true, false>(a, item, w)) return;
-  if (w.groups == 1) L1::run(a, w, h, s_mem);
-  else if (w.groups == 2) L2::run(a, w, h, s_mem);
-  else L4::run(a, w, h, s_mem);
+  if (w.groups == 2) Latent<FP8, 2>::run(a, w, h, s_mem);
+  else Latent<FP8, 1>::run(a, w, h, s_mem);
 }
 
 // Merge of the splits' partial results of 32 rows and 128 dims: SG sets of four waves, each with
@@ -1291,7 +1470,7 @@ struct ChunkPlan {
 };
 
 // Workgroups that splitting aims at. With that many unsplit row tiles the chip is full.
-constexpr int kTargetWorkgroups = 512;
+constexpr int kTargetWorkgroups = 256;
 
 ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& c) {
   ChunkPlan p{};
@@ -1299,33 +1478,40 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   const bool latent = kv.layout == HISPARSE_KV_LATENT;
   const int64_t chunk = std::min<int64_t>(c.max_chunk, std::max(c.total_tokens, 1));
   const int64_t max_rows = chunk * c.q_heads;
-  const int64_t bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent);
   const int64_t tokens = (int64_t)c.max_records * kv.tokens_per_record;
-  // every request has a last row tile that may not be full; the others are of the most rows
-  p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
-  p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / (latent ? 128 : 256) +
-                                  c.num_requests,
-                              (int64_t)c.num_requests * p.uni_tiles);
   const int64_t span =
       c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
   const int64_t blocks = (span + 63) / 64 + 1;  // a first token inside a block adds one
+  int64_t bm = 0;
+  auto count_tiles = [&](bool split) {
+    bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent, split);
+    p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
+    // every request has a last row tile that may not be full; the others are of the most rows
+    const int64_t most = latent ? bm : 256;
+    p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / most + c.num_requests,
+                                (int64_t)c.num_requests * p.uni_tiles);
+  };
   p.max_splits = 1;
   p.uni_splits = 1;
-  p.items = p.tiles;
+  count_tiles(false);
   if (c.num_splits > 0) {
     p.max_splits = (int32_t)std::min<int64_t>(c.num_splits, blocks);
     p.uni_splits = p.max_splits;
+    count_tiles(p.max_splits > 1);
     p.items = p.tiles * p.max_splits;
-  } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > kMinSplitTokens) {
+  } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > min_split(latent)) {
     p.target = kTargetWorkgroups;
+    count_tiles(true);
     const int64_t part = std::max<int64_t>(
-        kMinSplitTokens, ((int64_t)c.num_requests * p.uni_tiles * c.kv_heads * span + p.target -
-                          1) / p.target);
+        min_split(latent), ((int64_t)c.num_requests * p.uni_tiles * c.kv_heads * span +
+                            p.target - 1) / p.target);
     p.uni_splits = (int32_t)std::min<int64_t>((span + part - 1) / part, kMaxSplits);
-    p.max_splits = (int32_t)std::min<int64_t>((span + kMinSplitTokens - 1) / kMinSplitTokens,
+    p.max_splits = (int32_t)std::min<int64_t>((span + min_split(latent) - 1) / min_split(latent),
                                               kMaxSplits);
     p.items = std::min(p.tiles * p.max_splits, p.tiles + p.target / c.kv_heads + 1);
     p.items = std::max(p.items, (int64_t)c.num_requests * p.uni_tiles * p.uni_splits);
+  } else {
+    p.items = p.tiles;
   }
   if (p.max_splits > 1) {
     p.groups = (int32_t)(bm / 32);
@@ -1422,6 +1608,7 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.max_tokens = c->max_records << a.l.tpr_shift;
   a.window = c->window;
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
+  a.split = p.max_splits > 1;
   a.target = p.target;
   a.num_splits = c->num_splits;
   a.uni_tiles = p.uni_tiles;
