@@ -904,14 +904,16 @@ struct Latent {
   static constexpr int LOADS = FP8 ? 5 * TG + 1 : 9 * TG;
   static constexpr int TILE = FP8 ? PTile::BYTES + RTile::BYTES + RG * 256 : LTile::BYTES;
   // LDS: tiles (8-bit: latent rows, rotary dims, a copy of the 32 scales per wave), at whose end the
-  // query passes first and in whose place the token groups' outputs are last; table entries of
-  // WINDOW tokens; bad-token marks; the token groups' (reference, sum) pairs
+  // query passes first and in whose place the token groups' outputs are last; where WINDOW tokens
+  // are (8-bit: also their rotary dims and scales) and which of them exist; bad-token marks; the
+  // token groups' (reference, sum) pairs
   static constexpr int WINDOW = 512;
   static constexpr int ENTRIES = std::max(TG * NB * TILE, 4 * LTile::BYTES);
   static constexpr int QUERY = ENTRIES - RG * LTile::BYTES;
   // the first tiles, clear of the query: sent for before it is here
   static constexpr int EARLY = QUERY / (TG * TILE) < 1 ? 0 : 1;
-  static constexpr int MARKS = ENTRIES + WINDOW * 4;
+  static constexpr int EXIST = ENTRIES + WINDOW * (FP8 ? 24 : 8);
+  static constexpr int MARKS = EXIST + WINDOW / 8;
   static constexpr int N_MARKS = TG * NB * (CT + 1) + 1;  // the last: a row outgrew its reference
   static constexpr int ML = (MARKS + N_MARKS * 4 + 15) / 16 * 16;
   static constexpr int LDS = ML + 4 * 32 * 8;
@@ -928,7 +930,8 @@ struct Latent {
       asm volatile("" : "+v"(x));
       return x;
     };
-    int32_t* s_entry = reinterpret_cast<int32_t*>(s_mem + ENTRIES);
+    uint64_t* s_where = reinterpret_cast<uint64_t*>(s_mem + ENTRIES);
+    uint64_t* s_exist = reinterpret_cast<uint64_t*>(s_mem + EXIST);
     int* s_marks = reinterpret_cast<int*>(s_mem + MARKS);
     int* s_outgrown = s_marks + N_MARKS - 1;
     const View v = view_of<32 * RG>(a, w, h, rg, threadIdx.x & 31);
@@ -941,72 +944,62 @@ struct Latent {
     auto marks_at = [&](int it) { return s_marks + (tg * NB + it % NB) * (CT + 1); };
     auto partial = [&](int base) { return base + CT > v.hi_min || base < v.lo_max; };
 
-    // ---- table entries, checked (-1: no token), of WINDOW tokens from the current 256 on, so that
-    // nothing in the loop waits for a load younger than the tiles' ----
+    // ---- where tokens are, worked out once per token, of WINDOW tokens from the current 256 on, so
+    // that nothing in the loop waits for a load younger than the tiles': offsets from the pool, of
+    // tokens that do not exist those of g_zero_row ----
+    const uint8_t* const zero = zero_row();
     auto load_entry = [&](int block) {  // this thread's of 256 tokens
       const int t = v.t0 + block * 256 + (int)threadIdx.x;
       return t < v.t1 ? v.table[t >> a.l.tpr_shift] : -1;
     };
     auto store_entry = [&](int block, int32_t r) {
-      s_entry[(block & 1) * 256 + threadIdx.x] = r >= 0 && r < a.num_records ? r : -1;
+      const int at = (block & 1) * 256 + threadIdx.x;
+      const bool ok = r >= 0 && r < a.num_records;
+      const uint64_t rec = (uint64_t)(uint32_t)r * (uint32_t)a.record_stride;
+      const uint64_t none = (uint64_t)(uintptr_t)zero - (uint64_t)(uintptr_t)v.pool;
+      const int in = (v.t0 + block * 256 + (int)threadIdx.x) & ((1 << a.l.tpr_shift) - 1);
+      s_where[at] = ok ? rec + __umul24(in, a.l.row_bytes) : none;
+      if constexpr (FP8) {
+        s_where[WINDOW + at] = ok ? rec + a.l.rope_offset + 128 * in : none;
+        // scales lie in the order of the scores: token t's at its place in that order
+        const int t = at & 31, p = 16 * (t & 1) + 8 * (t >> 4) + 4 * ((t >> 1) & 1) + ((t >> 2) & 3);
+        s_where[2 * WINDOW + (at & ~31) + p] = ok ? rec + a.l.scale_offset + 4 * in : none;
+      }
+      const uint64_t mask = __ballot(ok);
+      if ((threadIdx.x & 63) == 0) s_exist[at >> 6] = mask;
     };
     int32_t e_first, e_next;  // of the window's first 256 tokens; of the 256 after the window
     auto load_window = [&]() {
       e_first = load_entry(0);
       e_next = load_entry(1);
     };
-    // the entries of this lane's rows of tile `ahead`, of token lane & 31 of tile `it`, and, 8-bit,
-    // of the token of `ahead` whose scale this lane fetches: scales lie in the order of the scores
-    int32_t e[TG], ev, es;
-    auto scale_token = [](int lane) { return score_token(lane & 15) + ((lane >> 4) & 1); };
-    auto read_entries = [&](int ahead, int it) {
-      const int lane = lane_now();
-      auto at = [&](int t) { return lds_addr(s_entry + (t & (WINDOW - 1))); };
-      const int t = first_token(ahead);
-      const uint32_t p = at(t + 8 * TG * rg + (lane >> 3)), q = at(first_token(it) + (lane & 31));
-      const uint32_t r = FP8 ? at(t + scale_token(lane)) : q;
-      asm volatile(
-          "ds_read_b32 %0, %3\n\tds_read_b32 %1, %4\n\tds_read_b32 %2, %5\n\t"
-          "s_waitcnt lgkmcnt(0)"
-          : "=&v"(e[0]), "=&v"(ev), "=&v"(es)
-          : "v"(p), "v"(q), "v"(r)
-          : "memory");
-      if constexpr (TG == 2)
-        asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)"
-                     : "=&v"(e[1])
-                     : "v"(at(t + 16 * rg + 8 + (lane >> 3)))
-                     : "memory");
-    };
 
     // ---- staging: a wave stages TG groups of eight rows of its token group's tiles ----
-    const uint8_t* const zero = zero_row();
-    auto record = [&](int32_t r) {
-      return v.pool + (uint64_t)(uint32_t)r * (uint32_t)a.record_stride;
+    auto scale_token = [](int place) { return score_token(place & 15) + (place >> 4); };
+    // offset `which` (0 row, 1 rotary dims, 2 scale) of token t (from t0 on)
+    auto where = [&](int which, int t) {
+      const uint32_t at = lds_addr(s_where + which * WINDOW + (t & (WINDOW - 1)));
+      uint64_t x;
+      asm volatile("ds_read_b64 %0, %1\n\ts_waitcnt lgkmcnt(0)" : "=v"(x) : "v"(at) : "memory");
+      return v.pool + x;
     };
     const uint8_t* src;  // this lane's row (or its rotary dims) of the group at hand
-    auto find_row = [&](int32_t r, int it, int group, bool rope) {
-      const int lane = lane_now();
-      const int in = (tile_base(it) + 8 * group + (lane >> 3)) & ((1 << a.l.tpr_shift) - 1);
-      const int at = rope ? a.l.rope_offset + 128 * in : (int)__umul24(in, a.l.row_bytes);
-      src = (r >= 0 ? record(r) + at : zero) + stage_piece(lane, group);
-    };
     // load x of tile `it`: the segments of a group's rows, then the next group's; 8-bit: segment 4 is
     // the rotary dims, the last load the scales
     auto direct = [&](auto x, int it) {
       constexpr int SEGS = FP8 ? 5 : 9, y = x / SEGS, seg = x % SEGS;
       const int group = TG * rg + y;
-      if constexpr (x < SEGS * TG && (seg == 0 || (FP8 && seg == 4)))
-        find_row(e[y], it, group, seg == 4 && FP8);
       if constexpr (x == SEGS * TG) {
-        const int lane = lane_now();
-        const int in = (tile_base(it) + scale_token(lane)) & ((1 << a.l.tpr_shift) - 1);
-        load_lds4(es >= 0 ? record(es) + a.l.scale_offset + 4 * in : zero, scales_at(it));
-      } else if constexpr (!FP8) {
-        stage_block<72, seg>(tile_at(it), group, src);
-      } else if constexpr (seg < 4) {
-        stage_block<32, seg>(tile_at(it), group, src);
+        load_lds4(where(2, first_token(it) + (lane_now() & 31)), scales_at(it));
       } else {
-        stage_block<8, 0>(tile_at(it) + PTile::BYTES, group, src);
+        if constexpr (seg == 0 || (FP8 && seg == 4)) {
+          const int lane = lane_now();
+          src = where(seg == 0 ? 0 : 1, first_token(it) + 8 * group + (lane >> 3)) +
+                stage_piece(lane, group);
+        }
+        if constexpr (!FP8) stage_block<72, seg>(tile_at(it), group, src);
+        else if constexpr (seg < 4) stage_block<32, seg>(tile_at(it), group, src);
+        else stage_block<8, 0>(tile_at(it) + PTile::BYTES, group, src);
       }
     };
     // What is not finite in this wave's rows of a tile, and in its copy of the scales, is cleared.
@@ -1050,10 +1043,8 @@ struct Latent {
       lds_barrier();
     };
     auto begin_tiles = [&](int from, int to) {
-      for (int t = from; t < min(to, n_it); ++t) {
-        read_entries(t, t);
+      for (int t = from; t < min(to, n_it); ++t)
         static_for<LOADS>([&](auto x) { direct(x, t); });
-      }
     };
     // The start of an iteration: tile `it` is stored, and tile it - 1 read, by every wave. `exist`:
     // its tokens.
@@ -1067,8 +1058,13 @@ struct Latent {
         store_entry(it / EVERY + 1, e_next);
         e_next = load_entry(it / EVERY + 2);
       }
-      read_entries(it + AHEAD, it);
-      return (uint32_t)__ballot(ev >= 0);
+      // word (tokens / 32) of the masks
+      uint32_t exist;
+      asm volatile("ds_read_b32 %0, %1\n\ts_waitcnt lgkmcnt(0)"
+                   : "=v"(exist)
+                   : "v"(lds_addr(s_exist) + ((first_token(it) & (WINDOW - 1)) >> 3))
+                   : "memory");
+      return (uint32_t)__builtin_amdgcn_readfirstlane(exist);
     };
 
     load_window();
