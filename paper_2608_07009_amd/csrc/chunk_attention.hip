@@ -1388,19 +1388,30 @@ struct Latent {
     const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
     uint16_t* out =
         a.out + (int64_t)(w.q.begin + u.tok) * a.out_stride + (int64_t)u.head * 512 + 4 * half;
-    static_for<16 / TG>([&](auto n) {
-      const int tile = (n + 8 * tg) & 15;  // its dims
+    // token groups: two accumulator tiles at a time, for the branches between them would make each
+    // read of the other group's wait for itself
+    constexpr int NX = 4 * TG;
+    static_for<64 / TG / NX>([&](auto i) {
+      f32x4 r[NX];
+      if constexpr (TG > 1) {
+        const f32x4* theirs = s_o + ((wave ^ RG) * 32 + NX * i) * 64 + lane;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        f32x4 r = quad(n, x);
-        if constexpr (TG > 1) {
-          const f32x4 y = s_o[((wave ^ RG) * 32 + 4 * n + x) * 64 + lane];
-          r = tg == 0 ? r * mine + y * other : y * other + r * mine;
-        }
-        if (w.splits > 1)
-          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, 4 * tile + x, lane)) = r;
-        else if (u.live)
-          store_bf16x4(out + 32 * tile + 8 * x, r * inv);
+        for (int x = 0; x < NX; ++x) r[x] = theirs[x * 64];
+      }
+#pragma unroll
+      for (int x = 0; x < NX; ++x) {
+        const f32x4 y = quad((NX * i + x) >> 2, x & 3);
+        if constexpr (TG == 1) r[x] = y;
+        else r[x] = tg == 0 ? y * mine + r[x] * other : r[x] * other + y * mine;
+      }
+      const int first = (NX * i + 32 * tg) & 63;  // the quad of dims of the first
+      if (w.splits > 1) {
+#pragma unroll
+        for (int x = 0; x < NX; ++x)
+          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, first + x, lane)) = r[x];
+      } else if (u.live) {
+#pragma unroll
+        for (int x = 0; x < NX; ++x) store_bf16x4(out + 8 * (first + x), r[x] * inv);
       }
     });
     if (u.live && tg == 0 && half == 0) {
