@@ -41,7 +41,7 @@ struct ChunkArgs {
   int64_t num_records, head_part_rows;
   KvLayout l;
   int32_t requests, kv_heads, g, total, max_chunk, max_tokens, window, causal;
-  int32_t split;                // the cached tokens may be split
+  int32_t split;                // row tiles are split as a rule, not only those of long requests
   int32_t target;               // workgroups that splitting aims at (0: none)
   int32_t num_splits;           // asked for (0: chosen)
   int32_t uni_tiles, uni_splits;  // of every request, where they are alike (start and kv_len null)
@@ -100,8 +100,10 @@ __device__ inline int wave_prefix(int x) {  // inclusive
 
 // Item `item` of a kv head's work: MERGE: row tiles, else (row tile, split)s, request by request,
 // each request's tiles from the last (which see most) to the first. Splits follow from the
-// requests' lengths alone: cached tokens in parts of W / (target - row tiles), W the tokens of all
-// row tiles, so that the parts are at most `target` and all start at once.
+// requests' lengths alone: with fewer row tiles than `target`, cached tokens in parts of
+// W / (target - row tiles), W the tokens of all row tiles, so that the parts are at most `target`
+// and all start at once; with more, in parts of W / (2 target), which only the tiles of long
+// requests are split into, so that the last of them ends not long after the others.
 // False if there are fewer items. Wave-uniform.
 template <bool LATENT, bool MERGE>
 __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w) {
@@ -129,6 +131,9 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
   auto span_of = [&](const Request& q) {
     return a.window ? min(q.len, a.window + q.n - 1) : q.len;
   };
+  // the first requests, one a lane: loaded once for both passes
+  Request first{0, 0, 0};
+  if (lane < a.requests) first = request_of(a, lane);
   int part = 0x7fffffff;  // tokens of a split
   if (a.target && !a.num_splits) {
     float sum = 0.f, tiles = 0.f;  // (a rounding of them moves the parts, nothing else)
@@ -136,20 +141,21 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
       const int r = base + lane;
       float x = 0.f, t = 0.f;
       if (r < a.requests) {
-        const Request q = request_of(a, r);
+        const Request q = base == 0 ? first : request_of(a, r);
         int groups;
         t = (float)tiles_of(q, groups);
         x = t * (float)((span_of(q) + 63) >> 6);
       }
       sum += wave_sum(x);
-      tiles += wave_sum(t);
+      if (a.split) tiles += wave_sum(t);
     }
     // every row tile may leave a part that is not full: what is over the tiles is shared out, and a
-    // little less than that, so that there are no more items than the host allows for
-    const float heads = (float)a.kv_heads, over = fmaxf((float)a.target - tiles * heads,
-                                                       0.5f * (float)a.target);
-    const float p = sum * heads * (64.01f / over) + 1.f;
-    part = (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1.5e9f);
+    // little less than that (sums of many requests round), so that there are no more items than the
+    // host allows for
+    const float heads = (float)a.kv_heads, target = (float)a.target;
+    const float over = a.split ? fmaxf(target - tiles * heads, 0.5f * target) : 2.f * target;
+    const float p = sum * heads * (64.1f / over) + 1.f;
+    part = (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
   }
   int items = 0;
   int64_t rows = 0;
@@ -158,13 +164,14 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     Request q{0, 0, 0};
     int groups = 1, tiles = 0, splits = 1;
     if (r < a.requests) {
-      q = request_of(a, r);
+      q = base == 0 ? first : request_of(a, r);
       tiles = tiles_of(q, groups);
       const int span = span_of(q);
       if (a.num_splits) splits = min(a.num_splits, max(1, (span + 63) >> 6));
       else if (a.target) splits = min(max((span + part - 1) / part, 1), kMaxSplits);
     }
-    const int mine = MERGE ? tiles : tiles * splits, mine_rows = tiles * splits * groups;
+    const int mine = MERGE ? tiles : tiles * splits;
+    const int mine_rows = splits > 1 ? tiles * splits * groups : 0;
     const int pi = wave_prefix(mine), pr = wave_prefix(mine_rows);
     const uint64_t hit = __ballot(items + pi > item);
     if (hit) {
@@ -1519,6 +1526,7 @@ struct ChunkPlan {
   int64_t part_rows;     // rows of partial results, all kv heads
   int32_t d_v, target, uni_tiles, uni_splits, max_splits;
   int32_t groups;        // of 32 rows of the largest row tile
+  bool split;            // row tiles are split as a rule, not only those of long requests
   size_t workspace_bytes;
 };
 
@@ -1536,7 +1544,7 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   const int64_t span =
       c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
   const int64_t blocks = (span + 63) / 64 + 1;  // a first token inside a block adds one
-  int64_t bm = 0;
+  int64_t bm = 0, parts = 0;  // rows of a tile; items with partial results
   auto count_tiles = [&](bool split) {
     bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent, split);
     p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
@@ -1551,9 +1559,12 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   if (c.num_splits > 0) {
     p.max_splits = (int32_t)std::min<int64_t>(c.num_splits, blocks);
     p.uni_splits = p.max_splits;
-    count_tiles(p.max_splits > 1);
+    p.split = p.max_splits > 1;
+    count_tiles(p.split);
     p.items = p.tiles * p.max_splits;
+    parts = p.items;
   } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > min_split(latent)) {
+    p.split = true;
     p.target = kTargetWorkgroups;
     count_tiles(true);
     const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
@@ -1566,12 +1577,27 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
                        std::max<int64_t>(p.target / c.kv_heads,
                                          p.tiles + p.target / 2 / c.kv_heads) + 2);
     p.items = std::max(p.items, alike * p.uni_splits);
+    parts = p.items;
   } else {
+    // Parts of W / (2 target): at most 2 target more items than row tiles, and a tile that is split
+    // is longer than one, so that it has at most twice as many as it is long. One request of 65536
+    // 8-bit tokens among 63 of 1000, 8 kv heads x 4: 578 us without, 84 with; latent, 16 heads, among
+    // 299: 2480 and 146. 64 requests of 4096 tokens, which are not split: 109 and 113 for working
+    // that out. Where no request can have four parts of the least length that is not tried (64 of
+    // 512: 25 us, 33).
     p.items = p.tiles;
+    const int64_t more = 2 * kTargetWorkgroups / c.kv_heads;
+    const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
+    if (most >= 4 && more > 0) {
+      p.target = kTargetWorkgroups;
+      p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
+      p.items = std::min(p.tiles * p.max_splits, p.tiles + more);
+      parts = std::min(p.items, 2 * more + 1);
+    }
   }
   if (p.max_splits > 1) {
     p.groups = (int32_t)(bm / 32);
-    p.part_rows = p.items * bm * c.kv_heads;
+    p.part_rows = parts * bm * c.kv_heads;
     p.workspace_bytes = (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2));
   }
   return p;
@@ -1664,7 +1690,7 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.max_tokens = c->max_records << a.l.tpr_shift;
   a.window = c->window;
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
-  a.split = p.max_splits > 1;
+  a.split = p.split;
   a.target = p.target;
   a.num_splits = c->num_splits;
   a.uni_tiles = p.uni_tiles;
@@ -1683,7 +1709,7 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
     if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
   }
-  if (p.max_splits > 1) {
+  if (p.max_splits > 1 && (d_chunk_start || d_kv_len || p.uni_splits > 1)) {
     // few workgroups with many splits each: four times the threads
     const dim3 merge((unsigned)(p.tiles * c->kv_heads), p.groups * (latent ? 4 : 1));
     const bool deep = p.max_splits > 8 && (int64_t)merge.x * merge.y <= kTargetWorkgroups;
