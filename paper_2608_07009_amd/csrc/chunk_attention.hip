@@ -43,6 +43,8 @@ struct ChunkArgs {
   int32_t requests, kv_heads, g, total, max_chunk, max_tokens, window, causal;
   int32_t split;                // row tiles are split as a rule, not only those of long requests
   int32_t target;               // workgroups that splitting aims at (0: none)
+  int32_t* n_split;             // where few row tiles are split: how many of a kv head, left for the
+                                // merge by the last workgroup; or NULL
   int32_t num_splits;           // asked for (0: chosen)
   int32_t uni_tiles, uni_splits;  // of every request, where they are alike (start and kv_len null)
   FastDiv div_g;
@@ -98,12 +100,84 @@ __device__ inline int wave_prefix(int x) {  // inclusive
   return x;
 }
 
-// Item `item` of a kv head's work: MERGE: row tiles, else (row tile, split)s, request by request,
-// each request's tiles from the last (which see most) to the first. Splits follow from the
-// requests' lengths alone: with fewer row tiles than `target`, cached tokens in parts of
-// W / (target - row tiles), W the tokens of all row tiles, so that the parts are at most `target`
-// and all start at once; with more, in parts of W / (2 target), which only the tiles of long
-// requests are split into, so that the last of them ends not long after the others.
+// Row tiles of a request, of `groups` groups of 32 rows.
+template <bool LATENT>
+__device__ __forceinline__ int tiles_of(const ChunkArgs& a, const Request& q, int& groups) {
+  const int rows = q.n * a.g;
+  groups = row_groups(rows, LATENT, a.split);
+  return (rows + 32 * groups - 1) / (32 * groups);
+}
+// Splits follow from the requests' lengths alone: with fewer row tiles than `target`, cached tokens
+// in parts of W / (target - row tiles), W the tokens of all row tiles, so that the parts are at most
+// `target` and all start at once; with more, in parts of W / (2 target), which only the tiles of
+// long requests are split into, so that the last of them ends not long after the others.
+__device__ __forceinline__ int span_of(const ChunkArgs& a, const Request& q) {
+  return a.window ? min(q.len, a.window + q.n - 1) : q.len;
+}
+template <bool LATENT>
+__device__ __forceinline__ int part_of(const ChunkArgs& a, const Request& first) {
+  if (!a.target || a.num_splits) return 0;
+  const int lane = threadIdx.x & 63;
+  float sum = 0.f, tiles = 0.f;  // (a rounding of them moves the parts, nothing else)
+  for (int base = 0; base < a.requests; base += 64) {
+    const int r = base + lane;
+    float x = 0.f, t = 0.f;
+    if (r < a.requests) {
+      const Request q = base == 0 ? first : request_of(a, r);
+      int groups;
+      t = (float)tiles_of<LATENT>(a, q, groups);
+      x = t * (float)((span_of(a, q) + 63) >> 6);
+    }
+    sum += wave_sum(x);
+    if (a.split) tiles += wave_sum(t);
+  }
+  // every row tile may leave a part that is not full: what is over the tiles is shared out, and a
+  // little less than that (sums of many requests round), so that there are no more items than the
+  // host allows for
+  const float heads = (float)a.kv_heads, target = (float)a.target;
+  const float over = a.split ? fmaxf(target - tiles * heads, 0.5f * target) : 2.f * target;
+  const float p = sum * heads * (64.1f / over) + 1.f;
+  return (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
+}
+__device__ __forceinline__ int splits_of(const ChunkArgs& a, const Request& q, int part) {
+  const int span = span_of(a, q);
+  if (a.num_splits) return min(a.num_splits, max(1, (span + 63) >> 6));
+  return a.target ? min(max((span + part - 1) / part, 1), kMaxSplits) : 1;
+}
+__device__ __forceinline__ Request first_request(const ChunkArgs& a) {
+  const int lane = threadIdx.x & 63;
+  return lane < a.requests ? request_of(a, lane) : Request{0, 0, 0};
+}
+
+// How many row tiles of a kv head are split. Wave-uniform.
+template <bool LATENT>
+__device__ __forceinline__ int split_tiles(const ChunkArgs& a) {
+  const int lane = threadIdx.x & 63;
+  const Request first = first_request(a);
+  const int part = part_of<LATENT>(a, first);
+  int n = 0;
+  for (int base = 0; base < a.requests; base += 64) {
+    const int r = base + lane;
+    int groups, tiles = 0;
+    if (r < a.requests) {
+      const Request q = base == 0 ? first : request_of(a, r);
+      if (splits_of(a, q, part) > 1) tiles = tiles_of<LATENT>(a, q, groups);
+    }
+    n += __builtin_amdgcn_readlane(wave_prefix(tiles), 63);
+  }
+  return n;
+}
+
+template <bool LATENT>
+__device__ __forceinline__ void leave_split_tiles(const ChunkArgs& a) {
+  if (a.n_split && blockIdx.x == gridDim.x - 1) {
+    const int n = split_tiles<LATENT>(a);
+    if (threadIdx.x == 0) *a.n_split = n;
+  }
+}
+
+// Item `item` of a kv head's work: MERGE: row tiles that are split, else (row tile, split)s, request
+// by request, each request's tiles from the last (which see most) to the first.
 // False if there are fewer items. Wave-uniform.
 template <bool LATENT, bool MERGE>
 __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w) {
@@ -123,40 +197,8 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     w.tile = a.uni_tiles - 1 - w.tile;
     return true;
   }
-  auto tiles_of = [&](const Request& q, int& groups) {
-    const int rows = q.n * a.g;
-    groups = row_groups(rows, LATENT, a.split);
-    return (rows + 32 * groups - 1) / (32 * groups);
-  };
-  auto span_of = [&](const Request& q) {
-    return a.window ? min(q.len, a.window + q.n - 1) : q.len;
-  };
-  // the first requests, one a lane: loaded once for both passes
-  Request first{0, 0, 0};
-  if (lane < a.requests) first = request_of(a, lane);
-  int part = 0x7fffffff;  // tokens of a split
-  if (a.target && !a.num_splits) {
-    float sum = 0.f, tiles = 0.f;  // (a rounding of them moves the parts, nothing else)
-    for (int base = 0; base < a.requests; base += 64) {
-      const int r = base + lane;
-      float x = 0.f, t = 0.f;
-      if (r < a.requests) {
-        const Request q = base == 0 ? first : request_of(a, r);
-        int groups;
-        t = (float)tiles_of(q, groups);
-        x = t * (float)((span_of(q) + 63) >> 6);
-      }
-      sum += wave_sum(x);
-      if (a.split) tiles += wave_sum(t);
-    }
-    // every row tile may leave a part that is not full: what is over the tiles is shared out, and a
-    // little less than that (sums of many requests round), so that there are no more items than the
-    // host allows for
-    const float heads = (float)a.kv_heads, target = (float)a.target;
-    const float over = a.split ? fmaxf(target - tiles * heads, 0.5f * target) : 2.f * target;
-    const float p = sum * heads * (64.1f / over) + 1.f;
-    part = (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
-  }
+  const Request first = first_request(a);  // loaded once for both passes
+  const int part = part_of<LATENT>(a, first);
   int items = 0;
   int64_t rows = 0;
   for (int base = 0; base < a.requests; base += 64) {
@@ -165,12 +207,10 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     int groups = 1, tiles = 0, splits = 1;
     if (r < a.requests) {
       q = base == 0 ? first : request_of(a, r);
-      tiles = tiles_of(q, groups);
-      const int span = span_of(q);
-      if (a.num_splits) splits = min(a.num_splits, max(1, (span + 63) >> 6));
-      else if (a.target) splits = min(max((span + part - 1) / part, 1), kMaxSplits);
+      tiles = tiles_of<LATENT>(a, q, groups);
+      splits = splits_of(a, q, part);
     }
-    const int mine = MERGE ? tiles : tiles * splits;
+    const int mine = !MERGE ? tiles * splits : splits > 1 ? tiles : 0;
     const int mine_rows = splits > 1 ? tiles * splits * groups : 0;
     const int pi = wave_prefix(mine), pr = wave_prefix(mine_rows);
     const uint64_t hit = __ballot(items + pi > item);
@@ -872,6 +912,7 @@ struct Grouped {
 template <bool FP8>
 __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
   __shared__ __align__(1024) uint8_t s_mem[kGroupedLds];
+  leave_split_tiles<false>(a);
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
   if (!find_work<false, false>(a, item, w)) return;
@@ -1166,9 +1207,7 @@ struct Latent {
           : "v"(at));
     };
     // The loads of the tile AHEAD of the one at hand go out between its MFMAs, SOON of them between
-    // the scores', the others between the output's: the CU takes one of its waves' loads about every
-    // 16 cycles, and a wave whose load has to wait issues no MFMAs (all of them between the scores'
-    // of a workgroup of two token groups: 2550 cycles for those, of which 1152 MFMAs).
+    // the scores', the others between the output's.
     constexpr int SOON = LOADS / 2;
     auto send = [&](auto from, auto to, int it) {
       if constexpr (from < to) {
@@ -1432,6 +1471,7 @@ struct Latent {
 template <bool FP8>
 __global__ __launch_bounds__(256, 1) void chunk_latent_kernel(ChunkArgs a) {
   __shared__ __align__(1024) uint8_t s_mem[std::max(Latent<FP8, 1>::LDS, Latent<FP8, 2>::LDS)];
+  leave_split_tiles<true>(a);
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
   Work w;
   if (!find_work<true, false>(a, item, w)) return;
@@ -1449,8 +1489,9 @@ __global__ __launch_bounds__(256 * SG) void chunk_merge_kernel(ChunkArgs a) {
   __shared__ float s_m[32], s_l[32], s_red[SG * 8][32];
   __shared__ f32x4 s_o[SG][16][64];
   const int item = blockIdx.x / a.kv_heads, h = blockIdx.x - item * a.kv_heads;
+  if (a.n_split && item >= *a.n_split) return;  // 512 latent row tiles, none split: 5 us, not 17
   Work w;
-  if (!find_work<(DV == 512), true>(a, item, w) || w.splits == 1) return;
+  if (!find_work<(DV == 512), true>(a, item, w)) return;
   const int group = blockIdx.y / (DV / 128), block = blockIdx.y % (DV / 128);
   const int n_rows = w.q.n * a.g, row0 = (w.tile * w.groups + group) * 32;
   if (group >= w.groups || row0 >= n_rows) return;
@@ -1598,7 +1639,8 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   if (p.max_splits > 1) {
     p.groups = (int32_t)(bm / 32);
     p.part_rows = parts * bm * c.kv_heads;
-    p.workspace_bytes = (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2));
+    p.workspace_bytes =
+        (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2)) + sizeof(int32_t);
   }
   return p;
 }
@@ -1692,6 +1734,10 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
   a.split = p.split;
   a.target = p.target;
+  const bool ragged = d_chunk_start || d_kv_len;
+  const bool merges = p.max_splits > 1 && (ragged || p.uni_splits > 1);
+  if (merges && p.target && !p.split)
+    a.n_split = reinterpret_cast<int32_t*>(a.part_ml + p.part_rows);
   a.num_splits = c->num_splits;
   a.uni_tiles = p.uni_tiles;
   a.uni_splits = p.uni_splits;
@@ -1709,7 +1755,7 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
     if (fp8) hipLaunchKernelGGL(chunk_grouped_kernel<true>, grid, dim3(512), 0, s, a);
     else hipLaunchKernelGGL(chunk_grouped_kernel<false>, grid, dim3(512), 0, s, a);
   }
-  if (p.max_splits > 1 && (d_chunk_start || d_kv_len || p.uni_splits > 1)) {
+  if (merges) {
     // few workgroups with many splits each: four times the threads
     const dim3 merge((unsigned)(p.tiles * c->kv_heads), p.groups * (latent ? 4 : 1));
     const bool deep = p.max_splits > 8 && (int64_t)merge.x * merge.y <= kTargetWorkgroups;
