@@ -1730,7 +1730,7 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.total = c->total_tokens;
   a.max_chunk = std::min(c->max_chunk, c->total_tokens);
   a.max_tokens = c->max_records << a.l.tpr_shift;
-  a.window = c->window;
+  a.window = c->window < a.max_tokens ? c->window : 0;  // (its sums stay in 32 bits)
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
   a.split = p.split;
   a.target = p.target;

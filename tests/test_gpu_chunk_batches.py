@@ -67,6 +67,15 @@ def test_long_windows(kind, type_, tpr, splits):
 
 
 @pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 30, 4096])
+def test_windows_longer_than_any_request(kind, type_, tpr, window):
+    """Nothing is cut off, also where a request has fewer cached than new tokens."""
+    lens = [(9, 700), (1, 900), (40, 3), (5, 5), (0, 9)] + decoding(60, 300, 4)
+    run(kind, type_, tpr, 1, 4, lens, window=window)
+    run(kind, type_, tpr, 1, 4, lens, window=window, splits=1)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
 @pytest.mark.parametrize("q_heads,splits", [(2, 1), (16, 1), (16, 2)])
 def test_long_contexts_whose_scores_grow(kind, type_, tpr, q_heads, splits):
     p = Problem(kind, type_, tpr, 1, q_heads, [(12, 1000), (1, 600)], splits=splits)
