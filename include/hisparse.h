@@ -592,7 +592,8 @@ hisparse_status_t hisparse_validate_kv(const hisparse_kv_desc_t* kv);
  * Nothing but the slots' own rows and scales is written. num_tokens 0 does nothing.
  * HISPARSE_ERR_INVALID_ARG for a bad descriptor, null pointers, d_pool not a multiple of 16, heads
  * < 1, num_tokens < 0, negative strides, or head_stride < record_bytes with several heads;
- * HISPARSE_ERR_UNSUPPORTED if num_tokens * heads is 2^31 or more. */
+ * HISPARSE_ERR_UNSUPPORTED if num_tokens * heads is more than 2^28 - 16 (grouped) or 2^26 - 4
+ * (latent): one launch. */
 hisparse_status_t hisparse_write_tokens(const hisparse_kv_desc_t* kv, int32_t heads,
                                         int32_t num_tokens, const void* d_k,
                                         int64_t k_token_stride, const void* d_v,
@@ -600,9 +601,9 @@ hisparse_status_t hisparse_write_tokens(const hisparse_kv_desc_t* kv, int32_t he
                                         void* d_pool, void* stream);
 
 /* [async] The reverse: the rows that num_tokens token slots hold, in bf16 (8-bit values exactly), to
- * d_k and d_v laid out as above. A slot outside the pool
- * gives rows of zeros. Slots may repeat. Errors as above; a token stride below heads * dims is
- * HISPARSE_ERR_INVALID_ARG too where num_tokens > 1 (the rows would overlap). */
+ * d_k and d_v laid out as above. A slot outside the pool gives rows of zeros. Slots may repeat.
+ * Errors as above; a token stride below heads * dims is HISPARSE_ERR_INVALID_ARG too where num_tokens
+ * > 1 (the rows would overlap). */
 hisparse_status_t hisparse_read_tokens(const hisparse_kv_desc_t* kv, int32_t heads,
                                        int32_t num_tokens, const void* d_pool,
                                        const int64_t* d_slots, void* d_k, int64_t k_token_stride,
@@ -673,9 +674,11 @@ size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
  * A new token that sees no cached token gives zeros and an lse of -inf. Scores, their maximum and
  * sums are kept in fp32; softmax weights are rounded to bf16 for the product with V. Rows that are
  * not seen (padding, later tokens, tokens before the window, page ends) have no influence, whatever
- * they hold, infinities and NaN included. Results do not depend on where records lie.
+ * they hold, infinities and NaN included; one that is seen and holds such a value makes results not
+ * finite (latent: NaN). Results do not depend on where records lie.
  * HISPARSE_ERR_INVALID_ARG for bad descriptors, null or misaligned pointers, or a workspace too
- * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more. */
+ * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more, or where
+ * one launch would need 2^32 threads (512 for each 256 or fewer rows, kv head and split). */
 hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
                                            const hisparse_chunk_desc_t* chunk, const void* d_pool,
                                            const int32_t* d_table, const int32_t* d_chunk_start,

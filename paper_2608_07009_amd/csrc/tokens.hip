@@ -213,7 +213,9 @@ hisparse_status_t token_args(const hisparse_kv_desc_t* kv, int32_t heads, int32_
       (uintptr_t)v % 2 != 0 || (uintptr_t)slots % 8 != 0)
     return HISPARSE_ERR_INVALID_ARG;
   if (heads > 1 && kv->head_stride < kv->record_bytes) return HISPARSE_ERR_INVALID_ARG;
-  if ((int64_t)tokens * heads > (int64_t)INT32_MAX) return HISPARSE_ERR_UNSUPPORTED;
+  // a launch's threads are counted in 32 bits
+  const int64_t lanes = kv->layout == HISPARSE_KV_GROUPED ? 16 : 64;
+  if ((int64_t)tokens * heads > ((int64_t)UINT32_MAX - 255) / lanes) return HISPARSE_ERR_UNSUPPORTED;
   a->pool = const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(pool));
   a->k = const_cast<uint16_t*>(reinterpret_cast<const uint16_t*>(k));
   a->v = const_cast<uint16_t*>(reinterpret_cast<const uint16_t*>(v));

@@ -122,6 +122,29 @@ def test_write_one_row_to_every_token():
     write_and_check(G, F8, 16, 2, k, v, None, 3, wide=wide)
 
 
+@pytest.mark.parametrize("kind,type_,tpr", SHAPES)
+def test_two_rows_for_one_slot_leave_the_others_alone(kind, type_, tpr):
+    n, heads, records = 33, 2, (64 + tpr - 1) // tpr
+    k, v = rows(kind, 4, n, heads)
+    slots = torch.arange(n) * 61 % 64  # its order shuffled, all different
+    twice = torch.cat((slots, slots[5:6]))
+    R = hs.hisparse_kv_record_bytes(kind, type_, tpr)
+    pools = []
+    for s, kk, vv in ((slots, k, v), (twice, torch.cat((k, k[:1])), torch.cat((v, v[:1])))):
+        pool = torch.full((records, heads, R), 0xA5, dtype=torch.uint8, device="cuda")
+        hs.hisparse_write_tokens(desc(kind, type_, tpr, pool), heads, len(s), kk.cuda(),
+                                 kk.stride(0), vv.cuda(), vv.stride(0), s.cuda(), pool,
+                                 torch.cuda.current_stream())
+        pools.append(ref.views(kind, type_, tpr, pool.cpu()))
+    rec, off = int(slots[5]) // tpr, int(slots[5]) % tpr
+    for name, a in pools[0].items():
+        b = pools[1][name]
+        a, b = (x.view(torch.uint8) if x.dtype == torch.float8_e4m3fn else x for x in (a, b))
+        a[rec, :, off] = 0
+        b[rec, :, off] = 0
+        assert torch.equal(a, b)
+
+
 def special_rows(kind):
     """One token per special case, in both rows."""
     inf, nan, big = math.inf, math.nan, 3.3895e38  # the largest bf16 number

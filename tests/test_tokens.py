@@ -141,6 +141,27 @@ def test_token_calls_refused(fn):
         hs.hisparse_read_tokens(kv(), 2, 0, None, None, None, 256, None, 256)
 
 
+@pytest.mark.parametrize("layout,most", [(G, (1 << 28) - 16), (L, (1 << 26) - 4)])
+def test_more_tokens_than_one_launch_takes(layout, most):
+    x = np.zeros(64, np.uint8)
+    base = (x.ctypes.data + 15) // 16 * 16
+    d = kv(layout, tpr=1, record_bytes=656, record_stride=656, head_stride=0)
+    for call in (lambda n: hs.hisparse_write_tokens(d, 1, n, base, 512, base, 512, None, base),
+                 lambda n: hs.hisparse_read_tokens(d, 1, n, base, None, base, 512, base, 512)):
+        for n in (most + 1, 2 ** 31 - 1):
+            with pytest.raises(hs.HisparseError) as e:
+                call(n)
+            assert e.value.status == UNSUPPORTED
+
+
+def test_more_parts_than_one_launch_takes():
+    c = dict(num_requests=1, kv_heads=1, q_heads=256, total_tokens=1 << 22, max_chunk=1 << 22,
+             out_token_stride=256 * 128)
+    d = kv()
+    assert hs.hisparse_validate_chunk(d, chunk(**c)) == hs.HISPARSE_OK
+    assert hs.hisparse_validate_chunk(d, chunk(**c, num_splits=4)) == UNSUPPORTED
+
+
 def test_reference_rounding_is_torch_e4m3():
     g = torch.Generator().manual_seed(1)
     x = torch.randn(20000, generator=g, dtype=torch.float64) * torch.exp2(
