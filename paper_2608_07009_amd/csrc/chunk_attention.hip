@@ -129,13 +129,14 @@ __device__ __forceinline__ int part_of(const ChunkArgs& a, const Request& first)
       x = t * (float)((span_of(a, q) + 63) >> 6);
     }
     sum += wave_sum(x);
-    if (a.split) tiles += wave_sum(t);
+    tiles += wave_sum(t);
   }
   // every row tile may leave a part that is not full: what is over the tiles is shared out, and a
   // little less than that (sums of many requests round), so that there are no more items than the
   // host allows for
   const float heads = (float)a.kv_heads, target = (float)a.target;
-  const float over = a.split ? fmaxf(target - tiles * heads, 0.5f * target) : 2.f * target;
+  const float over = tiles * heads < target ? fmaxf(target - tiles * heads, 0.5f * target)
+                                            : 2.f * target;
   const float p = sum * heads * (64.1f / over) + 1.f;
   return (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
 }
@@ -1596,7 +1597,7 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   };
   p.max_splits = 1;
   p.uni_splits = 1;
-  count_tiles(false);
+  count_tiles(true);
   if (c.num_splits > 0) {
     p.max_splits = (int32_t)std::min<int64_t>(c.num_splits, blocks);
     p.uni_splits = p.max_splits;
@@ -1605,9 +1606,10 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     p.items = p.tiles * p.max_splits;
     parts = p.items;
   } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > min_split(latent)) {
+    // (latent: tiles of 64 rows; as soon as those would be more than the CUs, tiles of 128 rows: 190
+    // requests of 128 heads over 2048 16-bit tokens 150 us, 202 with 64; 240 8-bit ones 190, 208)
     p.split = true;
     p.target = kTargetWorkgroups;
-    count_tiles(true);
     const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
     p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
     // requests alike: as many splits as all start at once
@@ -1626,6 +1628,7 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     // 299: 2480 and 146. 64 requests of 4096 tokens, which are not split: 109 and 113 for working
     // that out. Where no request can have four parts of the least length that is not tried (64 of
     // 512: 25 us, 33).
+    count_tiles(false);
     p.items = p.tiles;
     const int64_t more = 2 * kTargetWorkgroups / c.kv_heads;
     const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
