@@ -1605,22 +1605,25 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     count_tiles(p.split);
     p.items = p.tiles * p.max_splits;
     parts = p.items;
-  } else if (p.tiles * c.kv_heads < kTargetWorkgroups && span > min_split(latent)) {
+  } else if (p.tiles * c.kv_heads < kTargetWorkgroups) {
     // (latent: tiles of 64 rows; as soon as those would be more than the CUs, tiles of 128 rows: 190
     // requests of 128 heads over 2048 16-bit tokens 150 us, 202 with 64; 240 8-bit ones 190, 208)
     p.split = true;
-    p.target = kTargetWorkgroups;
-    const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
-    p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
-    // requests alike: as many splits as all start at once
-    const int64_t alike = (int64_t)c.num_requests * p.uni_tiles;
-    p.uni_splits = (int32_t)std::min<int64_t>(
-        p.max_splits, std::max<int64_t>(1, p.target / (alike * c.kv_heads)));
-    p.items = std::min(p.tiles * p.max_splits,
-                       std::max<int64_t>(p.target / c.kv_heads,
-                                         p.tiles + p.target / 2 / c.kv_heads) + 2);
-    p.items = std::max(p.items, alike * p.uni_splits);
-    parts = p.items;
+    p.items = p.tiles;
+    if (span > min_split(latent)) {
+      p.target = kTargetWorkgroups;
+      const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
+      p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
+      // requests alike: as many splits as all start at once
+      const int64_t alike = (int64_t)c.num_requests * p.uni_tiles;
+      p.uni_splits = (int32_t)std::min<int64_t>(
+          p.max_splits, std::max<int64_t>(1, p.target / (alike * c.kv_heads)));
+      p.items = std::min(p.tiles * p.max_splits,
+                         std::max<int64_t>(p.target / c.kv_heads,
+                                           p.tiles + p.target / 2 / c.kv_heads) + 2);
+      p.items = std::max(p.items, alike * p.uni_splits);
+      parts = p.items;
+    }
   } else {
     // Parts of W / (2 target): at most 2 target more items than row tiles, and a tile that is split
     // is longer than one, so that it has at most twice as many as it is long. One request of 65536
