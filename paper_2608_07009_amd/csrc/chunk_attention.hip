@@ -85,19 +85,29 @@ struct Work {
   int64_t part_row;  // first partial-result row of the tile's split 0
 };
 
-__device__ inline float wave_sum(float x) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d, 64);
-  return x;
+// Lane moves inside the vector unit (a shuffle by way of LDS takes about ten times as long).
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int moved(int x) {  // 0 where nothing comes from
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
-__device__ inline int wave_prefix(int x) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d, 64);
-    if (lane >= d) x += y;
-  }
-  return x;
+__device__ __forceinline__ float wave_sum(float x) {
+  auto add = [&](int y) { x += __int_as_float(y); };
+  add(moved<0x128>(__float_as_int(x)));  // 16 lanes: rotations by 8, 4, 2, 1
+  add(moved<0x124>(__float_as_int(x)));
+  add(moved<0x122>(__float_as_int(x)));
+  add(moved<0x121>(__float_as_int(x)));
+  auto of = [&](int lane) {
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+  };
+  return (of(0) + of(16)) + (of(32) + of(48));
+}
+__device__ __forceinline__ int wave_prefix(int x) {  // inclusive
+  x += moved<0x111>(x);  // 16 lanes: shifts by 1, 2, 4, 8
+  x += moved<0x112>(x);
+  x += moved<0x114>(x);
+  x += moved<0x118>(x);
+  x += moved<0x142, 0xa>(x);         // lane 15 of rows 0 and 2 to the row behind
+  return x + moved<0x143, 0xc>(x);  // lane 31 to the upper half
 }
 
 // Row tiles of a request, of `groups` groups of 32 rows.
@@ -107,13 +117,21 @@ __device__ __forceinline__ int tiles_of(const ChunkArgs& a, const Request& q, in
   groups = row_groups(rows, LATENT, a.split);
   return (rows + 32 * groups - 1) / (32 * groups);
 }
-// Splits follow from the requests' lengths alone: with fewer row tiles than `target`, cached tokens
-// in parts of W / (target - row tiles), W the tokens of all row tiles, so that the parts are at most
-// `target` and all start at once; with more, in parts of W / (2 target), which only the tiles of
-// long requests are split into, so that the last of them ends not long after the others.
 __device__ __forceinline__ int span_of(const ChunkArgs& a, const Request& q) {
   return a.window ? min(q.len, a.window + q.n - 1) : q.len;
 }
+__device__ __forceinline__ int splits_of(const ChunkArgs& a, const Request& q, int part) {
+  const int span = span_of(a, q);
+  if (a.num_splits) return min(a.num_splits, max(1, (span + 63) >> 6));
+  return a.target ? min(max((span + part - 1) / part, 1), kMaxSplits) : 1;
+}
+// Splits follow from the requests' lengths alone. With fewer row tiles than `target`, cached tokens
+// lie in parts of W / target, W the tokens of all row tiles, if those are at most `target` parts (a
+// tile's last may be short), so that all start at once; else of 4/3 of that, or of W / (target - row
+// tiles) if that is less: with those they always are. (16 requests of 4096 8-bit tokens, 8 kv heads x 4,
+// 128 row tiles: 40 us in two parts each, 52 in one.) With more row tiles, in parts of W / (2 target),
+// which only the tiles of long requests are split into, so that the last of them ends not long after
+// the others.
 template <bool LATENT>
 __device__ __forceinline__ int part_of(const ChunkArgs& a, const Request& first) {
   if (!a.target || a.num_splits) return 0;
@@ -131,19 +149,29 @@ __device__ __forceinline__ int part_of(const ChunkArgs& a, const Request& first)
     sum += wave_sum(x);
     tiles += wave_sum(t);
   }
-  // every row tile may leave a part that is not full: what is over the tiles is shared out, and a
-  // little less than that (sums of many requests round), so that there are no more items than the
-  // host allows for
   const float heads = (float)a.kv_heads, target = (float)a.target;
-  const float over = tiles * heads < target ? fmaxf(target - tiles * heads, 0.5f * target)
-                                            : 2.f * target;
-  const float p = sum * heads * (64.1f / over) + 1.f;
-  return (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
-}
-__device__ __forceinline__ int splits_of(const ChunkArgs& a, const Request& q, int part) {
-  const int span = span_of(a, q);
-  if (a.num_splits) return min(a.num_splits, max(1, (span + 63) >> 6));
-  return a.target ? min(max((span + part - 1) / part, 1), kMaxSplits) : 1;
+  // (a little more: sums of many requests round, and the host allows for so many items only)
+  auto part = [&](float parts) {
+    const float p = sum * heads * (64.1f / parts) + 1.f;
+    return (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
+  };
+  if (tiles * heads >= target) return part(2.f * target);
+  const float sure = fmaxf(target - tiles * heads, 0.5f * target);
+  for (float parts = target; parts > sure; parts -= 0.25f * target) {
+    const int p = part(parts);
+    float items = 0.f;
+    for (int base = 0; base < a.requests; base += 64) {
+      const int r = base + lane;
+      int groups, n = 0;
+      if (r < a.requests) {
+        const Request q = base == 0 ? first : request_of(a, r);
+        n = tiles_of<LATENT>(a, q, groups) * splits_of(a, q, p);
+      }
+      items += wave_sum((float)n);
+    }
+    if (items * heads <= target) return p;
+  }
+  return part(sure);
 }
 __device__ __forceinline__ Request first_request(const ChunkArgs& a) {
   const int lane = threadIdx.x & 63;
