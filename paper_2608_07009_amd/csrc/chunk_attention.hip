@@ -51,6 +51,14 @@ struct ChunkArgs {
   float scale_log2;
 };
 
+// The kernel's arguments once more: what is read from here is loaded then, and not kept in scalar
+// registers through a loop that is short of them.
+__device__ __forceinline__ const ChunkArgs& arguments_again() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const ChunkArgs*)p;
+}
+
 // ---- which piece of the call a workgroup does ------------------------------------------------
 
 // Rows (new token, query head of the kv head) of one workgroup, in groups of 32; what waves are left
@@ -899,7 +907,7 @@ struct Grouped {
         for (int t = 0; t < TG; ++t)
           r[x] += s_o[((t * RW + hg) * 16 + tg * NQ + x) * 64 + lane] * wt[t];
       }
-      if (v.live) finish<NQ>(a, w, v, h, r, tg * NQ, hg * 32 + col, m, l, half);
+      if (v.live) finish<NQ>(arguments_again(), w, v, h, r, tg * NQ, hg * 32 + col, m, l, half);
     } else {
       f32x4 r[16];
 #pragma unroll
@@ -907,7 +915,7 @@ struct Grouped {
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           r[4 * n + x] = f32x4{o[n][4 * x], o[n][4 * x + 1], o[n][4 * x + 2], o[n][4 * x + 3]};
-      if (v.live) finish<16>(a, w, v, h, r, 0, hg * 32 + col, m, l, half);
+      if (v.live) finish<16>(arguments_again(), w, v, h, r, 0, hg * 32 + col, m, l, half);
     }
   }
 
@@ -1458,11 +1466,12 @@ struct Latent {
       // in the groups' order, so that both halves of a row have one sum
       l = tg == 0 ? l_run * mine + g.y * other : g.y * other + l_run * mine;
     }
-    const View u = view_of<32 * RG>(a, w, h, rg, col);  // again, rather than kept
+    const ChunkArgs& b = arguments_again();
+    const View u = view_of<32 * RG>(b, w, h, rg, col);  // again, rather than kept
     const float inv = l > 0.f ? 1.f / l : l;
-    const int64_t pr = h * a.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
+    const int64_t pr = h * b.head_part_rows + w.part_row + (w.split * RG + rg) * 32;
     uint16_t* out =
-        a.out + (int64_t)(w.q.begin + u.tok) * a.out_stride + (int64_t)u.head * 512 + 4 * half;
+        b.out + (int64_t)(w.q.begin + u.tok) * b.out_stride + (int64_t)u.head * 512 + 4 * half;
     // token groups: two accumulator tiles at a time, for the branches between them would make each
     // read of the other group's wait for itself
     constexpr int NX = 4 * TG;
@@ -1483,16 +1492,16 @@ struct Latent {
       if (w.splits > 1) {
 #pragma unroll
         for (int x = 0; x < NX; ++x)
-          *reinterpret_cast<f32x4*>(part_quad(a.part_o, pr, 512, first + x, lane)) = r[x];
+          *reinterpret_cast<f32x4*>(part_quad(b.part_o, pr, 512, first + x, lane)) = r[x];
       } else if (u.live) {
 #pragma unroll
         for (int x = 0; x < NX; ++x) store_bf16x4(out + 8 * (first + x), r[x] * inv);
       }
     });
     if (u.live && tg == 0 && half == 0) {
-      if (w.splits > 1) a.part_ml[pr + col] = make_float2(m, l);
-      else if (a.lse)
-        a.lse[(int64_t)(w.q.begin + u.tok) * (a.kv_heads * a.g) + u.head] = natural(m, l);
+      if (w.splits > 1) b.part_ml[pr + col] = make_float2(m, l);
+      else if (b.lse)
+        b.lse[(int64_t)(w.q.begin + u.tok) * (b.kv_heads * b.g) + u.head] = natural(m, l);
     }
   }
 };
