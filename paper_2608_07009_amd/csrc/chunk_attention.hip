@@ -51,8 +51,8 @@ struct ChunkArgs {
   float scale_log2;
 };
 
-// The kernel's arguments once more: what is read from here is loaded then, and not kept in scalar
-// registers through a loop that is short of them.
+// The kernel's arguments (its only parameter) once more: what is read from here is loaded then, and
+// not kept in scalar registers through a loop that is short of them.
 __device__ __forceinline__ const ChunkArgs& arguments_again() {
   auto p = __builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
