@@ -63,9 +63,11 @@ __device__ __forceinline__ const ChunkArgs& arguments_again() {
 
 // Rows (new token, query head of the kv head) of one workgroup, in groups of 32; what waves are left
 // over take other tokens. Grouped-query records: as many groups as the request's rows fill, up to
-// eight. Latent ones: four, or two where the cached tokens are split: a split's partial results are
-// 2 KB a row, written and read again, and a workgroup of half the rows covers twice the tokens (32
-// requests of 128 heads over 2048 8-bit tokens: 59 us with four, of which 28 partial results).
+// eight (four at most: a 2048-token chunk of 16384 1140 us instead of 1043). Latent ones: four, or two
+// where tiles of 64 rows are fewer than the CUs (`split`): a split's partial results are 2 KB a row,
+// written and read again, and a workgroup of half the rows covers twice the tokens (32 requests of 128
+// heads over 2048 8-bit tokens: 59 us with four, 51 with two; 3 requests' 2 tokens of 100, 64 heads: 25
+// and 18.5).
 __device__ __host__ inline int row_groups(int rows, bool latent, bool split) {
   if (latent) return rows <= 64 || split ? 2 : 4;
   return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
@@ -502,12 +504,17 @@ __device__ __forceinline__ void next_weights(uint32_t (&pw)[N][8], f32x16 (&s)[N
 // A workgroup is eight waves, RW row waves of 32 rows each in TG = 8 / RW token groups; a group's
 // waves share tiles of CT tokens (K | V in bf16) in LDS, staged by way of registers: the next
 // tile's loads are in flight while one is computed on, 8-bit rows are widened on their way to LDS
-// (exact: the scale is a power of two), and tokens that nobody may see are stored as zeros.
+// (exact: the scale is a power of two), and tokens that nobody may see are stored as zeros. (16-bit
+// tiles of 256 rows: by direct loads.)
 //   S^T[token][row] = K[token][:] . Q^T[:][row]    v_mfma_f32_32x32x16_bf16, Q in registers
 //   O^T[dim][row]  += V^T[dim][token] P^T[token][row]   the same, V by LDS transpose reads
 // A lane holds one row: 16 of a tile's 32 scores (lane ^ 32 holds the others), which in the token
 // order of mla_row are its P operands, and the row's reference, sum and limits are one register
 // each.
+//
+// Many rows are bound by the issue of MFMAs and of the softmax (6 other vector instructions for each
+// MFMA): 2048 tokens x 64 heads on 4 kv heads over 16384 tokens in 1030 us, 1.00 PFLOP/s. Few rows are
+// bound by HBM: one token of 64 requests x 8 kv heads x 4 over 4096 8-bit tokens in 111 us, 5.0 TB/s.
 
 using GTile = Tile<32>;  // 32 tokens of 32 pieces: K 0..15, V 16..31
 
@@ -969,11 +976,15 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
 // row's reference stays the largest score of the first tile that it sees. If some row's weights
 // outgrow the range (kWeightLimit), the workgroup goes over its tokens twice more: for every row's
 // largest score, then for the result against those.
-// Tiles are stored by direct loads NB - 1 tiles ahead, sent in the shadow of the score MFMAs. 8-bit
+// Tiles are stored by direct loads NB - 1 tiles ahead, sent in the shadow of the MFMAs. 8-bit
 // tiles stay so in LDS (half the traffic) and are widened by the wave that reads an operand, exactly:
 // e4m3 fits bf16. Their scales join where they cost least: the latent part of a score is multiplied
 // by its token's (the rotary part, a chain of MFMAs of its own, is not), and so is the weight that
 // goes with the token's value.
+// Bound by the issue of one wave a SIMD (a vector instruction costs it about 8 cycles, an MFMA 32): 512
+// tokens of 128 heads over 8192 16-bit tokens in 1021 us, 1.11 PFLOP/s; 8-bit 1240, 0.91, for 256
+// widening instructions a tile. One token of 32 requests over 2048 8-bit tokens: 41 us and 9 for the
+// merge, of which start 6, eight rounds of two tiles 26, results 4.5.
 
 using LTile = Tile<72>;  // 16-bit rows
 using PTile = Tile<32>;  // 8-bit latent rows of 512 bytes

@@ -39,6 +39,55 @@ def test_one_long_request_among_many(kind, type_, tpr, at):
 
 
 @pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("splits", [0, 3])
+def test_many_requests_without_starts(kind, type_, tpr, splits):
+    """Lengths only, two new tokens each; split as chosen and as asked for."""
+    lens = [(2, t) for _, t in decoding(279, 40, 5)]
+    lens[200] = (2, 3000)
+    run(kind, type_, tpr, 1, 4, lens, uniform=True, splits=splits)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_captured_batch_whose_lengths_change(kind, type_, tpr):
+    """One graph of a batch for up to 270 requests, replayed with one long request, with none, and with
+    few requests at all: each equals a call of its own."""
+    lens = decoding(269, 40, 6)
+    lens[100:100] = [(1, 2500)]
+    p = Problem(kind, type_, tpr, 1, 4, lens, tail=2)
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        p.run(side)
+    all_start, all_len = p.start.clone(), p.kv_len.clone()
+    for turn in range(4):
+        p.start.copy_(all_start)
+        p.kv_len.copy_(all_len)
+        p.starts, p.lens = all_start.tolist(), list(lens)
+        if turn == 1:  # none is long
+            p.lens[100] = (1, 17)
+        if turn == 2:  # the requests behind the first 102 have no new tokens
+            p.start[102:] = 102
+            p.starts = p.starts[:103]
+            p.lens = p.lens[:102]
+        p.kv_len[100] = p.lens[100][1]
+        short = Problem.__new__(Problem)
+        short.__dict__.update(p.__dict__)
+        if turn == 1:  # the request's first 17 tokens, in whole pages
+            n = (17 + tpr - 1) // tpr * tpr
+            short.k, short.v, short.hole = ([x[:n] if i == 100 else x for i, x in enumerate(y)]
+                                            for y in (p.k, p.v, p.hole))
+        p.out.fill_(MARK)
+        p.lse.fill_(MARK)
+        torch.cuda.synchronize()
+        graph.replay()
+        short.check(f"turn {turn}")
+        out, lse = p.out.clone(), p.lse.clone()
+        p.run()
+        torch.cuda.synchronize()
+        assert torch.equal(out, p.out) and torch.equal(lse, p.lse)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
 def test_long_chunk_among_many(kind, type_, tpr):
     """The same with a chunk of many row tiles, the largest ones, and two heads."""
     lens = decoding(150, 40, 3)
