@@ -672,10 +672,11 @@ size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
  *   d_workspace    at least hisparse_chunk_workspace_bytes bytes, a multiple of 16; calls that may
  *                  overlap (other streams, graphs replayed side by side) need one each.
  * A new token that sees no cached token gives zeros and an lse of -inf. Scores, their maximum and
- * sums are kept in fp32; softmax weights are rounded to bf16 for the product with V. Rows that are
- * not seen (padding, later tokens, tokens before the window, page ends) have no influence, whatever
- * they hold, infinities and NaN included; one that is seen and holds such a value makes results not
- * finite (latent: NaN). Results do not depend on where records lie.
+ * sums are kept in fp32; softmax weights are rounded to bf16 for the product with V. Where scores are
+ * finite in fp32, results are too as long as the number of cached tokens times the largest |v| is below
+ * 2^111. Rows that are not seen (padding, later tokens, tokens before the window, page ends) have no
+ * influence, whatever they hold, infinities and NaN included; one that is seen and holds such a value
+ * makes results not finite (latent: NaN). Results do not depend on where records lie.
  * HISPARSE_ERR_INVALID_ARG for bad descriptors, null or misaligned pointers, or a workspace too
  * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more, or where
  * one launch would need 2^32 threads (512 for each 256 or fewer rows, kv head and split). */

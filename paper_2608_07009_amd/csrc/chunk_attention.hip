@@ -15,10 +15,19 @@ namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
 // Exponentials are taken against a reference per row, the largest score of the first tile that it
-// sees, which moves only when a tile's weights add up to more than this: exact softmax arithmetic
-// with another reference point, and no search for the largest score in the other tiles. (Weights
-// up to 2^64 and their sums over 2^30 tokens stay inside the float range; the score that the
-// reference was taken from weighs 1, so that a row's sum is at least that.)
+// sees, which moves only when weights outgrow it: exact softmax arithmetic with another reference
+// point, and no search for the largest score in the other tiles. (The score that the reference was
+// taken from weighs 1, so that a row's sum is at least that.) What must stay inside the float range is
+// the sums, and the output, which is up to them times the largest value.
+// Grouped-query records: the weights that a lane has of a tile add up to this at most, 2^16, so that
+// values up to 2^111 over the number of tokens seen leave the output finite. (With 2^64 values from 2^64
+// on did not; a smaller limit moves the reference oftener where scores are sharp: the mixed batch of
+// 8-bit pages with queries times 12 takes 242 us with 2^64, 280 with 2^16, 301 with 2^8; with its own
+// queries 242 in all three.)
+constexpr float kTileLimit = 65536.f;
+// Latent ones, for which moving the reference costs two more passes: a row's weights add up to this
+// at most (2^64, far inside the range of sums over 2^30 tokens), and where they add up to more than
+// the number of tokens the output is looked at.
 constexpr float kWeightLimit = 18446744073709551616.f;
 // Up to this reference a weight comes from one fused multiply-add; beyond it the product is rounded
 // first, as the reference was, or a weight could leave the float range.
@@ -493,7 +502,7 @@ __device__ __forceinline__ void next_weights(uint32_t (&pw)[N][8], f32x16 (&s)[N
   bool rare = __ballot(!(__builtin_fabsf(m_run) <= kFused)) != 0;  // -inf: none yet
   if (__builtin_expect(!rare, 1)) {
     sum = weights_of<N>(pw, s, scale, m_run);
-    rare = __ballot(!(sum <= kWeightLimit)) != 0;
+    rare = __ballot(!(sum <= kTileLimit)) != 0;
   }
   if (__builtin_expect(rare, 0)) sum = weights_moved<N, NO>(pw, s, scale, m_run, l_run, o);
   l_run += sum;
@@ -973,9 +982,9 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
 // 32 tokens of 1152 bytes (512 latent and 64 rotary dims in bf16; the value is the latent part).
 // A wave keeps its 32 rows' query (144 registers a lane) and output (256 accumulators; the score
 // MFMAs are assembly so that theirs are not, see mfma_qk). Nothing but MFMAs touches the output: a
-// row's reference stays the largest score of the first tile that it sees. If some row's weights
-// outgrow the range (kWeightLimit), the workgroup goes over its tokens twice more: for every row's
-// largest score, then for the result against those.
+// row's reference stays the largest score of the first tile that it sees. If some row's weights, or
+// their products with its values, outgrow the range (kWeightLimit), the workgroup goes over its tokens
+// twice more: for every row's largest score, then for the result against those.
 // Tiles are stored by direct loads NB - 1 tiles ahead, sent in the shadow of the MFMAs. 8-bit
 // tiles stay so in LDS (half the traffic) and are widened by the wave that reads an operand, exactly:
 // e4m3 fits bf16. Their scales join where they cost least: the latent part of a score is multiplied
@@ -1320,6 +1329,19 @@ struct Latent {
     // of group 1's, so that at the end each group finishes its tiles 0..7 and leaves the other group
     // tiles 8..15 with the same code (registers cannot be chosen at run time).
     f32x16 o[16];
+    // They are read one by one (arithmetic on them would move all of them to vector registers); the
+    // wait states after the last MFMA are given here.
+    auto accumulated = []() { asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory"); };
+    auto quad = [&](int n, int x) {
+      f32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y;
+        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(o[n][4 * x + i]));
+        r[i] = y;
+      }
+      return r;
+    };
     float m_run = -INFINITY, l_run = 0.f;
     begin_tiles(EARLY, AHEAD);
     for (int attempt = 0;; ++attempt) {
@@ -1423,8 +1445,19 @@ struct Latent {
         }
       }
       // some row's weights outgrew its reference? (A sum that is NaN is no reason: it stays so.)
-      if (attempt == 0 && __ballot(l_run > kWeightLimit) && (threadIdx.x & 63) == 0)
-        *s_outgrown = 1;
+      if (attempt == 0 && __ballot(l_run > (float)(v.t1 - v.t0))) {  // some weigh more than 1: 1 us
+        float x = 0.f;
+        accumulated();
+#pragma unroll
+        for (int n = 0; n < 16; ++n)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const f32x4 r = quad(n, y);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x = __builtin_fmaf(r[i], 0.f, x);  // NaN if not finite
+          }
+        if (__ballot(x != 0.f || l_run > kWeightLimit) && (threadIdx.x & 63) == 0) *s_outgrown = 1;
+      }
       lds_barrier();  // every wave is past its tiles
       if (attempt == 1 || __builtin_amdgcn_readfirstlane(*s_outgrown) == 0) break;
       auto again = [&]() {
@@ -1446,19 +1479,8 @@ struct Latent {
     }
     l_run += __shfl_xor(l_run, 32, 64);
 
-    // ---- results: the accumulators are read one by one (arithmetic on them would move all of them
-    // to vector registers); the wait states after the last MFMA are given here ----
-    asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 7" ::: "memory");
-    auto quad = [&](int n, int x) {
-      f32x4 r;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float y;
-        asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(y) : "a"(o[n][4 * x + i]));
-        r[i] = y;
-      }
-      return r;
-    };
+    // ---- results ----
+    accumulated();
     const int lane = lane_now(), half = lane >> 5, col = lane & 31;
     float m = m_run, l = l_run, mine = 1.f, other = 0.f;
     f32x4* s_o = reinterpret_cast<f32x4*>(s_mem);  // [wave][8 tiles][4 quads][64 lanes]
