@@ -641,8 +641,10 @@ typedef struct {
 hisparse_status_t hisparse_validate_chunk(const hisparse_kv_desc_t* kv,
                                           const hisparse_chunk_desc_t* chunk);
 
-/* [pure host] Bytes of device scratch the call needs (0: none, d_workspace may be NULL); 0 too for
- * invalid descriptors. */
+/* [pure host] Bytes of device scratch for the call (0: none, d_workspace may be NULL); 0 too for
+ * invalid descriptors. A workspace of this size serves every call of at most as many requests, total
+ * tokens, new tokens per request and records with the same kv, heads, window and num_splits: a server
+ * that sizes one for its largest batch needs no other. */
 size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
                                       const hisparse_chunk_desc_t* chunk);
 

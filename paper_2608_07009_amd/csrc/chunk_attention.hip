@@ -1639,7 +1639,8 @@ struct ChunkPlan {
   int32_t d_v, target, uni_tiles, uni_splits, max_splits;
   int32_t groups;        // of 32 rows of the largest row tile
   bool split;            // row tiles are split as a rule, not only those of long requests
-  size_t workspace_bytes;
+  size_t workspace_bytes;  // of this call
+  size_t serves_bytes;     // of this call and every smaller batch's
 };
 
 // Workgroups that splitting aims at: one per CU, which is what LDS holds. (512: 24% more time for 8
@@ -1656,7 +1657,8 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   const int64_t span =
       c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
   const int64_t blocks = (span + 63) / 64 + 1;  // a first token inside a block adds one
-  int64_t bm = 0, parts = 0;  // rows of a tile; items with partial results
+  int64_t bm = 0;     // rows of a tile
+  int64_t parts = 0;  // items of a kv head with partial results
   auto count_tiles = [&](bool split) {
     bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent, split);
     p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
@@ -1665,6 +1667,20 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / most + c.num_requests,
                                 (int64_t)c.num_requests * p.uni_tiles);
   };
+  auto bytes_of = [&](int64_t part_rows) {
+    return part_rows == 0 ? 0 : (size_t)part_rows * (p.d_v * sizeof(float) + sizeof(float2)) +
+                                    sizeof(int32_t);
+  };
+  // Splits of fewer row tiles than CUs: the most of one tile, and of `tiles` of them together (what
+  // part_of allows for).
+  const int64_t least = (span + min_split(latent) - 1) / min_split(latent);
+  const int64_t few_splits = std::min<int64_t>(least, kMaxSplits);
+  auto few_items = [&](int64_t tiles) {
+    const int64_t t = kTargetWorkgroups;
+    return std::min(tiles * few_splits,
+                    std::max<int64_t>(t / c.kv_heads, tiles + t / 2 / c.kv_heads) + 2);
+  };
+  size_t smaller = 0;  // what the largest batch of fewer row tiles than CUs needs
   p.max_splits = 1;
   p.uni_splits = 1;
   count_tiles(true);
@@ -1680,21 +1696,18 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     // requests of 128 heads over 2048 16-bit tokens 150 us, 202 with 64; 240 8-bit ones 190, 208)
     p.split = true;
     p.items = p.tiles;
-    if (span > min_split(latent)) {
+    if (least > 1) {
       p.target = kTargetWorkgroups;
-      const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
-      p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
-      // requests alike: as many splits as all start at once
-      const int64_t alike = (int64_t)c.num_requests * p.uni_tiles;
+      p.max_splits = (int32_t)few_splits;
+      // requests alike (p.tiles is then exact): as many splits as all start at once
       p.uni_splits = (int32_t)std::min<int64_t>(
-          p.max_splits, std::max<int64_t>(1, p.target / (alike * c.kv_heads)));
-      p.items = std::min(p.tiles * p.max_splits,
-                         std::max<int64_t>(p.target / c.kv_heads,
-                                           p.tiles + p.target / 2 / c.kv_heads) + 2);
-      p.items = std::max(p.items, alike * p.uni_splits);
+          p.max_splits, std::max<int64_t>(1, p.target / (p.tiles * c.kv_heads)));
+      p.items = few_items(p.tiles);
       parts = p.items;
     }
   } else {
+    const int64_t fewer = (kTargetWorkgroups - 1) / c.kv_heads;
+    if (least > 1 && fewer > 0) smaller = bytes_of(few_items(fewer) * bm * c.kv_heads);
     // Parts of W / (2 target): at most 2 target more items than row tiles, and a tile that is split
     // is longer than one, so that it has at most twice as many as it is long. One request of 65536
     // 8-bit tokens among 63 of 1000, 8 kv heads x 4: 578 us without, 84 with; latent, 16 heads, among
@@ -1704,10 +1717,9 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
     count_tiles(false);
     p.items = p.tiles;
     const int64_t more = 2 * kTargetWorkgroups / c.kv_heads;
-    const int64_t most = (span + min_split(latent) - 1) / min_split(latent);
-    if (most >= 4 && more > 0) {
+    if (least >= 4 && more > 0) {
       p.target = kTargetWorkgroups;
-      p.max_splits = (int32_t)std::min<int64_t>(most, kMaxSplits);
+      p.max_splits = (int32_t)few_splits;
       p.items = std::min(p.tiles * p.max_splits, p.tiles + more);
       parts = std::min(p.items, 2 * more + 1);
     }
@@ -1715,9 +1727,9 @@ ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& 
   if (p.max_splits > 1) {
     p.groups = (int32_t)(bm / 32);
     p.part_rows = parts * bm * c.kv_heads;
-    p.workspace_bytes =
-        (size_t)p.part_rows * (p.d_v * sizeof(float) + sizeof(float2)) + sizeof(int32_t);
   }
+  p.workspace_bytes = bytes_of(p.part_rows);
+  p.serves_bytes = std::max(p.workspace_bytes, smaller);
   return p;
 }
 
@@ -1756,7 +1768,7 @@ hisparse_status_t hisparse_validate_chunk(const hisparse_kv_desc_t* kv,
 size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
                                       const hisparse_chunk_desc_t* c) {
   if (hisparse_validate_chunk(kv, c) != HISPARSE_OK) return 0;
-  return hisparse::plan_chunk(*kv, *c).workspace_bytes;
+  return hisparse::plan_chunk(*kv, *c).serves_bytes;
 }
 
 hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,

@@ -1,0 +1,55 @@
+"""hisparse_chunk_attention's ways of dividing a call. Compared as in test_gpu_chunk_attention."""
+import pytest
+import torch
+
+import token_reference as ref
+from paper_2608_07009_amd import hisparse as hs
+from test_gpu_chunk_attention import MARK, TYPES, Problem
+
+pytestmark = pytest.mark.gpu
+
+
+def shared(kind, type_, tpr, kv_heads, q_heads, lens, T, tail=0, splits=0, uniform=False,
+           max_chunk=0, seed=3):
+    """A Problem whose requests all have one table of T tokens (a stride of 0 between theirs), of which
+    each sees its first ones. uniform: no starts and no lengths."""
+    p = Problem(kind, type_, tpr, kv_heads, q_heads, [(1, T)], splits=splits, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    R, H = len(lens), p.H
+    p.lens, p.uniform = list(lens), uniform
+    p.k, p.v, p.hole = p.k * R, p.v * R, p.hole * R
+    p.starts = [0]
+    for n, _ in lens:
+        p.starts.append(p.starts[-1] + n)
+    p.total = p.starts[-1] + tail
+    p.q = torch.randn((p.total, H, ref.D_QK[kind]), generator=g).to(torch.bfloat16)
+    p.qd = p.q.flatten(1).cuda()
+    p.start = None if uniform else torch.tensor(p.starts, dtype=torch.int32, device="cuda")
+    p.kv_len = None if uniform else torch.tensor([t for _, t in lens], dtype=torch.int32,
+                                                 device="cuda")
+    c = p.chunk
+    c.num_requests, c.total_tokens, c.table_request_stride = R, p.total, 0
+    c.max_chunk = max_chunk or max(n for n, _ in lens)
+    p.out = torch.full((p.total, H * ref.D_V[kind]), MARK, dtype=torch.bfloat16, device="cuda")
+    p.lse = torch.full((p.total, H), MARK, dtype=torch.float32, device="cuda")
+    p.ws_bytes = hs.hisparse_chunk_workspace_bytes(p.kv, c)
+    p.ws = torch.full((p.ws_bytes + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+    p.run()
+    p.check()
+    return p
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_one_workspace_for_the_largest_batch(kind, type_, tpr):
+    """Sized for 66 requests of 4 kv heads, which fill the CUs and are not split, it serves fewer, which
+    are."""
+    big = shared(kind, type_, tpr, 4, 4, [(1, 384)] * 66, 384)
+    assert big.ws_bytes > 0
+    for n in (63, 20, 1):
+        p = shared(kind, type_, tpr, 4, 4, [(1, 384)] * n, 384)
+        assert 0 < p.ws_bytes <= big.ws_bytes
+        p.ws, p.ws_bytes = big.ws, big.ws_bytes
+        p.out.fill_(MARK)
+        p.lse.fill_(MARK)
+        p.run()
+        p.check(f"{n} requests")
