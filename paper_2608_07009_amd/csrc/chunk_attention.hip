@@ -7,6 +7,7 @@
 #include <algorithm>
 
 #include "attention_device.h"
+#include "chunk_plan.h"
 #include "fetch_device.h"
 #include "tokens.h"
 
@@ -32,14 +33,10 @@ constexpr float kWeightLimit = 18446744073709551616.f;
 // Up to this reference a weight comes from one fused multiply-add; beyond it the product is rounded
 // first, as the reference was, or a weight could leave the float range.
 constexpr float kFused = 16777216.f;
-constexpr int kMaxSplits = 128;  // parts of one request's cached tokens
-// The least tokens of a split: a workgroup's two rounds of two tiles (latent records), its eight
-// tiles (grouped-query ones).
-__device__ __host__ constexpr int min_split(bool latent) { return latent ? 128 : 256; }
 
-struct ChunkArgs {
+struct ChunkArgs : ChunkShape {
   const uint8_t* pool;
-  const int32_t *table, *start, *kv_len;
+  const int32_t* table;
   const uint16_t* q;
   uint16_t* out;
   float* lse;
@@ -47,15 +44,11 @@ struct ChunkArgs {
   float2* part_ml;  // [part rows] (reference in log2 units, sum)
   int64_t record_stride, head_stride, request_stride;
   int64_t q_stride, out_stride, table_request_stride, table_head_stride;
-  int64_t num_records, head_part_rows;
+  int64_t num_records;
   KvLayout l;
-  int32_t requests, kv_heads, g, total, max_chunk, max_tokens, window, causal;
-  int32_t split;                // row tiles are split as a rule, not only those of long requests
-  int32_t target;               // workgroups that splitting aims at (0: none)
+  int32_t causal;
   int32_t* n_split;             // where few row tiles are split: how many of a kv head, left for the
                                 // merge by the last workgroup; or NULL
-  int32_t num_splits;           // asked for (0: chosen)
-  int32_t uni_tiles, uni_splits;  // of every request, where they are alike (start and kv_len null)
   FastDiv div_g;
   float scale_log2;
 };
@@ -70,34 +63,6 @@ __device__ __forceinline__ const ChunkArgs& arguments_again() {
 
 // ---- which piece of the call a workgroup does ------------------------------------------------
 
-// Rows (new token, query head of the kv head) of one workgroup, in groups of 32; what waves are left
-// over take other tokens. Grouped-query records: as many groups as the request's rows fill, up to
-// eight (four at most: a 2048-token chunk of 16384 1140 us instead of 1043). Latent ones: four, or two
-// where tiles of 64 rows are fewer than the CUs (`split`): a split's partial results are 2 KB a row,
-// written and read again, and a workgroup of half the rows covers twice the tokens (32 requests of 128
-// heads over 2048 8-bit tokens: 59 us with four, 51 with two; 3 requests' 2 tokens of 100, 64 heads: 25
-// and 18.5).
-__device__ __host__ inline int row_groups(int rows, bool latent, bool split) {
-  if (latent) return rows <= 64 || split ? 2 : 4;
-  return rows <= 32 ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
-}
-
-struct Request {
-  int begin, n, len;
-};
-__device__ __forceinline__ Request request_of(const ChunkArgs& a, int r) {
-  Request q;
-  if (a.start) {
-    q.begin = min(max(a.start[r], 0), a.total);
-    q.n = min(min(max(a.start[r + 1], q.begin), a.total) - q.begin, a.max_chunk);
-  } else {
-    q.begin = r * a.max_chunk;
-    q.n = a.max_chunk;
-  }
-  q.len = a.kv_len ? min(max(a.kv_len[r], 0), a.max_tokens) : a.max_tokens;
-  return q;
-}
-
 struct Work {
   Request q;
   int req, groups, tile, split, splits;
@@ -109,15 +74,12 @@ template <int CTRL, int ROWS = 0xf>
 __device__ __forceinline__ int moved(int x) {  // 0 where nothing comes from
   return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
 }
-__device__ __forceinline__ float wave_sum(float x) {
-  auto add = [&](int y) { x += __int_as_float(y); };
-  add(moved<0x128>(__float_as_int(x)));  // 16 lanes: rotations by 8, 4, 2, 1
-  add(moved<0x124>(__float_as_int(x)));
-  add(moved<0x122>(__float_as_int(x)));
-  add(moved<0x121>(__float_as_int(x)));
-  auto of = [&](int lane) {
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
-  };
+__device__ __forceinline__ uint32_t wave_sum(uint32_t x) {
+  x += moved<0x128>(x);  // 16 lanes: rotations by 8, 4, 2, 1
+  x += moved<0x124>(x);
+  x += moved<0x122>(x);
+  x += moved<0x121>(x);
+  auto of = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); };
   return (of(0) + of(16)) + (of(32) + of(48));
 }
 __device__ __forceinline__ int wave_prefix(int x) {  // inclusive
@@ -129,68 +91,39 @@ __device__ __forceinline__ int wave_prefix(int x) {  // inclusive
   return x + moved<0x143, 0xc>(x);  // lane 31 to the upper half
 }
 
-// Row tiles of a request, of `groups` groups of 32 rows.
-template <bool LATENT>
-__device__ __forceinline__ int tiles_of(const ChunkArgs& a, const Request& q, int& groups) {
-  const int rows = q.n * a.g;
-  groups = row_groups(rows, LATENT, a.split);
-  return (rows + 32 * groups - 1) / (32 * groups);
-}
-__device__ __forceinline__ int span_of(const ChunkArgs& a, const Request& q) {
-  return a.window ? min(q.len, a.window + q.n - 1) : q.len;
-}
-__device__ __forceinline__ int splits_of(const ChunkArgs& a, const Request& q, int part) {
-  const int span = span_of(a, q);
-  if (a.num_splits) return min(a.num_splits, max(1, (span + 63) >> 6));
-  return a.target ? min(max((span + part - 1) / part, 1), kMaxSplits) : 1;
-}
-// Splits follow from the requests' lengths alone. With fewer row tiles than `target`, cached tokens
-// lie in parts of W / target, W the tokens of all row tiles, if those are at most `target` parts (a
-// tile's last may be short), so that all start at once; else of 4/3 of that, or of W / (target - row
-// tiles) if that is less: with those they always are. (16 requests of 4096 8-bit tokens, 8 kv heads x 4,
-// 128 row tiles: 40 us in two parts each, 52 in one.) With more row tiles, in parts of W / (2 target),
-// which only the tiles of long requests are split into, so that the last of them ends not long after
-// the others.
+// The length of parts (see choose_part). Wave-uniform.
 template <bool LATENT>
 __device__ __forceinline__ int part_of(const ChunkArgs& a, const Request& first) {
   if (!a.target || a.num_splits) return 0;
   const int lane = threadIdx.x & 63;
-  float sum = 0.f, tiles = 0.f;  // (a rounding of them moves the parts, nothing else)
+  uint64_t blocks = 0;
+  uint32_t tiles = 0;
   for (int base = 0; base < a.requests; base += 64) {
     const int r = base + lane;
-    float x = 0.f, t = 0.f;
+    uint64_t x = 0;
+    int groups, t = 0;
     if (r < a.requests) {
       const Request q = base == 0 ? first : request_of(a, r);
-      int groups;
-      t = (float)tiles_of<LATENT>(a, q, groups);
-      x = t * (float)((span_of(a, q) + 63) >> 6);
+      t = tiles_of(a, LATENT, q, groups);
+      x = blocks_of(a, q, t);  // below 2^50
     }
-    sum += wave_sum(x);
-    tiles += wave_sum(t);
+    blocks += wave_sum((uint32_t)x & 0xffffff);
+    if (__ballot(x >> 24)) blocks += (uint64_t)wave_sum((uint32_t)(x >> 24)) << 24;
+    tiles += wave_sum((uint32_t)t);
   }
-  const float heads = (float)a.kv_heads, target = (float)a.target;
-  // (a little more: sums of many requests round, and the host allows for so many items only)
-  auto part = [&](float parts) {
-    const float p = sum * heads * (64.1f / parts) + 1.f;
-    return (int)fminf(fmaxf(p, (float)min_split(LATENT)), 1073741824.f);
-  };
-  if (tiles * heads >= target) return part(2.f * target);
-  const float sure = fmaxf(target - tiles * heads, 0.5f * target);
-  for (float parts = target; parts > sure; parts -= 0.25f * target) {
-    const int p = part(parts);
-    float items = 0.f;
+  return choose_part(blocks, (int)tiles, a.kv_heads, LATENT, [&](int part) {
+    uint32_t items = 0;
     for (int base = 0; base < a.requests; base += 64) {
       const int r = base + lane;
       int groups, n = 0;
       if (r < a.requests) {
         const Request q = base == 0 ? first : request_of(a, r);
-        n = tiles_of<LATENT>(a, q, groups) * splits_of(a, q, p);
+        n = tiles_of(a, LATENT, q, groups) * splits_of(a, q, part);
       }
-      items += wave_sum((float)n);
+      items += wave_sum((uint32_t)n);
     }
-    if (items * heads <= target) return p;
-  }
-  return part(sure);
+    return items;
+  });
 }
 __device__ __forceinline__ Request first_request(const ChunkArgs& a) {
   const int lane = threadIdx.x & 63;
@@ -209,7 +142,7 @@ __device__ __forceinline__ int split_tiles(const ChunkArgs& a) {
     int groups, tiles = 0;
     if (r < a.requests) {
       const Request q = base == 0 ? first : request_of(a, r);
-      if (splits_of(a, q, part) > 1) tiles = tiles_of<LATENT>(a, q, groups);
+      if (splits_of(a, q, part) > 1) tiles = tiles_of(a, LATENT, q, groups);
     }
     n += __builtin_amdgcn_readlane(wave_prefix(tiles), 63);
   }
@@ -255,7 +188,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
     int groups = 1, tiles = 0, splits = 1;
     if (r < a.requests) {
       q = base == 0 ? first : request_of(a, r);
-      tiles = tiles_of<LATENT>(a, q, groups);
+      tiles = tiles_of(a, LATENT, q, groups);
       splits = splits_of(a, q, part);
     }
     const int mine = !MERGE ? tiles * splits : splits > 1 ? tiles : 0;
@@ -1631,108 +1564,6 @@ __global__ __launch_bounds__(256 * SG) void chunk_merge_kernel(ChunkArgs a) {
   }
 }
 
-// ---- host: the call's plan ----------------------------------------------------------------
-
-struct ChunkPlan {
-  int64_t tiles, items;  // at most so many row tiles, (tile, split)s of a kv head
-  int64_t part_rows;     // rows of partial results, all kv heads
-  int32_t d_v, target, uni_tiles, uni_splits, max_splits;
-  int32_t groups;        // of 32 rows of the largest row tile
-  bool split;            // row tiles are split as a rule, not only those of long requests
-  size_t workspace_bytes;  // of this call
-  size_t serves_bytes;     // of this call and every smaller batch's
-};
-
-// Workgroups that splitting aims at: one per CU, which is what LDS holds. (512: 24% more time for 8
-// requests of 8 kv heads x 4 over 4096 8-bit tokens, 30% for one over 32768 16-bit ones.)
-constexpr int kTargetWorkgroups = 256;
-
-ChunkPlan plan_chunk(const hisparse_kv_desc_t& kv, const hisparse_chunk_desc_t& c) {
-  ChunkPlan p{};
-  p.d_v = kv.layout == HISPARSE_KV_GROUPED ? 128 : 512;
-  const bool latent = kv.layout == HISPARSE_KV_LATENT;
-  const int64_t chunk = std::min<int64_t>(c.max_chunk, std::max(c.total_tokens, 1));
-  const int64_t max_rows = chunk * c.q_heads;
-  const int64_t tokens = (int64_t)c.max_records * kv.tokens_per_record;
-  const int64_t span =
-      c.window ? std::min<int64_t>(tokens, c.window + chunk - 1) : tokens;
-  const int64_t blocks = (span + 63) / 64 + 1;  // a first token inside a block adds one
-  int64_t bm = 0;     // rows of a tile
-  int64_t parts = 0;  // items of a kv head with partial results
-  auto count_tiles = [&](bool split) {
-    bm = 32 * row_groups((int)std::min<int64_t>(max_rows, 1 << 20), latent, split);
-    p.uni_tiles = (int32_t)((max_rows + bm - 1) / bm);
-    // every request has a last row tile that may not be full; the others are of the most rows
-    const int64_t most = latent ? bm : 256;
-    p.tiles = std::min<int64_t>((int64_t)c.total_tokens * c.q_heads / most + c.num_requests,
-                                (int64_t)c.num_requests * p.uni_tiles);
-  };
-  auto bytes_of = [&](int64_t part_rows) {
-    return part_rows == 0 ? 0 : (size_t)part_rows * (p.d_v * sizeof(float) + sizeof(float2)) +
-                                    sizeof(int32_t);
-  };
-  // Splits of fewer row tiles than CUs: the most of one tile, and of `tiles` of them together (what
-  // part_of allows for).
-  const int64_t least = (span + min_split(latent) - 1) / min_split(latent);
-  const int64_t few_splits = std::min<int64_t>(least, kMaxSplits);
-  auto few_items = [&](int64_t tiles) {
-    const int64_t t = kTargetWorkgroups;
-    return std::min(tiles * few_splits,
-                    std::max<int64_t>(t / c.kv_heads, tiles + t / 2 / c.kv_heads) + 2);
-  };
-  size_t smaller = 0;  // what the largest batch of fewer row tiles than CUs needs
-  p.max_splits = 1;
-  p.uni_splits = 1;
-  count_tiles(true);
-  if (c.num_splits > 0) {
-    p.max_splits = (int32_t)std::min<int64_t>(c.num_splits, blocks);
-    p.uni_splits = p.max_splits;
-    p.split = p.max_splits > 1;
-    count_tiles(p.split);
-    p.items = p.tiles * p.max_splits;
-    parts = p.items;
-  } else if (p.tiles * c.kv_heads < kTargetWorkgroups) {
-    // (latent: tiles of 64 rows; as soon as those would be more than the CUs, tiles of 128 rows: 190
-    // requests of 128 heads over 2048 16-bit tokens 150 us, 202 with 64; 240 8-bit ones 190, 208)
-    p.split = true;
-    p.items = p.tiles;
-    if (least > 1) {
-      p.target = kTargetWorkgroups;
-      p.max_splits = (int32_t)few_splits;
-      // requests alike (p.tiles is then exact): as many splits as all start at once
-      p.uni_splits = (int32_t)std::min<int64_t>(
-          p.max_splits, std::max<int64_t>(1, p.target / (p.tiles * c.kv_heads)));
-      p.items = few_items(p.tiles);
-      parts = p.items;
-    }
-  } else {
-    const int64_t fewer = (kTargetWorkgroups - 1) / c.kv_heads;
-    if (least > 1 && fewer > 0) smaller = bytes_of(few_items(fewer) * bm * c.kv_heads);
-    // Parts of W / (2 target): at most 2 target more items than row tiles, and a tile that is split
-    // is longer than one, so that it has at most twice as many as it is long. One request of 65536
-    // 8-bit tokens among 63 of 1000, 8 kv heads x 4: 578 us without, 84 with; latent, 16 heads, among
-    // 299: 2480 and 146. 64 requests of 4096 tokens, which are not split: 109 and 113 for working
-    // that out. Where no request can have four parts of the least length that is not tried (64 of
-    // 512: 25 us, 33).
-    count_tiles(false);
-    p.items = p.tiles;
-    const int64_t more = 2 * kTargetWorkgroups / c.kv_heads;
-    if (least >= 4 && more > 0) {
-      p.target = kTargetWorkgroups;
-      p.max_splits = (int32_t)few_splits;
-      p.items = std::min(p.tiles * p.max_splits, p.tiles + more);
-      parts = std::min(p.items, 2 * more + 1);
-    }
-  }
-  if (p.max_splits > 1) {
-    p.groups = (int32_t)(bm / 32);
-    p.part_rows = parts * bm * c.kv_heads;
-  }
-  p.workspace_bytes = bytes_of(p.part_rows);
-  p.serves_bytes = std::max(p.workspace_bytes, smaller);
-  return p;
-}
-
 }  // namespace
 }  // namespace hisparse
 
@@ -1792,11 +1623,9 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   if (p.workspace_bytes > 0 && (!d_workspace || (uintptr_t)d_workspace % 16 != 0 ||
                                 workspace_bytes < p.workspace_bytes))
     return HISPARSE_ERR_INVALID_ARG;
-  ChunkArgs a{};
+  ChunkArgs a{chunk_shape(*kv, *c, p, d_chunk_start, d_kv_len)};
   a.pool = reinterpret_cast<const uint8_t*>(d_pool);
   a.table = d_table;
-  a.start = d_chunk_start;
-  a.kv_len = d_kv_len;
   a.q = reinterpret_cast<const uint16_t*>(d_q);
   a.out = reinterpret_cast<uint16_t*>(d_out);
   a.lse = d_lse;
@@ -1810,25 +1639,12 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
   a.table_request_stride = c->table_request_stride;
   a.table_head_stride = c->table_head_stride;
   a.num_records = kv->num_records;
-  a.head_part_rows = p.part_rows / c->kv_heads;
   a.l = kv_layout(*kv);
-  a.requests = c->num_requests;
-  a.kv_heads = c->kv_heads;
-  a.g = c->q_heads;
-  a.total = c->total_tokens;
-  a.max_chunk = std::min(c->max_chunk, c->total_tokens);
-  a.max_tokens = c->max_records << a.l.tpr_shift;
-  a.window = c->window < a.max_tokens ? c->window : 0;  // (its sums stay in 32 bits)
   a.causal = (c->flags & HISPARSE_CHUNK_CAUSAL) != 0;
-  a.split = p.split;
-  a.target = p.target;
   const bool ragged = d_chunk_start || d_kv_len;
   const bool merges = p.max_splits > 1 && (ragged || p.uni_splits > 1);
   if (merges && p.target && !p.split)
     a.n_split = reinterpret_cast<int32_t*>(a.part_ml + p.part_rows);
-  a.num_splits = c->num_splits;
-  a.uni_tiles = p.uni_tiles;
-  a.uni_splits = p.uni_splits;
   a.div_g = make_fastdiv((uint32_t)c->q_heads);
   a.scale_log2 = c->scale * 1.4426950408889634f;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);

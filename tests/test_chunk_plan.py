@@ -1,5 +1,8 @@
 """The host's plan of hisparse_chunk_attention, without a GPU."""
+import os
 import random
+import shutil
+import subprocess
 
 import pytest
 
@@ -7,6 +10,7 @@ import token_reference as ref
 from paper_2608_07009_amd import hisparse as hs
 
 G, L = ref.GROUPED, ref.LATENT
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 def workspace(kind, tpr, kv_heads, q_heads, requests, total, chunk, records, window=0, splits=0):
@@ -45,3 +49,28 @@ def test_a_workspace_serves_every_smaller_batch(kind, splits):
             continue
         b = workspace(kind, tpr, kv_heads, q_heads, *small, window, splits)
         assert b is not None and b <= a, (kv_heads, q_heads, tpr, window, (requests, total, chunk, records), small)
+
+
+def check_plans(tmp_path, name, *flags):
+    exe = str(tmp_path / name)
+    subprocess.check_call(["g++", "-std=c++17", "-O2", *flags, "-I", os.path.join(ROOT, "include"),
+                           "-I", os.path.join(ROOT, "paper_2608_07009_amd", "csrc"),
+                           os.path.join(ROOT, "tests", "chunk_plan_check.cc"), "-o", exe])
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.startswith("ok"), r.stdout + r.stderr[-3000:]
+    return r.stdout
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+def test_what_the_device_finds_fits_the_host_s_bounds(tmp_path):
+    """Random batches, with the arithmetic checked for overflow."""
+    out = check_plans(tmp_path, "plain", "-fsanitize=undefined", "-fno-sanitize-recover=all")
+    assert int(out.split()[1]) > 10000
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs g++")
+@pytest.mark.skipif("fma" not in open("/proc/cpuinfo").read(), reason="needs a CPU with FMA")
+def test_parts_do_not_depend_on_how_the_compiler_contracts(tmp_path):
+    """The attention and the merge are compiled apart and each works out the parts."""
+    assert (check_plans(tmp_path, "off", "-mfma", "-ffp-contract=off")
+            == check_plans(tmp_path, "fast", "-mfma", "-ffp-contract=fast", "-O3"))
