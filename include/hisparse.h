@@ -660,7 +660,8 @@ size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
  *   d_chunk_start  int32 [num_requests + 1], ascending: request q's new tokens are rows start[q] ..
  *                  start[q + 1] - 1 of d_q and d_out. Rows outside every chunk (a batch padded to
  *                  a fixed size) are neither read nor written. Values are held to [0,
- *                  total_tokens]. NULL: every request has max_chunk new tokens, request q's from
+ *                  total_tokens]; where they do not ascend, what the rows of d_out and d_lse hold
+ *                  afterwards is unspecified. NULL: every request has max_chunk new tokens, request q's from
  *                  row q * max_chunk; total_tokens >= num_requests * max_chunk.
  *   d_kv_len       int32 [num_requests]: cached tokens of each request, its new ones included; held
  *                  to [0, max_records * tokens_per_record]. NULL: that many everywhere. A request

@@ -180,7 +180,7 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
   }
   const Request first = first_request(a);  // loaded once for both passes
   const int part = part_of<LATENT>(a, first);
-  int items = 0;
+  uint32_t items = 0;
   int64_t rows = 0;
   for (int base = 0; base < a.requests; base += 64) {
     const int r = base + lane;
@@ -191,10 +191,11 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
       tiles = tiles_of(a, LATENT, q, groups);
       splits = splits_of(a, q, part);
     }
-    const int mine = !MERGE ? tiles * splits : splits > 1 ? tiles : 0;
-    const int mine_rows = splits > 1 ? tiles * splits * groups : 0;
-    const int pi = wave_prefix(mine), pr = wave_prefix(mine_rows);
-    const uint64_t hit = __ballot(items + pi > item);
+    const uint32_t pieces = items_of(tiles, splits);
+    const uint32_t mine = !MERGE ? pieces : splits > 1 ? (uint32_t)tiles : 0;
+    const uint32_t mine_rows = splits > 1 ? pieces * (uint32_t)groups : 0;
+    const uint32_t pi = wave_prefix((int)mine), pr = wave_prefix((int)mine_rows);
+    const uint64_t hit = __ballot(items + pi > (uint32_t)item);
     if (hit) {
       const int src = __builtin_ctzll(hit);
       auto get = [&](int x) { return __builtin_amdgcn_readlane(x, src); };
@@ -202,15 +203,16 @@ __device__ __forceinline__ bool find_work(const ChunkArgs& a, int item, Work& w)
       w.q = Request{get(q.begin), get(q.n), get(q.len)};
       w.groups = get(groups);
       w.splits = get(splits);
-      const int x = item - items - get(pi - mine);
+      const int x = item - (int)(items + (uint32_t)get((int)(pi - mine)));
       w.tile = MERGE ? x : x / w.splits;
       w.split = MERGE ? 0 : x - w.tile * w.splits;
-      w.part_row = (rows + get(pr - mine_rows) + (int64_t)w.tile * w.splits * w.groups) * 32;
+      w.part_row = (rows + (uint32_t)get((int)(pr - mine_rows)) +
+                    (int64_t)w.tile * w.splits * w.groups) * 32;
       w.tile = get(tiles) - 1 - w.tile;
-      return true;
+      return partial_rows_fit(a, w.part_row, w.splits, w.groups);
     }
-    items += __builtin_amdgcn_readlane(pi, 63);
-    rows += __builtin_amdgcn_readlane(pr, 63);
+    items += (uint32_t)__builtin_amdgcn_readlane((int)pi, 63);
+    rows += (uint32_t)__builtin_amdgcn_readlane((int)pr, 63);
   }
   return false;
 }

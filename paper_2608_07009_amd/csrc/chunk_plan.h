@@ -72,7 +72,7 @@ HISPARSE_BOTH Request request_of(const ChunkShape& a, int r) {
 HISPARSE_BOTH int tiles_of(const ChunkShape& a, bool latent, const Request& q, int& groups) {
   const int rows = q.n * a.g;
   groups = row_groups(rows, latent, a.split);
-  return (rows + 32 * groups - 1) / (32 * groups);
+  return (int)(((uint32_t)rows + 32 * groups - 1) / (32 * groups));
 }
 HISPARSE_BOTH int span_of(const ChunkShape& a, const Request& q) {
   return a.window ? least_of(q.len, a.window + q.n - 1) : q.len;
@@ -85,6 +85,19 @@ HISPARSE_BOTH int splits_of(const ChunkShape& a, const Request& q, int part) {
 // 64-token blocks that a request's row tiles read.
 HISPARSE_BOTH uint64_t blocks_of(const ChunkShape& a, const Request& q, int tiles) {
   return (uint64_t)(uint32_t)tiles * (uint32_t)((span_of(a, q) + 63) >> 6);
+}
+
+// A request's (row tile, split)s. A call has fewer than 2^23, but starts that descend give requests more
+// rows between them than there are, so that each is held to it: sums over 64 requests then stay in 32
+// bits, in groups of 32 rows too, and what does not fit the workspace is seen in partial_rows_fit.
+HISPARSE_BOTH uint32_t items_of(int tiles, int splits) {
+  constexpr uint32_t most = (1u << 23) - 1;
+  return least_of(least_of((uint32_t)tiles, most) * (uint32_t)splits, most);
+}
+// Whether the partial results of a row tile, from row `first` on, lie in the workspace. Always, if
+// starts ascend; else such a tile is left out by the attention and the merge.
+HISPARSE_BOTH bool partial_rows_fit(const ChunkShape& a, int64_t first, int splits, int groups) {
+  return splits == 1 || first + splits * groups * 32 <= a.head_part_rows;
 }
 
 // Tokens of a part, of which `blocks` blocks make at most n (128 .. 512) and a started one per row tile;

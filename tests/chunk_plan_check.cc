@@ -27,6 +27,32 @@ static void fail(const char* what, const ChunkShape& a, const ChunkPlan& p, int6
   std::exit(1);
 }
 
+// Starts in any order: no row tile that is done has partial results outside the workspace. Requests 64 at
+// a time, as a wave takes them.
+static void check_disorder(const ChunkShape& a, const ChunkPlan& p, bool latent, int part) {
+  int64_t rows = 0;
+  for (int base = 0; base < a.requests; base += 64) {
+    uint32_t in_wave = 0;
+    for (int r = base; r < std::min(base + 64, a.requests); ++r) {
+      const Request q = request_of(a, r);
+      if (q.begin < 0 || q.n < 0 || (int64_t)q.begin + q.n > a.total) fail("rows", a, p, q.begin, q.n);
+      int groups;
+      const int tiles = tiles_of(a, latent, q, groups), splits = splits_of(a, q, part);
+      const uint32_t items = items_of(tiles, splits);
+      for (uint32_t tile : {0u, items / splits / 2, items / splits - 1}) {
+        if (splits == 1 || tile >= items / splits) continue;
+        const int64_t first = (rows + in_wave + (int64_t)tile * splits * groups) * 32;
+        const int64_t end = first + (int64_t)splits * groups * 32;
+        if (partial_rows_fit(a, first, splits, groups) && (first < 0 || end > a.head_part_rows))
+          fail("partial results", a, p, end, a.head_part_rows);
+      }
+      if (splits > 1 && __builtin_add_overflow(in_wave, items * (uint32_t)groups, &in_wave))
+        fail("sum over a wave", a, p, items, 0);
+    }
+    rows += in_wave;
+  }
+}
+
 int main() {
   uint64_t sum = 0;
   int calls = 0;
@@ -54,6 +80,12 @@ int main() {
       len[r] = (int32_t)(chance(0.05) ? tokens : chance(0.5) ? upto(most_len) : most_len);
     }
     c.total_tokens = start[c.num_requests] + (chance(0.3) ? (int)upto(5000) : 0);
+    const bool disorder = chance(0.2);
+    if (disorder) {
+      if (chance(0.3)) c.total_tokens = (int)std::min<int64_t>(INT32_MAX / (c.kv_heads * c.q_heads), 1 << 30);
+      if (chance(0.3)) c.max_chunk = (int)upto(INT32_MAX);
+      for (int32_t& x : start) x = (int32_t)(rng() % 3 == 0 ? rng() : rng() % (c.total_tokens + 1u));
+    }
     if (c.total_tokens == 0 || (int64_t)c.total_tokens * c.kv_heads * c.q_heads > INT32_MAX) continue;
     const ChunkPlan p = plan_chunk(kv, c);
     const ChunkShape a = chunk_shape(kv, c, p, start.data(), len.data());
@@ -75,6 +107,10 @@ int main() {
           }
           return n;
         });
+    if (disorder) {
+      check_disorder(a, p, latent, part);
+      continue;
+    }
     int64_t items = 0, rows = 0, split = 0;
     for (int r = 0; r < a.requests; ++r) {
       const Request q = request_of(a, r);

@@ -53,3 +53,21 @@ def test_one_workspace_for_the_largest_batch(kind, type_, tpr):
         p.lse.fill_(MARK)
         p.run()
         p.check(f"{n} requests")
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("splits", [0, 3])
+def test_starts_that_descend_stay_inside_the_arrays(kind, type_, tpr, splits):
+    """Requests that have more rows between them than there are: whatever the rows hold, nothing is
+    written past them or past the workspace."""
+    p = shared(kind, type_, tpr, 2, 16, [(40, 960), (3, 500), (1, 960), (40, 64)] * 3, 960,
+               splits=splits)
+    rows = p.total
+    p.start = torch.tensor([0, 40, 0, 84, 10, 252, -9, 10 ** 9, 3, 44, 0, 84, 0], dtype=torch.int32,
+                           device="cuda")
+    p.out = torch.full((rows + 64, p.out.shape[1]), MARK, dtype=torch.bfloat16, device="cuda")
+    p.lse = torch.full((rows + 64, p.H), MARK, dtype=torch.float32, device="cuda")
+    p.run()
+    torch.cuda.synchronize()
+    assert bool((p.ws[p.ws_bytes:] == 0xFF).all())
+    assert bool((p.out[rows:] == torch.tensor(MARK).to(torch.bfloat16).cuda()).all()) and bool((p.lse[rows:] == MARK).all())
