@@ -631,8 +631,11 @@ typedef struct {
                                     share one row (a block table) */
   int32_t window;              /* 0, or the newest tokens a new token sees, its own included
                                   (needs HISPARSE_CHUNK_CAUSAL) */
-  int32_t num_splits;          /* parts the cached tokens are split into, 1 .. 64, merged in a fixed
-                                  order; 0 = chosen from the shape alone */
+  int32_t num_splits;          /* parts the cached tokens of a request are split into, merged in a fixed
+                                  order: 1 .. 64 (fewer where it has fewer blocks of 64), and its
+                                  results then do not depend on the rest of the batch; 0: chosen from
+                                  the descriptors and the lengths of all requests of the call, so that
+                                  a request's roundings may change with its neighbours */
   float scale;                 /* softmax scale applied to q.k, > 0, at most 1e6 */
   int32_t flags;               /* 0 or HISPARSE_CHUNK_CAUSAL */
 } hisparse_chunk_desc_t;

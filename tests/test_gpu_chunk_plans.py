@@ -70,4 +70,22 @@ def test_starts_that_descend_stay_inside_the_arrays(kind, type_, tpr, splits):
     p.run()
     torch.cuda.synchronize()
     assert bool((p.ws[p.ws_bytes:] == 0xFF).all())
-    assert bool((p.out[rows:] == torch.tensor(MARK).to(torch.bfloat16).cuda()).all()) and bool((p.lse[rows:] == MARK).all())
+    mark = torch.tensor(MARK).to(torch.bfloat16).cuda()
+    assert bool((p.out[rows:] == mark).all()) and bool((p.lse[rows:] == MARK).all())
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("splits", [1, 3])
+def test_a_given_number_of_splits_makes_results_independent_of_the_batch(kind, type_, tpr, splits):
+    """num_splits from 1 on: a request's bits do not change with its neighbours' lengths."""
+    mine = (5, 900)
+    p = shared(kind, type_, tpr, 2, 4, [(2, 70), mine, (1, 33)], 1120, splits=splits)
+    rows = slice(p.starts[1], p.starts[2])
+    a, la = p.out[rows].clone(), p.lse[rows].clone()
+    o = shared(kind, type_, tpr, 2, 4, [(7, 1120)] * 9 + [mine] + [(1, 1)] * 40, 1120,
+               splits=splits)
+    at = slice(o.starts[9], o.starts[10])
+    o.qd[at] = p.qd[rows]
+    o.run()
+    torch.cuda.synchronize()
+    assert torch.equal(o.out[at], a) and torch.equal(o.lse[at], la)
