@@ -680,9 +680,13 @@ size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
  * A new token that sees no cached token gives zeros and an lse of -inf. Scores, their maximum and
  * sums are kept in fp32; softmax weights are rounded to bf16 for the product with V. Where scores are
  * finite in fp32, results are too as long as the number of cached tokens times the largest |v| is below
- * 2^111. Rows that are not seen (padding, later tokens, tokens before the window, page ends) have no
- * influence, whatever they hold, infinities and NaN included; one that is seen and holds such a value
- * makes results not finite (latent: NaN). Results do not depend on where records lie.
+ * 2^111. Tokens that are not seen (padding, later tokens, tokens before the window, page ends) have no
+ * influence, whatever they hold, infinities and NaN included. One that is seen weighs by its score: at
+ * -inf nothing (a new token that sees no other score gives what one that sees nothing gives), at +inf
+ * or NaN every dim of the result and its lse are NaN. An infinity or NaN in a value that is seen makes
+ * its dim of the result not finite; in a latent, key and value at once, NaN, and where its score is
+ * not -inf all of the result and the lse (at -inf other dims and the lse are right or NaN too). Results
+ * do not depend on where records lie.
  * HISPARSE_ERR_INVALID_ARG for bad descriptors, null or misaligned pointers, or a workspace too
  * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more, or where
  * one launch would need 2^32 threads (512 for each 256 or fewer rows, kv head and split). */
