@@ -548,7 +548,10 @@ typedef enum {
    * least one with (largest finite magnitude of the part) <= 448 * scale, at least 2^-117, and 1
    * for a part without a finite nonzero value. Values round to nearest even, infinities become
    * +-448 * scale, NaN stays NaN. Being powers of two, the scales round nothing: reading back gives
-   * exactly the rounded values, and writing those again gives the same values. */
+   * exactly the rounded values, and writing those again gives the same values. The exception is a part
+   * whose largest finite magnitude is above 448 * 2^119, so that its scale is 2^120: from 248 * 2^120
+   * on a value rounds to 2^128, which bf16 cannot hold, and with it infinities beside it are read back
+   * (and attended to) as infinities. */
   HISPARSE_KV_FP8 = 1
 } hisparse_kv_type_t;
 

@@ -6,7 +6,7 @@
 //   q = round(x / s) to nearest even, at most 448;   read back: q s.
 // Dividing and multiplying by s only moves exponents, so e4m3's own rounding (half of 2^-3 of the
 // value) is the only one, and reading back rounds nothing in bf16 (4 significant bits of 8, exponents
-// from 2^-126 on: e >= -117, q >= 2^-9).
+// from 2^-126 on: e >= -117, q >= 2^-9; but for q from 256 on at e = 120, which become infinities).
 //
 // A group of lanes owns one (token, head): 16 lanes for grouped records (K and V rows of 256
 // bytes, 16 bytes of each per lane), 64 for latent ones (1024 bytes and, from 8 lanes, the 128

@@ -278,3 +278,25 @@ def test_captured_write_and_read_replay():
         rk, rv, _ = ref.stored(kind, k, v, type_)
         assert same(ok, rk) and same(ov, rv)
         ok.zero_()
+
+
+@pytest.mark.parametrize("kind,type_,tpr", [(G, F8, 16), (L, F8, 1)])
+def test_the_last_binade_reads_back_finite_or_as_infinity(kind, type_, tpr):
+    """Of values next to the largest bf16 number, those that round below 2^128 come back, the others as
+    infinities; a part of up to 448 * 2^119 has none."""
+    unit = 2.0 ** 120
+    cases = [[224.0, 100.0, -224.0], [225.0, 224.0, 1.0], [247.0, -247.0, 232.0], [248.0, 247.0, -64.0],
+             [255.0, -248.0, 3.0], [math.inf, 224.0, -math.inf], [math.inf, 225.0, 8.0]]
+    want = [[224.0, 96.0, -224.0], [224.0, 224.0, 1.0], [240.0, -240.0, 224.0],
+            [math.inf, 240.0, -64.0], [math.inf, -math.inf, 3.0], [224.0, 224.0, -224.0],
+            [math.inf, 224.0, 8.0]]
+    n = len(cases)
+    rows_, back = [], []
+    for d in ref.DIMS[kind]:
+        at = [c % 3 for c in range(d)]
+        rows_.append((torch.tensor(cases).double()[:, at] * unit).to(torch.bfloat16)[:, None])
+        back.append((torch.tensor(want).double()[:, at] * unit).to(torch.bfloat16)[:, None])
+    pool = write_and_check(kind, type_, tpr, 1, *rows_, None, (n + tpr - 1) // tpr)
+    got = read(kind, type_, tpr, pool, torch.arange(n), 1)
+    assert same(got[0], back[0])
+    assert same(got[1], back[1] if kind == G else rows_[1])  # rotary dims keep their bits
