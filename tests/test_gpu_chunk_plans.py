@@ -1,10 +1,14 @@
-"""hisparse_chunk_attention's ways of dividing a call. Compared as in test_gpu_chunk_attention."""
+"""hisparse_chunk_attention's ways of dividing a call: chunks without starts and lengths (split, in
+several row tiles, more tiles than CUs), batches padded to many more rows than they use, thousands of
+requests, and what a request's result may depend on. Compared as in test_gpu_chunk_attention."""
+import random
+
 import pytest
 import torch
 
 import token_reference as ref
 from paper_2608_07009_amd import hisparse as hs
-from test_gpu_chunk_attention import MARK, TYPES, Problem
+from test_gpu_chunk_attention import G, MARK, TYPES, Problem
 
 pytestmark = pytest.mark.gpu
 
@@ -56,22 +60,43 @@ def test_one_workspace_for_the_largest_batch(kind, type_, tpr):
 
 
 @pytest.mark.parametrize("kind,type_,tpr", TYPES)
-@pytest.mark.parametrize("splits", [0, 3])
-def test_starts_that_descend_stay_inside_the_arrays(kind, type_, tpr, splits):
-    """Requests that have more rows between them than there are: whatever the rows hold, nothing is
-    written past them or past the workspace."""
-    p = shared(kind, type_, tpr, 2, 16, [(40, 960), (3, 500), (1, 960), (40, 64)] * 3, 960,
-               splits=splits)
-    rows = p.total
-    p.start = torch.tensor([0, 40, 0, 84, 10, 252, -9, 10 ** 9, 3, 44, 0, 84, 0], dtype=torch.int32,
-                           device="cuda")
-    p.out = torch.full((rows + 64, p.out.shape[1]), MARK, dtype=torch.bfloat16, device="cuda")
-    p.lse = torch.full((rows + 64, p.H), MARK, dtype=torch.float32, device="cuda")
-    p.run()
-    torch.cuda.synchronize()
-    assert bool((p.ws[p.ws_bytes:] == 0xFF).all())
-    mark = torch.tensor(MARK).to(torch.bfloat16).cuda()
-    assert bool((p.out[rows:] == mark).all()) and bool((p.lse[rows:] == MARK).all())
+@pytest.mark.parametrize("requests,kv_heads,q_heads,n,splits", [
+    (3, 2, 4, 1, 0), (2, 1, 4, 5, 2), (3, 1, 4, 2, 3), (1, 8, 1, 1, 0), (2, 2, 16, 40, 0),
+    (2, 2, 16, 40, 3), (2, 1, 16, 21, 1)])
+def test_uniform_chunks_in_parts(kind, type_, tpr, requests, kv_heads, q_heads, n, splits):
+    """Neither starts nor lengths: split as chosen and as asked for, in one and in several row tiles."""
+    p = shared(kind, type_, tpr, kv_heads, q_heads, [(n, 1120)] * requests, 1120, splits=splits,
+               uniform=True, tail=3)
+    assert (p.ws_bytes > 0) == (splits != 1)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("splits", [0, 2])
+def test_more_uniform_chunks_than_cus(kind, type_, tpr, splits):
+    shared(kind, type_, tpr, 2, 4, [(1, 1120)] * 131, 1120, splits=splits, uniform=True)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("n", [1, 40])
+def test_few_rows_of_a_batch_padded_to_more_tiles_than_cus(kind, type_, tpr, n):
+    """Descriptors whose rows fill more tiles than there are CUs, of which the device finds a few (of
+    the largest kind for 40 tokens of 64 heads); two requests without cached or new tokens."""
+    p = shared(kind, type_, tpr, 1, 64, [(n, 2000), (0, 50), (2, 0)], 2000, tail=1100,
+               max_chunk=1100)
+    bm, d_v = (256, 128) if kind == G else (128, 512)
+    tiles = 1024 // 4 if kind == G else 1024 // 2
+    # the plan of a batch with more tiles than CUs: room for parts of 512 more items than row tiles
+    assert p.ws_bytes >= (tiles + 512) * bm * (4 * d_v + 8)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_thousands_of_requests(kind, type_, tpr):
+    """2100 requests of few tokens, one of them long."""
+    g = random.Random(8)
+    lens = [(g.choice((0, 1, 1, 2)), g.randint(0, 40)) for _ in range(2100)]
+    lens[1345] = (3, 3000)
+    p = shared(kind, type_, tpr, 1, 2, lens, 3008, tail=1)
+    assert p.ws_bytes > 0
 
 
 @pytest.mark.parametrize("kind,type_,tpr", TYPES)
@@ -89,3 +114,22 @@ def test_a_given_number_of_splits_makes_results_independent_of_the_batch(kind, t
     o.run()
     torch.cuda.synchronize()
     assert torch.equal(o.out[at], a) and torch.equal(o.lse[at], la)
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+@pytest.mark.parametrize("splits", [0, 3])
+def test_starts_that_descend_stay_inside_the_arrays(kind, type_, tpr, splits):
+    """Requests that have more rows between them than there are: whatever the rows hold, nothing is
+    written past them or past the workspace."""
+    p = shared(kind, type_, tpr, 2, 16, [(40, 960), (3, 500), (1, 960), (40, 64)] * 3, 960,
+               splits=splits)
+    rows = p.total
+    p.start = torch.tensor([0, 40, 0, 84, 10, 252, -9, 10 ** 9, 3, 44, 0, 84, 0], dtype=torch.int32,
+                           device="cuda")
+    p.out = torch.full((rows + 64, p.out.shape[1]), MARK, dtype=torch.bfloat16, device="cuda")
+    p.lse = torch.full((rows + 64, p.H), MARK, dtype=torch.float32, device="cuda")
+    p.run()
+    torch.cuda.synchronize()
+    assert bool((p.ws[p.ws_bytes:] == 0xFF).all())
+    mark = torch.tensor(MARK).to(torch.bfloat16).cuda()
+    assert bool((p.out[rows:] == mark).all()) and bool((p.lse[rows:] == MARK).all())
