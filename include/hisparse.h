@@ -692,7 +692,8 @@ size_t hisparse_chunk_workspace_bytes(const hisparse_kv_desc_t* kv,
  * do not depend on where records lie.
  * HISPARSE_ERR_INVALID_ARG for bad descriptors, null or misaligned pointers, or a workspace too
  * small; HISPARSE_ERR_UNSUPPORTED for total_tokens * kv_heads * q_heads of 2^31 or more, or where
- * one launch would need 2^32 threads (512 for each 256 or fewer rows, kv head and split). */
+ * one launch would need 2^32 threads (512 for each 256 or fewer rows, kv head and split). More than
+ * 1024 requests with starts or lengths are several launches, divided each for itself. */
 hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
                                            const hisparse_chunk_desc_t* chunk, const void* d_pool,
                                            const int32_t* d_table, const int32_t* d_chunk_start,

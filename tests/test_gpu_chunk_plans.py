@@ -8,7 +8,7 @@ import torch
 
 import token_reference as ref
 from paper_2608_07009_amd import hisparse as hs
-from test_gpu_chunk_attention import G, MARK, TYPES, Problem
+from test_gpu_chunk_attention import G, MARK, TYPES, Problem, run
 
 pytestmark = pytest.mark.gpu
 
@@ -133,3 +133,54 @@ def test_starts_that_descend_stay_inside_the_arrays(kind, type_, tpr, splits):
     assert bool((p.ws[p.ws_bytes:] == 0xFF).all())
     mark = torch.tensor(MARK).to(torch.bfloat16).cuda()
     assert bool((p.out[rows:] == mark).all()) and bool((p.lse[rows:] == MARK).all())
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_thousands_of_requests_without_starts(kind, type_, tpr):
+    """Lengths only, two new tokens each; rows behind the last."""
+    g = random.Random(9)
+    lens = [(2, g.randint(0, 40)) for _ in range(2050)]
+    lens[1500] = (2, 1100)
+    p = shared(kind, type_, tpr, 1, 2, lens, 1120, tail=5)
+    p.start = None
+    p.out.fill_(MARK)
+    p.lse.fill_(MARK)
+    p.run()
+    p.check()
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_more_requests_than_one_launch_takes_with_tables_of_their_own(kind, type_, tpr):
+    g = random.Random(10)
+    run(kind, type_, tpr, 1, 2, [(g.choice((0, 1, 2)), g.randint(1, 30)) for _ in range(1100)])
+
+
+@pytest.mark.parametrize("kind,type_,tpr", TYPES)
+def test_more_requests_than_one_launch_takes_with_pools_of_their_own(kind, type_, tpr):
+    """Slot caches [request][record]: with and without lengths the same bits."""
+    R, B = 1027, 2
+    gen = torch.Generator().manual_seed(1)
+    kk, vv = (torch.randn((R, B, tpr, d), generator=gen).to(torch.bfloat16)
+              for d in ref.DIMS[kind])
+    pool = ref.make_pool(kind, type_, tpr, kk, vv).cuda()
+    rb = pool.shape[-1]
+    kv = hs.KvDesc(kind, type_, tpr, rb, B, rb, B * rb, B * rb)
+    table = torch.tensor([[r % B, (r + 1) % B] for r in range(R)], dtype=torch.int32, device="cuda")
+    q = torch.randn((R, 3, ref.D_QK[kind]), generator=gen).to(torch.bfloat16).cuda()
+    c = hs.ChunkDesc(R, 1, 3, R, 1, B, 3 * ref.D_QK[kind], 3 * ref.D_V[kind], B, 0, 0, 0, 0.1, 0)
+    ws = torch.empty(hs.hisparse_chunk_workspace_bytes(kv, c), dtype=torch.uint8, device="cuda")
+    lens = torch.full((R,), B * tpr, dtype=torch.int32, device="cuda")
+    results = []
+    for kv_len in (None, lens):
+        out = torch.zeros((R, 3, ref.D_V[kind]), dtype=torch.bfloat16, device="cuda")
+        lse = torch.zeros((R, 3), device="cuda")
+        hs.hisparse_chunk_attention(kv, c, pool, table, None, kv_len, q, out, lse, ws, ws.numel(),
+                                    torch.cuda.current_stream())
+        results.append((out, lse))
+    torch.cuda.synchronize()
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
+    for r in (0, 1023, 1024, R - 1):
+        rows = [x[r][table[r].long().cpu()].flatten(0, 1) for x in (kk, vv)]
+        sk, sv, _ = ref.stored(kind, *rows, type_)
+        e = ref.attend(kind, sk, sv, q[r:r + 1].cpu(), torch.ones((1, B * tpr), dtype=torch.bool), 0.1)
+        ref.check(kind, results[1][0][r:r + 1], results[1][1][r:r + 1], e, f"request {r}")
