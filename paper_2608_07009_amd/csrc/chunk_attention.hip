@@ -366,7 +366,10 @@ __device__ __forceinline__ void mask_scores(f32x16& s, uint32_t seen) {
   }
 }
 // Softmax weights of 16 N scores (raw products) of this lane's row against a reference, in pairs
-// rounded to bf16 (times their tokens' value scales, if given); returns their unrounded sum.
+// rounded to bf16 (times their tokens' value scales, if given: powers of two, which round nothing);
+// returns their unrounded sum. The rounding is the MFMA operand's: 2^-8 of a weight at most, each token's
+// its own, so that results are off by 0.0019 to 0.0024 of their norm, and by 0.0017 from their own
+// rounding to bf16 alone. A weight in two bf16 terms would double the MFMAs with V.
 template <int N>
 __device__ __forceinline__ float weights_of(uint32_t (&pw)[N][8], const f32x16 (&s)[N],
                                             float scale, float ref,
@@ -457,8 +460,9 @@ __device__ __forceinline__ void next_weights(uint32_t (&pw)[N][8], f32x16 (&s)[N
 // each.
 //
 // Many rows are bound by the issue of MFMAs and of the softmax (6 other vector instructions for each
-// MFMA): 2048 tokens x 64 heads on 4 kv heads over 16384 tokens in 1030 us, 1.00 PFLOP/s. Few rows are
-// bound by HBM: one token of 64 requests x 8 kv heads x 4 over 4096 8-bit tokens in 111 us, 5.0 TB/s.
+// MFMA): 2048 tokens x 64 heads on 4 kv heads over 16384 tokens in 1030 us, 1.00 PFLOP/s (other cards up
+// to 1060). Few rows are bound by HBM: one token of 64 requests x 8 kv heads x 4 over 4096 8-bit tokens
+// in 111 us, 5.0 TB/s.
 
 using GTile = Tile<32>;  // 32 tokens of 32 pieces: K 0..15, V 16..31
 
@@ -926,9 +930,10 @@ __global__ __launch_bounds__(512, 2) void chunk_grouped_kernel(ChunkArgs a) {
 // by its token's (the rotary part, a chain of MFMAs of its own, is not), and so is the weight that
 // goes with the token's value.
 // Bound by the issue of one wave a SIMD (a vector instruction costs it about 8 cycles, an MFMA 32): 512
-// tokens of 128 heads over 8192 16-bit tokens in 1021 us, 1.11 PFLOP/s; 8-bit 1240, 0.91, for 256
-// widening instructions a tile. One token of 32 requests over 2048 8-bit tokens: 41 us and 9 for the
-// merge, of which start 6, eight rounds of two tiles 26, results 4.5.
+// tokens of 128 heads over 8192 16-bit tokens in 1021 us (other cards up to 1060), 1.11 PFLOP/s; 8-bit
+// 1240, 0.91, for 256 widening instructions a tile. One token of 32 requests over 2048 8-bit tokens: 41 us
+// and 9 for the merge, of which start 6, eight rounds of two tiles 26, results 4.5. 59 vector registers
+// are spilled (8-bit; 16-bit 20), around the tiles' MFMAs, not between them.
 
 using LTile = Tile<72>;  // 16-bit rows
 using PTile = Tile<32>;  // 8-bit latent rows of 512 bytes

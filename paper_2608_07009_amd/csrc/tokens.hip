@@ -12,8 +12,10 @@
 // bytes, 16 bytes of each per lane), 64 for latent ones (1024 bytes and, from 8 lanes, the 128
 // rotary bytes). Rows are read and written in whole 16-byte pieces, runs of 128 to 1024 bytes, each
 // byte once; the amax is a reduction over the group's lanes in registers. Bound by HBM: 32768 tokens of
-// 8 kv heads written to 8-bit pages in 34 us (204 MB, 6.0 TB/s), 65536 latent tokens read back in 21
-// (118 MB, 5.6 TB/s); a copy of 1 GiB reaches 5.2. 32 tokens: 2.9 us.
+// 8 kv heads written to 8-bit pages in 34 us on the device (204 MB), 65536 latent tokens read back in 21
+// (118 MB). Both are above the 5.2 TB/s of a 1 GiB copy, for part of what they move stays in the
+// last-level cache. Call after call, in TB/s: 32768 tokens of 8 kv heads written 5.1 (16-bit) and 4.7 (8-bit),
+// read 5.2 and 4.8; 65536 latent tokens written 4.5 and 4.4, read 4.0 and 3.9. 32 tokens: 2.9 us.
 #include "fetch_device.h"
 #include "tokens.h"
 
