@@ -701,6 +701,261 @@ hisparse_status_t hisparse_chunk_attention(const hisparse_kv_desc_t* kv,
                                            float* d_lse, void* d_workspace,
                                            size_t workspace_bytes, void* stream);
 
+/* ---- Before the attention: a batch's tables, rotary positions, index rows, selections -------
+ *
+ * One layer's step over records, in order: hisparse_plan_tokens (once for all layers) says where the
+ * new tokens go, hisparse_rotate_tokens turns their rows, hisparse_write_tokens writes them,
+ * hisparse_summarize_records keeps the index rows of the records they went to, and
+ * hisparse_select_records chooses each new token's records, which hisparse_resolve or
+ * hisparse_chunk_attention takes. No call needs a cache handle. */
+
+/* The requests of a batch and their record tables, as in hisparse_chunk_desc_t. */
+typedef struct {
+  int32_t num_requests;          /* >= 1 */
+  int32_t kv_heads;              /* >= 1; at most 2^20 of all requests */
+  int32_t total_tokens;          /* rows of new tokens of all requests, or more; >= 0 */
+  int32_t max_chunk;             /* the most new tokens of a request, >= 1; a longer chunk is held to
+                                    its first max_chunk */
+  int32_t max_records;           /* entries of a record table row: the longest request's records;
+                                    max_records * tokens_per_record at most 2^30 */
+  int32_t tokens_per_record;     /* 1, 2, 4, ... 4096 */
+  int64_t table_request_stride;  /* entries from one request's table to the next one's, >= 0 */
+  int64_t table_head_stride;     /* and from one kv head's row to the next one's; 0: the heads share
+                                    one row (a block table) */
+} hisparse_batch_desc_t;
+
+/* [pure host] Check a batch descriptor. */
+hisparse_status_t hisparse_validate_batch(const hisparse_batch_desc_t* batch);
+
+/* [async] Block tables, slot map and positions of a batch of new tokens, from its lengths.
+ *   d_new_len        int32 [num_requests]: new tokens of each request, 0 for none; held to [0,
+ *                    max_chunk], to what its table row has room for, and all of them together, request
+ *                    by request, to total_tokens rows.
+ *   d_kv_len         int32 [num_requests]: tokens cached before, held to [0, max_records *
+ *                    tokens_per_record]. NULL: none.
+ *   d_free, num_free int32 [num_free]: records that no request has. The records that the new tokens
+ *                    begin are taken from it in order, request by request. NULL (num_free 0): the
+ *                    tables hold them already, and d_table is not written.
+ *   d_free_used      int32 [1]: entries of d_free used before, held to [0, num_free]. NULL: none.
+ *   d_table          int32, row of request q at q * table_request_stride (table_head_stride 0; rows
+ *                    apart by at least max_records with several requests and a free list): read where a
+ *                    request's cached tokens end inside a record; the entries of records that begin
+ *                    are written, no other one is. -1 is written where d_free has none left: tokens in
+ *                    such a record have no slot and are not seen by later calls.
+ *   d_chunk_start    int32 [num_requests + 1], out: request q's new tokens are rows start[q] ..
+ *                    start[q + 1] - 1.
+ *   d_kv_len_out     int32 [num_requests], out: cached tokens, the new ones included. May be d_kv_len.
+ *   d_free_used_out  int32 [1] or NULL, out: d_free_used and the records that begin. Above num_free: so
+ *                    many were missing. May be d_free_used.
+ *   d_positions      int32 [total_tokens] or NULL, out: each new token's position in its request; 0
+ *                    in rows behind the last.
+ *   d_slots          int64 [total_tokens] or NULL, out: its token slot, as hisparse_write_tokens takes
+ *                    it, or -1 (no record, or a row behind the last), which that call skips.
+ * The outputs and d_table, d_free, d_new_len must not overlap, but for the two pairs named.
+ * HISPARSE_ERR_INVALID_ARG for a bad descriptor, null (d_new_len, d_table, d_chunk_start,
+ * d_kv_len_out) or misaligned pointers, num_free < 0, num_free > 0 without d_free or d_free without
+ * it, or table strides other than said; HISPARSE_ERR_UNSUPPORTED for num_free + total_tokens of 2^31 or
+ * more. */
+hisparse_status_t hisparse_plan_tokens(const hisparse_batch_desc_t* batch,
+                                       const int32_t* d_new_len, const int32_t* d_kv_len,
+                                       const int32_t* d_free, int32_t num_free,
+                                       const int32_t* d_free_used, int32_t* d_table,
+                                       int32_t* d_chunk_start, int32_t* d_kv_len_out,
+                                       int32_t* d_free_used_out, int32_t* d_positions,
+                                       int64_t* d_slots, void* stream);
+
+/* Which dims make a pair, of the rotated dims 0 .. dims - 1. */
+typedef enum {
+  HISPARSE_ROTARY_HALF = 0,        /* i and i + dims / 2 */
+  HISPARSE_ROTARY_INTERLEAVED = 1  /* 2 i and 2 i + 1 */
+} hisparse_rotary_layout_t;
+
+/* The frequency of pair i, in radians a position; f = theta^(-2 i / dims). */
+typedef enum {
+  HISPARSE_ROTARY_PLAIN = 0,   /* f */
+  HISPARSE_ROTARY_LINEAR = 1,  /* f / factor: positions of a longer context squeezed into the trained one */
+  /* f * (s + (1 - s) / factor), s = (r - low_turns) / (high_turns - low_turns) held to [0, 1], r = the
+   * turns that the pair makes over the trained context, original_tokens * f / (2 pi): fast pairs as they
+   * are, slow ones squeezed, a ramp between. */
+  HISPARSE_ROTARY_BY_PARTS = 2
+} hisparse_rotary_scaling_t;
+
+/* hisparse_rotary_desc_t.flags: turn by the negative angle: the gradient of the rows from the gradient
+ * of the turned ones, or (magnitude 1) back to rows without a position. */
+#define HISPARSE_ROTARY_BACK 1
+
+typedef struct {
+  int32_t dims;      /* rotated dims of a head: even, 2 .. 256 */
+  int32_t layout;    /* hisparse_rotary_layout_t */
+  int32_t scaling;   /* hisparse_rotary_scaling_t */
+  int32_t flags;     /* 0 or HISPARSE_ROTARY_BACK */
+  double theta;      /* > 0 */
+  double factor;     /* > 0; not used by PLAIN */
+  double original_tokens, low_turns, high_turns;  /* BY_PARTS: > 0, and low_turns < high_turns */
+  double magnitude;  /* factor of the rotated dims, finite; 1: lengths are kept */
+} hisparse_rotary_desc_t;
+
+/* One array of rows to turn, bf16: row t of head h at d_in + t * in_token_stride + h * in_head_stride
+ * elements, `dims` elements of which first .. first + rotary.dims - 1 are turned and the others copied.
+ * Written to d_out likewise; token t's rows to row d_out_rows[t] of d_out if that is given, and nowhere
+ * if that row is outside [0, num_out_rows) (a slot map of a pool of rows). Any alignment.
+ * d_out may be d_in with the same strides and no d_out_rows: then only the rotated dims are written.
+ * Otherwise no array written may overlap one that is read or written in the same call; out rows of a
+ * token and head must not overlap, nor d_out_rows repeat a row. */
+typedef struct {
+  const void* d_in;
+  void* d_out;
+  const int64_t* d_out_rows;  /* int64 [num_tokens] or NULL */
+  int64_t num_out_rows;       /* >= 0; not used without d_out_rows */
+  int64_t in_token_stride, in_head_stride, out_token_stride, out_head_stride;  /* >= 0 */
+  int32_t heads;              /* >= 1 */
+  int32_t dims;               /* >= first + rotary.dims, at most 65536 */
+  int32_t first;              /* >= 0 */
+} hisparse_rotary_rows_t;
+
+/* Arrays of rows that one call takes. */
+#define HISPARSE_ROTARY_MAX_ROWS 4
+
+/* [pure host] Check a rotary descriptor. */
+hisparse_status_t hisparse_validate_rotary(const hisparse_rotary_desc_t* rotary);
+
+/* [pure host] The dims / 2 frequencies of a descriptor, in radians a position. */
+hisparse_status_t hisparse_rotary_frequencies(const hisparse_rotary_desc_t* rotary,
+                                              double* frequencies);
+
+/* [async] Rotary positions: in each of num_rows arrays (1 .. HISPARSE_ROTARY_MAX_ROWS: queries, keys, those of an
+ * index) every pair (a, b) of token t becomes
+ *   (a cos x - b sin x, b cos x + a sin x) * magnitude,  x = d_positions[t] * frequency of the pair,
+ * angles in 64 bits, the rest in fp32, rounded to bf16 once.
+ *   d_positions  int32 [num_tokens]; any value, of either sign.
+ * The rows structs are read before the call returns. num_tokens 0 does nothing.
+ * HISPARSE_ERR_INVALID_ARG for a bad descriptor, null or misaligned pointers, num_tokens < 0, bad heads,
+ * dims, first or strides (with several heads an out_head_stride below dims, with several tokens an
+ * out_token_stride below dims), or d_out equal to d_in with other strides or d_out_rows;
+ * HISPARSE_ERR_UNSUPPORTED if num_tokens * heads * dims of all arrays is 2^38 or more. */
+hisparse_status_t hisparse_rotate_tokens(const hisparse_rotary_desc_t* rotary, int32_t num_tokens,
+                                         const int32_t* d_positions,
+                                         const hisparse_rotary_rows_t* rows, int32_t num_rows,
+                                         void* stream);
+
+/* What a selection scores its candidates by, all bf16, 128 dims. */
+typedef enum {
+  /* a key of its own for each token: candidates are tokens; an index record holds
+   * [tokens_per_record][128] */
+  HISPARSE_INDEX_KEYS = 0,
+  /* the least and the largest value of each dim over a record's keys: candidates are records; [2][128],
+   * the least ones first */
+  HISPARSE_INDEX_BOUNDS = 1,
+  /* the mean of a record's keys: [128] */
+  HISPARSE_INDEX_MEANS = 2
+} hisparse_index_kind_t;
+
+/* Where the index records are: that of record r of kv head h of request q at
+ *   d_index + q * request_stride + h * head_stride + r * record_stride bytes.
+ * r is the entry of the record table, so that an index beside a pool of pages has a record per page; or,
+ * without a table, the record's place in its request (request_stride then tells the requests apart). */
+typedef struct {
+  int32_t kind;               /* hisparse_index_kind_t */
+  int32_t tokens_per_record;  /* 1, 2, 4, ... 4096 */
+  int64_t num_records;        /* 1 .. 2^31 - 1: entries outside [0, num_records) are padding */
+  int64_t record_stride;      /* bytes, multiples of 16, >= 0; record_stride at least a record's bytes and
+                                 below 2^31 */
+  int64_t head_stride;
+  int64_t request_stride;
+} hisparse_index_desc_t;
+
+/* [pure host] Check an index descriptor. */
+hisparse_status_t hisparse_validate_index(const hisparse_index_desc_t* index);
+
+/* [async] The index rows (BOUNDS or MEANS) of every record that holds new tokens of the batch, from the keys
+ * of all its tokens: call it after hisparse_write_tokens, with the same lengths.
+ *   kv             grouped records (HISPARSE_KV_GROUPED), bf16 or 8-bit; the keys are taken as read back.
+ *   d_table        int32 as in hisparse_chunk_attention, or NULL: record j of a request is its record j.
+ *                  Of an entry that is padding in the pool or in the index nothing is read or written.
+ *   d_chunk_start  int32 [num_requests + 1] and
+ *   d_kv_len       int32 [num_requests] as there, either may be NULL: new tokens (max_chunk each) and
+ *                  cached tokens (max_records * tokens_per_record) of each request. A last record that
+ *                  is not full is summarised over the tokens it holds.
+ *   d_index        out: one or two rows of 128 per record and kv head.
+ * Bounds are exact; a NaN in a dim makes its bounds NaN. Means are summed in fp32 in a fixed order and rounded
+ * to bf16 once. Index records of other records keep what they hold. If two requests share a record that
+ * both write to, its row is that of one of them.
+ * HISPARSE_ERR_INVALID_ARG for bad or differing descriptors (tokens_per_record alike in all three),
+ * index kind KEYS, null or misaligned pointers (pool and index 16 bytes), a head_stride that lets kv heads'
+ * index records overlap, or d_chunk_start NULL and total_tokens < num_requests * max_chunk;
+ * HISPARSE_ERR_UNSUPPORTED for latent records, or where a launch would need 2^32 threads (64 for each
+ * record and kv head). */
+hisparse_status_t hisparse_summarize_records(const hisparse_kv_desc_t* kv,
+                                             const hisparse_index_desc_t* index,
+                                             const hisparse_batch_desc_t* batch,
+                                             const void* d_pool, const int32_t* d_table,
+                                             const int32_t* d_chunk_start, const int32_t* d_kv_len,
+                                             void* d_index, void* stream);
+
+typedef struct {
+  int32_t q_heads;        /* queries on each kv head: KEYS 1 .. 128, else 1 .. 256 */
+  int32_t top_k;          /* 1 .. 4096 */
+  int32_t first_records;  /* >= 0: of the candidates a new token sees, so many first and */
+  int32_t last_records;   /* >= 0: so many newest are always chosen; at most top_k together */
+  int64_t q_token_stride;  /* elements from one new token's queries to the next one's, >= 0 */
+} hisparse_select_desc_t;
+
+/* [pure host] Check a selection's descriptors. */
+hisparse_status_t hisparse_validate_select(const hisparse_index_desc_t* index,
+                                           const hisparse_batch_desc_t* batch,
+                                           const hisparse_select_desc_t* select);
+
+/* [pure host] Bytes of device scratch for the call; 0 for invalid descriptors. A workspace of this size serves
+ * every call of at most as many tokens and records with the same index kind and select and as many or
+ * fewer kv heads. (The scores of all new tokens, held to 1 GiB or the scores of one tile of them: a call
+ * goes over its tokens in as many steps as its workspace takes, and smaller workspaces, down to one tile's,
+ * are accepted too. Results do not depend on it.) */
+size_t hisparse_select_workspace_bytes(const hisparse_index_desc_t* index,
+                                       const hisparse_batch_desc_t* batch,
+                                       const hisparse_select_desc_t* select);
+
+/* [async] The best candidates of each new token and kv head. New token i of n of a request with len cached
+ * tokens, at position p = len - n + i, sees candidates 0 .. p (KEYS), or 0 .. p / tokens_per_record
+ * (records, the one that holds it the last); padding entries are not seen. Candidate j scores, over the
+ * kv head's queries q_e,
+ *   KEYS    sum_e w_e max(0, q_e . key_j)
+ *   BOUNDS  sum_e sum_d max(q_ed least_jd, q_ed largest_jd), taken as the sum over d of largest_jd times
+ *           the sum of the positive q_ed, and least_jd times that of the negative ones
+ *   MEANS   (sum_e q_e) . mean_j
+ * and chosen are the first and last ones asked for and the best others, min(top_k, what it sees) in all.
+ * The choice is that of scores in 64 bits, the lower position first among equals, NaN above everything:
+ * fast scores only tell apart what their error bound does, and what that leaves open is scored again.
+ * It does not depend on the rest of the batch, and index rows that are not seen have no influence,
+ * whatever they hold.
+ *   d_table, d_chunk_start, d_kv_len  as in hisparse_summarize_records. Rows outside every chunk (a batch
+ *                padded to a fixed size) are neither read nor written.
+ *   d_q          bf16, token i's queries at i * q_token_stride, [kv_heads * q_heads][128]. Any alignment.
+ *   d_weights    float32 [total_tokens][kv_heads * q_heads], KEYS only, or NULL: 1.
+ *   d_sel        int32 [total_tokens][kv_heads][top_k], out: the chosen candidates' positions in the
+ *                request, ascending, and -1 behind them; with last_records > 0 the newest, p's own, stands
+ *                at place min(top_k, p's candidates) - 1 even where padding leaves others empty. With one
+ *                new token a request this is the selection hisparse_resolve takes.
+ *   d_records    int32 likewise or NULL: the entry of the record table (KEYS: that times tokens_per_record
+ *                and the token's place in it) instead of the position: with top_k as max_records, a
+ *                request per row, chunks of 1, this and d_sel_len are d_table and d_kv_len of
+ *                hisparse_chunk_attention over the selected records.
+ *   d_sel_len    int32 [total_tokens] or NULL, out: tokens up to the row's own in those tables (0 for a token
+ *                that sees nothing). Needs last_records > 0.
+ *   d_workspace  a multiple of 16; calls that may overlap need one each.
+ * HISPARSE_ERR_INVALID_ARG for bad descriptors (tokens_per_record of index and batch alike), null or
+ * misaligned pointers (d_index and d_workspace 16 bytes), d_weights with another kind than KEYS, d_sel_len
+ * without last_records, too small a workspace, or d_chunk_start NULL and total_tokens < num_requests * max_chunk;
+ * HISPARSE_ERR_UNSUPPORTED for KEYS with d_records and num_records * tokens_per_record of 2^31 or more,
+ * total_tokens * kv_heads of 2^31 or more, or kv_heads times candidates of 2^30 or more. */
+hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* index,
+                                          const hisparse_batch_desc_t* batch,
+                                          const hisparse_select_desc_t* select, const void* d_index,
+                                          const int32_t* d_table, const int32_t* d_chunk_start,
+                                          const int32_t* d_kv_len, const void* d_q,
+                                          const float* d_weights, int32_t* d_sel,
+                                          int32_t* d_records, int32_t* d_sel_len,
+                                          void* d_workspace, size_t workspace_bytes, void* stream);
+
 /* [sync] Copy an anchor layer's resolve state into host buffers (any may be NULL):
  * slot_pos int32 [units][B], slot_ts uint32 [units][B], page_table int32 [units][L],
  * order int32 [units][B] (slots by ascending (timestamp, slot)), clock uint32 [units]. */

@@ -39,6 +39,16 @@ HISPARSE_KV_LATENT = 1
 HISPARSE_KV_BF16 = 0
 HISPARSE_KV_FP8 = 1
 HISPARSE_CHUNK_CAUSAL = 1
+HISPARSE_ROTARY_HALF = 0
+HISPARSE_ROTARY_INTERLEAVED = 1
+HISPARSE_ROTARY_PLAIN = 0
+HISPARSE_ROTARY_LINEAR = 1
+HISPARSE_ROTARY_BY_PARTS = 2
+HISPARSE_ROTARY_BACK = 1
+HISPARSE_ROTARY_MAX_ROWS = 4
+HISPARSE_INDEX_KEYS = 0
+HISPARSE_INDEX_BOUNDS = 1
+HISPARSE_INDEX_MEANS = 2
 
 HISPARSE_RESOLVE_PHASE_SLOTS = 16
 HISPARSE_RESOLVE_PHASE_UNITS = 64
@@ -64,6 +74,10 @@ EXPORTED = (
     "hisparse_kv_record_bytes", "hisparse_validate_kv", "hisparse_write_tokens",
     "hisparse_read_tokens", "hisparse_validate_chunk", "hisparse_chunk_workspace_bytes",
     "hisparse_chunk_attention",
+    "hisparse_validate_batch", "hisparse_plan_tokens", "hisparse_validate_rotary",
+    "hisparse_rotary_frequencies", "hisparse_rotate_tokens", "hisparse_validate_index",
+    "hisparse_summarize_records", "hisparse_validate_select", "hisparse_select_workspace_bytes",
+    "hisparse_select_records",
     "hisparse_read_state", "hisparse_read_plan", "hisparse_check_errors",
     "hisparse_debug_resolve_phases",
 )
@@ -100,6 +114,40 @@ class ChunkDesc(ctypes.Structure):
                 ("table_request_stride", ctypes.c_int64), ("table_head_stride", ctypes.c_int64),
                 ("window", ctypes.c_int32), ("num_splits", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("flags", ctypes.c_int32)]
+
+
+class BatchDesc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("total_tokens", ctypes.c_int32), ("max_chunk", ctypes.c_int32),
+                ("max_records", ctypes.c_int32), ("tokens_per_record", ctypes.c_int32),
+                ("table_request_stride", ctypes.c_int64), ("table_head_stride", ctypes.c_int64)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("dims", ctypes.c_int32), ("layout", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("theta", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_tokens", ctypes.c_double), ("low_turns", ctypes.c_double),
+                ("high_turns", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class RotaryRows(ctypes.Structure):
+    _fields_ = [("d_in", ctypes.c_void_p), ("d_out", ctypes.c_void_p),
+                ("d_out_rows", ctypes.c_void_p), ("num_out_rows", ctypes.c_int64),
+                ("in_token_stride", ctypes.c_int64), ("in_head_stride", ctypes.c_int64),
+                ("out_token_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("dims", ctypes.c_int32), ("first", ctypes.c_int32)]
+
+
+class IndexDesc(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("tokens_per_record", ctypes.c_int32),
+                ("num_records", ctypes.c_int64), ("record_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("request_stride", ctypes.c_int64)]
+
+
+class SelectDesc(ctypes.Structure):
+    _fields_ = [("q_heads", ctypes.c_int32), ("top_k", ctypes.c_int32),
+                ("first_records", ctypes.c_int32), ("last_records", ctypes.c_int32),
+                ("q_token_stride", ctypes.c_int64)]
 
 
 class HisparseError(RuntimeError):
@@ -186,6 +234,28 @@ def lib() -> ctypes.CDLL:
             "hisparse_chunk_attention": (_I32, [ctypes.POINTER(KvDesc),
                                                 ctypes.POINTER(ChunkDesc), _V, _V, _V, _V, _V,
                                                 _V, _V, _V, ctypes.c_size_t, _V]),
+            "hisparse_validate_batch": (_I32, [ctypes.POINTER(BatchDesc)]),
+            "hisparse_plan_tokens": (_I32, [ctypes.POINTER(BatchDesc), _V, _V, _V, _I32, _V, _V,
+                                            _V, _V, _V, _V, _V, _V]),
+            "hisparse_validate_rotary": (_I32, [ctypes.POINTER(RotaryDesc)]),
+            "hisparse_rotary_frequencies": (_I32, [ctypes.POINTER(RotaryDesc), _V]),
+            "hisparse_rotate_tokens": (_I32, [ctypes.POINTER(RotaryDesc), _I32, _V,
+                                              ctypes.POINTER(RotaryRows), _I32, _V]),
+            "hisparse_validate_index": (_I32, [ctypes.POINTER(IndexDesc)]),
+            "hisparse_summarize_records": (_I32, [ctypes.POINTER(KvDesc),
+                                                  ctypes.POINTER(IndexDesc),
+                                                  ctypes.POINTER(BatchDesc), _V, _V, _V, _V, _V,
+                                                  _V]),
+            "hisparse_validate_select": (_I32, [ctypes.POINTER(IndexDesc),
+                                                ctypes.POINTER(BatchDesc),
+                                                ctypes.POINTER(SelectDesc)]),
+            "hisparse_select_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(IndexDesc),
+                                                                  ctypes.POINTER(BatchDesc),
+                                                                  ctypes.POINTER(SelectDesc)]),
+            "hisparse_select_records": (_I32, [ctypes.POINTER(IndexDesc),
+                                               ctypes.POINTER(BatchDesc),
+                                               ctypes.POINTER(SelectDesc), _V, _V, _V, _V, _V, _V,
+                                               _V, _V, _V, _V, ctypes.c_size_t, _V]),
             "hisparse_read_state": (_I32, [_V, _I32, _V, _V, _V, _V, _V]),
             "hisparse_read_plan": (_I32, [_V, _I32, _V, _V]),
             "hisparse_check_errors": (_I32, [_V, _V]),
@@ -476,6 +546,75 @@ def hisparse_chunk_attention(kv: KvDesc, chunk: ChunkDesc, d_pool, d_table, d_ch
                                           _p(d_table), _p(d_chunk_start), _p(d_kv_len), _p(d_q),
                                           _p(d_out), _p(d_lse), _p(d_workspace),
                                           workspace_bytes, _s(stream)))
+
+
+def hisparse_validate_batch(batch: BatchDesc) -> int:
+    return lib().hisparse_validate_batch(ctypes.byref(batch))
+
+
+def hisparse_plan_tokens(batch: BatchDesc, d_new_len, d_kv_len, d_free, num_free: int, d_free_used,
+                         d_table, d_chunk_start, d_kv_len_out, d_free_used_out=None,
+                         d_positions=None, d_slots=None, stream=None) -> None:
+    _check("hisparse_plan_tokens",
+           lib().hisparse_plan_tokens(ctypes.byref(batch), _p(d_new_len), _p(d_kv_len),
+                                      _p(d_free), num_free, _p(d_free_used), _p(d_table),
+                                      _p(d_chunk_start), _p(d_kv_len_out), _p(d_free_used_out),
+                                      _p(d_positions), _p(d_slots), _s(stream)))
+
+
+def hisparse_validate_rotary(rotary: RotaryDesc) -> int:
+    return lib().hisparse_validate_rotary(ctypes.byref(rotary))
+
+
+def hisparse_rotary_frequencies(rotary: RotaryDesc) -> np.ndarray:
+    """float64 [dims / 2], radians a position."""
+    out = np.zeros(max(1, rotary.dims // 2), dtype=np.float64)
+    _check("hisparse_rotary_frequencies",
+           lib().hisparse_rotary_frequencies(ctypes.byref(rotary), out.ctypes.data))
+    return out
+
+
+def hisparse_rotate_tokens(rotary: RotaryDesc, num_tokens: int, d_positions, rows, num_rows: int,
+                           stream=None) -> None:
+    """rows: a ctypes array of RotaryRows (or one RotaryRows)."""
+    p = ctypes.byref(rows) if isinstance(rows, RotaryRows) else rows
+    _check("hisparse_rotate_tokens",
+           lib().hisparse_rotate_tokens(ctypes.byref(rotary), num_tokens, _p(d_positions), p,
+                                        num_rows, _s(stream)))
+
+
+def hisparse_validate_index(index: IndexDesc) -> int:
+    return lib().hisparse_validate_index(ctypes.byref(index))
+
+
+def hisparse_summarize_records(kv: KvDesc, index: IndexDesc, batch: BatchDesc, d_pool, d_table,
+                               d_chunk_start, d_kv_len, d_index, stream=None) -> None:
+    _check("hisparse_summarize_records",
+           lib().hisparse_summarize_records(ctypes.byref(kv), ctypes.byref(index),
+                                            ctypes.byref(batch), _p(d_pool), _p(d_table),
+                                            _p(d_chunk_start), _p(d_kv_len), _p(d_index),
+                                            _s(stream)))
+
+
+def hisparse_validate_select(index: IndexDesc, batch: BatchDesc, select: SelectDesc) -> int:
+    return lib().hisparse_validate_select(ctypes.byref(index), ctypes.byref(batch),
+                                          ctypes.byref(select))
+
+
+def hisparse_select_workspace_bytes(index: IndexDesc, batch: BatchDesc, select: SelectDesc) -> int:
+    return lib().hisparse_select_workspace_bytes(ctypes.byref(index), ctypes.byref(batch),
+                                                 ctypes.byref(select))
+
+
+def hisparse_select_records(index: IndexDesc, batch: BatchDesc, select: SelectDesc, d_index,
+                            d_table, d_chunk_start, d_kv_len, d_q, d_weights, d_sel, d_records,
+                            d_sel_len, d_workspace, workspace_bytes: int, stream=None) -> None:
+    _check("hisparse_select_records",
+           lib().hisparse_select_records(ctypes.byref(index), ctypes.byref(batch),
+                                         ctypes.byref(select), _p(d_index), _p(d_table),
+                                         _p(d_chunk_start), _p(d_kv_len), _p(d_q), _p(d_weights),
+                                         _p(d_sel), _p(d_records), _p(d_sel_len), _p(d_workspace),
+                                         workspace_bytes, _s(stream)))
 
 
 def hisparse_read_state(cache: int, layer: int, slot_pos=None, slot_ts=None, page_table=None,

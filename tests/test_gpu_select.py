@@ -1,0 +1,433 @@
+"""hisparse_select_records against a full ranking of 64-bit scores. Choices are whole numbers: compared
+exactly. Real-valued rows give no equal scores (64-bit sums of 128 to 8192 products of 8-bit numbers, whose
+roundings, 2^-46 of a score at most, would have to hide a gap between neighbours); where scores are equal
+on purpose, all values are small whole numbers and every sum is exact."""
+import math
+import random
+
+import pytest
+import torch
+
+import step_reference as ref
+from paper_2608_07009_amd import hisparse as hs
+
+pytestmark = pytest.mark.gpu
+KEYS, BOUNDS, MEANS = ref.KEYS, ref.BOUNDS, ref.MEANS
+MARK = -77
+
+
+def randn(shape, seed, dtype=torch.bfloat16):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype)
+
+
+class Case:
+    """Index records [record][head][rows][128] and a batch over them."""
+
+    def __init__(self, kind, t, new, lens, heads=1, q_heads=4, k=8, first=0, last=0, seed=1, spare=3,
+                 tail=0, weights=True, uniform=None, data=None, per_head=False, q_pad=0):
+        g = torch.Generator().manual_seed(seed)
+        self.kind, self.t, self.heads, self.g, self.k = kind, t, heads, q_heads, k
+        self.first, self.last, self.uniform = first, last, uniform
+        self.new, self.lens = new, lens
+        R = len(new)
+        self.per = max(1, (max(lens) + t - 1) // t)
+        records = R * self.per * (heads if per_head else 1) + spare
+        shape = (records, heads, (t if kind == KEYS else ref.INDEX_ROWS[kind]), 128)
+        if data is None:
+            x = torch.randn(shape, generator=g)
+            if kind == BOUNDS:
+                x = torch.stack((x.amin(2), x.amax(2)), 2)
+            self.index = x.to(torch.bfloat16)
+        else:
+            self.index = data(shape, g)
+        ids = torch.randperm(records, generator=g)[:records - spare]
+        self.table = ids.view(R, heads if per_head else 1, self.per).int()
+        self.start = [0]
+        for n in new:
+            self.start.append(self.start[-1] + n)
+        self.total = self.start[-1] + tail
+        self.q = torch.randn((self.total, heads * q_heads * 128 + q_pad), generator=g).to(torch.bfloat16)
+        self.w = torch.randn((self.total, heads * q_heads), generator=g) + 0.3 if (
+            weights and kind == KEYS) else None
+        self.max_chunk = max(max(new), 1)
+        self.no_table = False
+
+    def descs(self):
+        x = self.index
+        records = x.shape[0] // (len(self.new) if self.no_table else 1)
+        self.x = hs.IndexDesc(self.kind, self.t, records, 2 * x.stride(0), 2 * x.stride(1),
+                              records * 2 * x.stride(0) if self.no_table else 0)
+        H = self.table.shape[1]
+        self.b = hs.BatchDesc(len(self.new), self.heads, self.total, self.max_chunk, self.per, self.t,
+                              H * self.per, self.per if H > 1 else 0)
+        self.d = hs.SelectDesc(self.g, self.k, self.first, self.last, self.q.stride(0))
+
+    def device(self, ws=None):
+        self.descs()
+        dev = lambda x: None if x is None else x.cuda()  # noqa: E731
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+        n = hs.hisparse_select_workspace_bytes(self.x, self.b, self.d)
+        assert n > 0
+        n = ws(n) if ws else n
+        shape = (self.total, self.heads, self.k)
+        qpad = 1 if self.q.stride(0) % 2 else 0   # odd strides: start at an odd element too
+        q = torch.zeros(self.q.numel() + qpad, dtype=torch.bfloat16, device="cuda")
+        q[qpad:] = self.q.flatten().cuda()
+        self.dv = dict(index=dev(self.index), table=None if self.no_table else dev(self.table),
+                       start=None if self.uniform else ints(self.start),
+                       lens=ints(self.lens), q=q[qpad:], w=dev(self.w),
+                       sel=torch.full(shape, MARK, dtype=torch.int32, device="cuda"),
+                       rec=torch.full(shape, MARK, dtype=torch.int32, device="cuda"),
+                       slen=torch.full((self.total,), MARK, dtype=torch.int32, device="cuda")
+                       if self.last else None,
+                       ws=torch.full((n,), 0xEE, dtype=torch.uint8, device="cuda"))
+
+    def call(self, stream=None, **kw):
+        d = dict(self.dv, **kw)
+        hs.hisparse_select_records(self.x, self.b, self.d, d["index"], d["table"], d["start"],
+                                   d["lens"], d["q"], d["w"], d["sel"], d["rec"], d["slen"], d["ws"],
+                                   d["ws"].numel(), stream or torch.cuda.current_stream())
+
+    def expected(self, rows=None):
+        """{row: [per head: list]}, records likewise, {row: length}."""
+        sel, rec, slen = {}, {}, {}
+        per = 1 if self.kind == KEYS else self.t
+        records = self.x.num_records
+        for r in range(len(self.new)):
+            begin, n, length = ref.request_rows(None if self.uniform else self.start, self.lens, r,
+                                                self.max_chunk, self.per * self.t, self.total)
+            for i in range(n):
+                row, p = begin + i, length - n + i
+                if rows is not None and row not in rows:
+                    continue
+                seen = 0 if p < 0 else p // per + 1
+                sel[row], rec[row] = [], []
+                for h in range(self.heads):
+                    if self.no_table:
+                        tab = torch.arange(self.per) + r * records
+                        ok_rec = torch.ones(self.per, dtype=torch.bool)
+                    else:
+                        tab = self.table[r, h if self.table.shape[1] > 1 else 0].long()
+                        ok_rec = (tab >= 0) & (tab < records)
+                    safe = torch.where(ok_rec, tab, 0)
+                    x = self.index[safe, h]
+                    base = tab - r * records if self.no_table else tab
+                    if self.kind == KEYS:
+                        x, ok = x.reshape(-1, 1, 128), ok_rec.repeat_interleave(self.t)
+                        ids = (base[:, None] * self.t + torch.arange(self.t)).flatten()
+                    else:
+                        ok, ids = ok_rec, base
+                    hh = slice(h * self.g, (h + 1) * self.g)
+                    q = self.q[row, :self.heads * self.g * 128].view(-1, 128)[hh]
+                    w = None if self.w is None else self.w[row, hh]
+                    out = ref.select_row(self.kind, q, w, x[:seen], ok[:seen], self.k, self.first,
+                                         self.last)
+                    sel[row].append(out)
+                    rec[row].append([ids[j].item() if j >= 0 else -1 for j in out])
+                K = min(self.k, seen)
+                slen[row] = (K - 1) * per + p % per + 1 if K else 0
+        return sel, rec, slen
+
+    def compare(self, rows=None):
+        sel, rec, slen = self.expected(rows)
+        got, got_rec = self.dv["sel"].cpu(), self.dv["rec"].cpu()
+        for row in sel:
+            for h in range(self.heads):
+                a, b = got[row, h].tolist(), sel[row][h]
+                assert a == b, (row, h, sorted(set(a) ^ set(b))[:20])
+                assert got_rec[row, h].tolist() == rec[row][h], (row, h)
+            if self.last:
+                assert self.dv["slen"][row].item() == slen[row], row
+        if rows is None:
+            dead = [r for r in range(self.total) if r not in sel]
+            assert bool((got[dead] == MARK).all()) and bool((got_rec[dead] == MARK).all())
+            if self.last and dead:
+                assert bool((self.dv["slen"].cpu()[dead] == MARK).all())
+
+    def check(self, ws=None, rows=None):
+        self.device(ws)
+        self.call()
+        self.compare(rows)
+        return self
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("t", [1, 4, 64])
+@pytest.mark.parametrize("first,last", [(0, 0), (1, 2), (0, 1), (3, 0)])
+def test_ragged_batches(kind, t, first, last):
+    scale = 1 if kind == KEYS else t
+    lens = [0, 1, 7 * scale, 8 * scale, 9 * scale, 40 * scale + 1, 333 * scale, 70 * scale - 1]
+    new = [0, 1, 5, 2, 9, 3, 11, 1]
+    Case(kind, t, new, lens, heads=2, k=8, first=first, last=last, tail=5).check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("q_heads", [1, 3, 16, 17, 32, 40, 64, 65, 128])
+def test_query_heads(kind, q_heads):
+    t = 16
+    n = 700 if kind == KEYS else 700 * t
+    Case(kind, t, [3, 1], [n, n - 5 * t + 1], heads=2, q_heads=q_heads, k=33, seed=q_heads,
+         weights=q_heads != 32).check()
+    if kind == MEANS and q_heads == 128:
+        Case(kind, t, [1], [n], q_heads=256, k=20).check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("k", [1, 2, 255, 1024, 2048, 4096])
+def test_numbers_chosen(kind, k):
+    t = 4
+    for cand in (k - 1, k, k + 1, 2 * k + 3, 5000):
+        n = max(1, cand) * (1 if kind == KEYS else t)
+        Case(kind, t, [2], [n], k=k, last=1, q_heads=16, seed=k + cand).check()
+    Case(kind, t, [1], [20000], k=k, first=k // 2, last=k - k // 2, seed=3).check()  # all forced
+
+
+@pytest.mark.parametrize("kind,cand,q_heads", [(KEYS, 33000, 64), (KEYS, 300001, 8), (BOUNDS, 40000, 4),
+                                               (MEANS, 131072, 2)])
+def test_long_caches(kind, cand, q_heads):
+    t = 64 if kind == KEYS else 1
+    Case(kind, t, [1], [cand], q_heads=q_heads, k=2048, seed=cand).check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_chunks_and_uniform_batches(kind):
+    t = 8
+    n = 900 if kind == KEYS else 900 * t
+    Case(kind, t, [70], [n], k=64, last=2, first=1, q_heads=8).check()
+    Case(kind, t, [1] * 37, [(53 * i) % n + 1 for i in range(37)], k=50, uniform=True, heads=2).check()
+    Case(kind, t, [6] * 5, [n, 3, 6, n - 1, 7], k=16, last=1, uniform=True).check()
+    # more rows than chunks: requests of a padded batch
+    Case(kind, t, [6] * 5, [n, 3, 6, n - 1, 7], k=16, last=1, uniform=True, tail=9).check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_padding(kind):
+    t = 4
+    for seed in range(4):
+        rng = random.Random(seed)
+        c = Case(kind, t, [5, 2, 1], [150, 131, 33 * t], k=20, first=2, last=2, heads=2, seed=seed,
+                 per_head=seed % 2 == 1)
+        for r in range(3):
+            for h in range(c.table.shape[1]):
+                for _ in range(rng.choice((1, 12, 25))):
+                    c.table[r, h, rng.randrange(c.per)] = rng.choice((-1, c.index.shape[0], 2 ** 31 - 1))
+        if seed > 1:  # the newest record, and the first
+            c.table[:, :, (150 - 1) // t] = -1
+            c.table[:, :, 0] = -5
+        c.check()
+    c = Case(kind, t, [2], [400], k=7, last=1)
+    c.table[:] = -1
+    c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_without_a_table(kind):
+    c = Case(kind, 4, [3, 2], [301, 90], k=9, last=1, heads=2, spare=0)
+    c.no_table = True
+    c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_strides_of_queries(kind):
+    for pad in (1, 2, 7, 128):
+        Case(kind, 4, [3, 2], [301, 90], k=9, heads=2, q_pad=pad).check()
+
+
+def small_whole(lo, hi, zeros=0.0):
+    def make(shape, g):
+        x = torch.randint(lo, hi + 1, shape, generator=g).float()
+        if zeros:
+            x[torch.rand(shape, generator=g) < zeros] = 0.0
+        return x.to(torch.bfloat16)
+    return make
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("cand", [300, 5000])
+def test_equal_scores_go_to_the_lower_position(kind, cand):
+    for zeros, k in ((0.97, 40), (0.995, 7), (0.999, 200)):
+        c = Case(kind, 1, [2], [cand], k=k, q_heads=2, data=small_whole(-1, 1, zeros), last=1,
+                 weights=False)
+        c.q = torch.randint(-1, 2, c.q.shape, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+        c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_thousands_of_equal_rows(kind):
+    """More candidates within the error bound than are kept at once: the same row again and again, with a few
+    better and worse ones between."""
+    def same(shape, g):
+        x = torch.randint(-3, 4, (1, 1, *shape[2:]), generator=g).float().expand(shape).clone()
+        if kind == KEYS:
+            x[:] = x[:, :, :1]
+        odd = torch.randperm(shape[0], generator=g)[:40]
+        x[odd] = torch.randint(-3, 4, x[odd].shape, generator=g).float()
+        return x.to(torch.bfloat16)
+    for cand, k in ((1500, 30), (6000, 2500), (6000, 20), (6000, 4096)):
+        c = Case(kind, 1 if kind != KEYS else 2, [1, 1], [cand, cand - 77], k=k, q_heads=3, data=same,
+                 weights=False)
+        c.q = torch.randint(-2, 3, c.q.shape, generator=torch.Generator().manual_seed(k)).to(torch.bfloat16)
+        c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_zero_queries_and_zero_rows(kind):
+    c = Case(kind, 4, [2], [4000 * (1 if kind == KEYS else 4)], k=100, last=1)
+    c.q[0] = 0
+    c.check()
+    z = Case(kind, 4, [2], [3000 * (1 if kind == KEYS else 4)], k=100, data=lambda s, g: torch.zeros(
+        s, dtype=torch.bfloat16))
+    z.check()
+    if kind == KEYS:
+        c = Case(kind, 4, [2], [900], k=100)
+        c.w[:] = 0
+        c.check()
+        c = Case(kind, 4, [2], [900], k=100)   # every score is negative or 0
+        c.w = -c.w.abs()
+        c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("scale_q,scale_x", [(1e-30, 1e-30), (1e30, 1e20), (1e-38, 1.0), (1.0, 1e-39),
+                                             (1e15, 1e-18)])
+def test_numbers_of_both_ends_of_the_range(kind, scale_q, scale_x):
+    """Products, squares and sums that leave the range of fp32; all are fine in 64 bits."""
+    def data(shape, g):
+        x = torch.randn(shape, generator=g) * scale_x
+        if kind == BOUNDS:
+            x = torch.stack((x.amin(2), x.amax(2)), 2)
+        return x.to(torch.bfloat16)
+    c = Case(kind, 1, [2], [700], k=50, q_heads=3, data=data)
+    c.q = (c.q.float() * scale_q).to(torch.bfloat16)
+    c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_outliers(kind):
+    """One row far above the others: the first division of the scores' range puts all others in one bin."""
+    def data(shape, g):
+        x = torch.randn(shape, generator=g)
+        if kind == BOUNDS:
+            x = torch.stack((x.amin(2), x.amax(2)), 2)
+        x[shape[0] // 2] *= 30000.0
+        x[shape[0] // 3] *= -1e8
+        return x.to(torch.bfloat16)
+    for k in (3, 300):
+        Case(kind, 1, [2], [9000], k=k, q_heads=8, data=data, seed=k).check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_rows_that_are_not_seen_have_no_influence(kind):
+    t = 16
+    new, lens = [3, 1, 2], [200, 150, 333]
+    clean = Case(kind, t, new, lens, k=5, heads=2)
+    for value in (math.nan, math.inf, -math.inf, 3e38):
+        c = Case(kind, t, new, lens, k=5, heads=2)
+        c.table[1, 0, 2] = clean.table[1, 0, 2] = -1
+        used = torch.zeros(c.index.shape[0], dtype=torch.bool)
+        for r, n in enumerate(lens):
+            tab = c.table[r, 0, :(n + t - 1) // t].long()
+            used[tab[tab >= 0]] = True
+            if kind == KEYS and n % t:
+                c.index[tab[-1], :, n % t:] = value
+        c.index[~used] = value
+        c.device()
+        c.call()
+        clean.check()
+        assert torch.equal(c.dv["sel"], clean.dv["sel"])
+
+
+def test_nan_and_infinities_that_are_seen():
+    """A NaN score ranks above everything, the lower position first; an infinity by its sign."""
+    for kind in (KEYS, MEANS):
+        c = Case(kind, 1, [2], [400], k=6, q_heads=2, weights=False)
+        c.q = c.q.abs()
+        tab = c.table[0, 0].long()
+        x = c.index[tab, 0, 0]
+        x[100, 5] = x[300, 7] = math.nan
+        x[200, 0] = x[201, 0] = math.inf
+        x[50, 0] = -math.inf
+        x[60, 0], x[60, 1] = math.inf, -math.inf
+        c.index[tab, 0, 0] = x
+        c.check()
+        for j in (100, 300, 60):
+            assert j in c.dv["sel"][0, 0].tolist()
+    c = Case(KEYS, 1, [1], [400], k=6, q_heads=2)
+    c.w[0, 1] = math.nan                       # every score is NaN
+    c.check()
+    assert c.dv["sel"][0, 0].tolist() == list(range(6))
+    c = Case(KEYS, 1, [1], [400], k=6, q_heads=2)
+    c.q[0, 3] = math.inf
+    c.check()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_small_workspaces_take_more_steps(kind):
+    c = Case(kind, 4, [13, 1, 6, 0, 9], [800, 333, 91, 7, 500], k=12, heads=2, last=1, first=1, tail=3)
+    c.check()
+    whole = c.dv["sel"].clone()
+    for rows in (4, 5, 11):
+        c.check(ws=lambda n: (n // c.total + 1) * rows + 64)
+        assert torch.equal(c.dv["sel"], whole)
+    with pytest.raises(hs.HisparseError):
+        c.device(ws=lambda n: n // c.total // 2)
+        c.call()
+
+
+def test_a_workspace_of_a_larger_batch_and_no_records():
+    c = Case(KEYS, 16, [2, 3], [500, 60], k=20, last=1)
+    c.device(ws=lambda n: 5 * n + 256)
+    c.call(rec=None, slen=None)
+    c.dv["rec"], keep = None, c.dv["rec"]
+    sel, _, _ = c.expected()
+    for row in sel:
+        assert c.dv["sel"][row, 0].tolist() == sel[row][0]
+    assert bool((keep == MARK).all())
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_captured_and_replayed(kind):
+    """Other lengths, queries and tables in one graph, beside eager calls of another batch."""
+    t = 4
+    c = Case(kind, t, [2, 1, 4], [2000, 1, 700], k=30, last=1, heads=2)
+    other = Case(kind, t, [3], [900], k=11, heads=2)
+    c.device()
+    other.device()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        c.call()
+    rng = random.Random(3)
+    for seed in range(4):
+        c.new = [rng.randint(0, 4) for _ in range(3)]
+        c.start = [0, c.new[0], c.new[0] + c.new[1], sum(c.new)] if sum(c.new) <= c.total else [0, 1, 1, 5]
+        c.new = [b - a for a, b in zip(c.start, c.start[1:])]
+        c.lens = [rng.randint(0, 2000) for _ in range(3)]
+        c.q = randn(c.q.shape, 50 + seed)
+        c.table = c.table.roll(1, -1)
+        dv = c.dv
+        dv["start"].copy_(torch.tensor(c.start, dtype=torch.int32))
+        dv["lens"].copy_(torch.tensor(c.lens, dtype=torch.int32))
+        dv["q"].copy_(c.q.flatten())
+        dv["table"].copy_(c.table)
+        for x in ("sel", "rec", "slen"):
+            dv[x].fill_(MARK)
+        torch.cuda.synchronize()
+        g.replay()
+        other.call()
+        torch.cuda.synchronize()
+        c.compare()
+        other.compare()
+
+
+def test_starts_that_do_not_ascend_stay_in_bounds():
+    """What the rows hold is unspecified; nothing outside the arrays is touched."""
+    for kind in (KEYS, BOUNDS, MEANS):
+        c = Case(kind, 4, [5, 5, 5], [300, 200, 100], k=8, last=1)
+        c.device()
+        room = torch.full((c.total + 4, 1, 8), MARK, dtype=torch.int32, device="cuda")
+        c.dv["start"].copy_(torch.tensor([9, 2, 14, -3], dtype=torch.int32))
+        c.call(sel=room[2:-2])
+        torch.cuda.synchronize()
+        assert bool((room[:2] == MARK).all()) and bool((room[-2:] == MARK).all())

@@ -1,0 +1,230 @@
+"""hisparse_summarize_records against 64-bit arithmetic over what the records stand for.
+
+Bounds are values of the keys: exact. Means: fp32 sums of n values in any order are off by at most n 2^-24
+of the sum of magnitudes, the quotient by 2^-24 of itself, the result by half a bf16 step, 2^-8 of it."""
+import math
+
+import pytest
+import torch
+
+import step_reference as ref
+import token_reference as tok
+from paper_2608_07009_amd import hisparse as hs
+
+pytestmark = pytest.mark.gpu
+G, BF, F8 = tok.GROUPED, tok.BF16, tok.FP8
+MARK = 0x5A5A
+
+
+class Pool:
+    """Records [record][head] whose tokens hold rows, in a random order of requests' tables."""
+
+    def __init__(self, type_, t, heads, records, seed, k=None):
+        g = torch.Generator().manual_seed(seed)
+        self.t, self.heads, self.type = t, heads, type_
+        n = records * t
+        k = torch.randn((n, heads, 128), generator=g) * torch.exp2(
+            torch.randint(-6, 6, (n, heads, 1), generator=g).float()) if k is None else k
+        self.k = k.to(torch.bfloat16)
+        v = torch.randn((n, heads, 128), generator=g).to(torch.bfloat16)
+        R = hs.hisparse_kv_record_bytes(G, type_, t)
+        self.pool = torch.full((records, heads, R), 0xA5, dtype=torch.uint8, device="cuda")
+        self.desc = hs.KvDesc(G, type_, t, R, records, heads * R, R, 0)
+        hs.hisparse_write_tokens(self.desc, heads, n, self.k.cuda(), heads * 128, v.cuda(),
+                                 heads * 128, None, self.pool, torch.cuda.current_stream())
+        stored = tok.stored(G, self.k, v, type_)[0]
+        self.rows = stored.view(records, t, heads, 128).transpose(1, 2)  # [record][head][t][128]
+
+
+def index_for(kind, pool, extra=0):
+    records = pool.desc.num_records
+    buf = torch.full((records, pool.heads, ref.INDEX_ROWS[kind] * 128 + extra), MARK,
+                     dtype=torch.int16, device="cuda")
+    return buf, hs.IndexDesc(kind, pool.t, records, 2 * buf.stride(0), 2 * buf.stride(1), 0)
+
+
+def expected(kind, pool, start, lens, table, max_chunk, total, num_records=None):
+    """{(record, head): (rows, tolerance)} of what has to be written."""
+    out = {}
+    R, t = len(table), pool.t
+    for r in range(R):
+        begin, n, length = ref.request_rows(start, lens, r, max_chunk, len(table[r]) * t, total)
+        if n == 0 or length == 0:
+            continue
+        for j in range(max(length - n, 0) // t, (length + t - 1) // t):
+            rec = table[r][j]
+            if not 0 <= rec < (num_records or pool.desc.num_records):
+                continue
+            c = min(t, length - j * t)
+            for h in range(pool.heads):
+                x = pool.rows[rec, h, :c]
+                if kind == ref.BOUNDS:
+                    out[rec, h] = torch.stack((x.amin(0), x.amax(0))), 0.0
+                else:
+                    m = x.mean(0)
+                    out[rec, h] = m[None], (m.abs() * (2.0 ** -8 + 2.0 ** -23) +
+                                            x.abs().mean(0) * c * 2.0 ** -24)[None]
+    return out
+
+
+def check(kind, pool, buf, want):
+    got = buf.cpu()
+    w = ref.INDEX_ROWS[kind] * 128
+    for (rec, h), (rows, tol) in want.items():
+        x = got[rec, h, :w].view(torch.bfloat16).double().view(-1, 128)
+        same = (x == rows) | (torch.isnan(x) & torch.isnan(rows))
+        assert bool((same | ((x - rows).abs() <= tol)).all()), (rec, h)
+        assert bool((got[rec, h, w:] == MARK).all())
+        got[rec, h] = MARK
+    assert bool((got == MARK).all()), "a record that holds no new token was written"
+
+
+def run(kind, pool, start, lens, table, max_chunk, total, extra=0, batch=None):
+    buf, desc = index_for(kind, pool, extra)
+    tab = torch.tensor(table, dtype=torch.int32, device="cuda")
+    b = batch or hs.BatchDesc(len(table), pool.heads, total, max_chunk, tab.shape[1], pool.t,
+                              tab.stride(0), 0)
+    dev = lambda x: None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    hs.hisparse_summarize_records(pool.desc, desc, b, pool.pool, tab, dev(start), dev(lens), buf,
+                                  torch.cuda.current_stream())
+    check(kind, pool, buf, expected(kind, pool, start, lens, table, max_chunk, total))
+
+
+def tables(pool, per, requests, seed):
+    ids = torch.randperm(pool.desc.num_records, generator=torch.Generator().manual_seed(seed))
+    return ids[:requests * per].view(requests, per).tolist()
+
+
+@pytest.mark.parametrize("kind", [ref.BOUNDS, ref.MEANS])
+@pytest.mark.parametrize("type_", [BF, F8])
+@pytest.mark.parametrize("t", [1, 2, 4, 16, 64, 256])
+def test_ragged_batches(kind, type_, t):
+    heads, per = 3, 5
+    pool = Pool(type_, t, heads, 4 * per + 2, t)
+    table = tables(pool, per, 4, 1)
+    top = per * t
+    for new, lens in (([1, 1, 1, 1], [1, t, min(t + 1, top), top]),
+                      ([0, top, 1, t], [top, top, min(2 * t, top), top - t // 2]),
+                      ([t // 2 + 1, 3, 0, 2], [t // 2 + 1, 3, 0, 2]),
+                      ([5, 1, 1, 1], [3, 0, 1, top])):  # more new tokens than cached ones; none cached
+        start = [0]
+        for n in new:
+            start.append(start[-1] + n)
+        run(kind, pool, start, lens, table, max(new + [1]), start[-1] + 4, extra=8)
+
+
+@pytest.mark.parametrize("kind,type_", [(ref.BOUNDS, BF), (ref.MEANS, F8)])
+def test_uniform_chunks_and_no_lengths(kind, type_):
+    pool = Pool(type_, 16, 2, 21, 3)
+    table = tables(pool, 7, 3, 2)
+    run(kind, pool, None, None, table, 40, 120)
+    run(kind, pool, None, [112, 17, 5], table, 3, 9)
+    run(kind, pool, None, [112, 17, 5], table, 1, 3)
+    run(kind, pool, [0, 2, 2, 50], None, table, 16, 50)  # the last chunk is held to 16
+
+
+def test_padding_and_identity_tables():
+    pool = Pool(BF, 4, 2, 30, 4)
+    table = tables(pool, 6, 4, 3)
+    table[0][2], table[1][0], table[3][5] = -1, 30, 1 << 30
+    for kind in (ref.BOUNDS, ref.MEANS):
+        run(kind, pool, [0, 24, 48, 72, 96], [24, 23, 21, 24], table, 24, 96)
+        # an index with fewer records than the pool: what it has no place for is left out
+        buf, desc = index_for(kind, pool)
+        desc.num_records = 17
+        tab = torch.tensor(table, dtype=torch.int32, device="cuda")
+        b = hs.BatchDesc(4, 2, 96, 24, 6, 4, 6, 0)
+        hs.hisparse_summarize_records(pool.desc, desc, b, pool.pool, tab, None, None, buf,
+                                      torch.cuda.current_stream())
+        check(kind, pool, buf, expected(kind, pool, None, None, table, 24, 96, 17))
+        # no table: request q's records are its own, one part of pool and index behind the other
+        kv = hs.KvDesc(G, BF, 4, pool.desc.record_bytes, 15, pool.desc.record_stride,
+                       pool.desc.head_stride, 15 * pool.desc.record_stride)
+        buf, desc = index_for(kind, pool)
+        desc.num_records, desc.request_stride = 15, 15 * desc.record_stride
+        b = hs.BatchDesc(2, 2, 62, 31, 15, 4, 0, 0)
+        lens = torch.tensor([33, 60], dtype=torch.int32, device="cuda")
+        hs.hisparse_summarize_records(kv, desc, b, pool.pool, None, None, lens, buf,
+                                      torch.cuda.current_stream())
+        ident = [list(range(15)), list(range(15, 30))]
+        check(kind, pool, buf, expected(kind, pool, None, [33, 60], ident, 31, 62))
+
+
+def test_tables_of_each_head():
+    pool = Pool(BF, 16, 2, 12, 6)
+    ids = torch.randperm(12, generator=torch.Generator().manual_seed(1)).view(2, 2, 3)  # [req][head]
+    for kind in (ref.BOUNDS, ref.MEANS):
+        buf, desc = index_for(kind, pool)
+        tab = ids.int().cuda()
+        b = hs.BatchDesc(2, 2, 40, 20, 3, 16, 6, 3)
+        hs.hisparse_summarize_records(pool.desc, desc, b, pool.pool, tab, None, None, buf,
+                                      torch.cuda.current_stream())
+        want = {}
+        for h in range(2):
+            e = expected(kind, pool, None, None, ids[:, h].tolist(), 20, 40)
+            want.update({k: v for k, v in e.items() if k[1] == h})
+        check(kind, pool, buf, want)
+
+
+def test_extreme_keys():
+    """Infinities, NaN and numbers of both ends of the range; a NaN shows in its dim only."""
+    k = torch.zeros((8, 1, 128))
+    k[0, 0, 0], k[1, 0, 1], k[2, 0, 2] = math.inf, -math.inf, math.nan
+    k[3, 0, 3], k[4, 0, 3], k[5, 0, 4], k[6, 0, 5] = 3e38, 3e38, 1e-40, -0.0
+    for t in (4, 8):
+        pool = Pool(BF, t, 1, 8 // t, 1, k=k)
+        for kind in (ref.BOUNDS, ref.MEANS):
+            buf, desc = index_for(kind, pool)
+            n = 8 // t
+            b = hs.BatchDesc(1, 1, 8, 8, n, t, n, 0)
+            tab = torch.arange(n, dtype=torch.int32, device="cuda")
+            hs.hisparse_summarize_records(pool.desc, desc, b, pool.pool, tab, None, None, buf,
+                                          torch.cuda.current_stream())
+            got = buf.cpu().view(torch.bfloat16).double().view(n, -1, 128)
+            x = pool.rows[:, 0]
+            nan = torch.isnan(x).any(1)
+            if kind == ref.BOUNDS:
+                want = torch.stack((x.amin(1), x.amax(1)), 1)
+            else:
+                want = x.mean(1)[:, None]
+                want[x.sum(1)[:, None] > 3.41e38] = math.inf  # 6e38 passes fp32
+            assert torch.equal(torch.isnan(got), torch.isnan(want))
+            assert torch.equal(torch.isnan(got).any(1), nan | (torch.isnan(want).any(1)))
+            ok = ~torch.isnan(want)
+            assert bool(((got[ok] == want[ok]) |
+                         ((got[ok] - want[ok]).abs() <= 2.0 ** -8 * want[ok].abs() + 2.0 ** -133)).all())
+
+
+@pytest.mark.parametrize("requests,chunk", [(1, 3000), (300, 1), (257, 9)])
+def test_many_records(requests, chunk):
+    t, per = 16, max(2, (chunk + 15) // 16 + 1)
+    pool = Pool(F8, t, 1, requests * per, 8)
+    table = tables(pool, per, requests, 9)
+    lens = [min(per * t, chunk + (7 * r) % (per * t - chunk + 1)) for r in range(requests)]
+    for kind in (ref.BOUNDS, ref.MEANS):
+        run(kind, pool, list(range(0, requests * chunk + 1, chunk)), lens, table, chunk,
+            requests * chunk)
+
+
+def test_captured_and_replayed_on_another_stream():
+    pool = Pool(BF, 16, 2, 12, 2)
+    table = tables(pool, 6, 2, 4)
+    buf, desc = index_for(ref.BOUNDS, pool)
+    tab = torch.tensor(table, dtype=torch.int32, device="cuda")
+    start = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([5, 90], dtype=torch.int32, device="cuda")
+    b = hs.BatchDesc(2, 2, 64, 32, 6, 16, 6, 0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        hs.hisparse_summarize_records(pool.desc, desc, b, pool.pool, tab, start, lens, buf,
+                                      torch.cuda.current_stream())
+    for s, l in (([0, 1, 2], [17, 96]), ([0, 30, 30], [31, 2]), ([0, 32, 64], [96, 33])):
+        buf.fill_(MARK)
+        start.copy_(torch.tensor(s, dtype=torch.int32))
+        lens.copy_(torch.tensor(l, dtype=torch.int32))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        check(ref.BOUNDS, pool, buf, expected(ref.BOUNDS, pool, s, l, table, 32, 64))
