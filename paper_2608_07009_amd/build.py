@@ -16,7 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libhisparse.so")
 SOURCES = ["api.hip", "resolve.hip", "attention.hip", "tokens.hip", "chunk_attention.hip",
-           "plan_tokens.hip", "rotary.hip", "summarize.hip", "select.hip"]
+           "plan_tokens.hip", "rotary.hip", "summarize.hip", "select.hip", "select_choose.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 instructions stay off: only plain fp32 VALU code is generated.

@@ -1,0 +1,99 @@
+// Selection of records by a cheap score: what its scores (select.hip) and its choice (select_choose.hip)
+// share.
+#pragma once
+
+#include <math.h>
+
+#include "batch.h"
+
+namespace hisparse {
+
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef u32x4_t any_u32x4_t __attribute__((aligned(2)));  // queries may start at any element
+
+// What the scores of padding, and (by the choice) of chosen candidates, are marked with; scores that are
+// NaN are kNan.
+constexpr uint32_t kPad = 0xffffffffu, kWin = 0x7fffffffu, kNan = 0x7fc00000u;
+constexpr int kLongBins = 2048;       // of a long row's division
+constexpr int kPart = 16384;          // candidates of a long row's part
+constexpr int kRegisterRow = 32768;   // a longer row is long
+constexpr int kMaxParts = 1024;
+
+struct TileFacts {
+  float norm, least, most;  // largest norm of a tile's rows, its least and largest score
+};
+
+struct SelectArgs : BatchArgs {
+  const uint8_t* index;
+  const uint16_t* q;
+  const float* weights;
+  int32_t *sel, *records, *sel_len;
+  // of this step's rows, each [rows][heads]:
+  float* scores;       // [row_pad]
+  TileFacts* facts;    // [tiles]
+  // long rows:
+  uint32_t* hist;      // [kLongBins]; null: no row is long
+  int32_t* survivors;  // [row_pad], a part of kPart each
+  int32_t* part_count; // [parts]
+  float* bound;        // [3]: the error bound, the range of the scores
+  int64_t record_stride, head_stride, request_stride, num_records, q_stride;
+  int64_t row_pad;
+  int32_t row0, rows;     // this step's rows of new tokens
+  int32_t tiles, parts;   // of a row
+  int32_t tile_size;      // candidates of a tile (log2)
+  int32_t q_heads, top_k, first, last;
+  int32_t cand_shift;     // tokens of a candidate (log2)
+};
+
+// Chooses from the scores of the step's rows; `candidates`: the most that a row has.
+hipError_t launch_choose(const SelectArgs& a, int kind, int64_t candidates, hipStream_t stream);
+
+template <int KIND>
+struct IndexShape {
+  static constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
+  static constexpr int DIMS = KIND == HISPARSE_INDEX_BOUNDS ? 2 * kIndexDims : kIndexDims;
+};
+
+__device__ __forceinline__ float low_half(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float high_half(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+__device__ __forceinline__ float bf16_value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// Candidates that the new token at position p sees.
+__device__ __forceinline__ int seen_at(const SelectArgs& a, int p) {
+  return p < 0 ? 0 : (p >> a.cand_shift) + 1;
+}
+
+// Index row of candidate j of request q, kv head h; false if it is padding. record: what the caller
+// knows the candidate by.
+template <bool KEYS>
+__device__ __forceinline__ bool find_row(const SelectArgs& a, int q, int h, int j,
+                                         const uint8_t*& row, int& record) {
+  const int entry = KEYS ? j >> a.tpr_shift : j;
+  const int rec =
+      a.table ? a.table[q * a.table_request_stride + h * a.table_head_stride + entry] : entry;
+  if (rec < 0 || rec >= a.num_records) return false;
+  const int in = KEYS ? j & ((1 << a.tpr_shift) - 1) : 0;
+  row = a.index + q * a.request_stride + h * a.head_stride + (int64_t)rec * a.record_stride +
+        in * kIndexRowBytes;
+  record = KEYS ? (int)(((uint32_t)rec << a.tpr_shift) + in) : rec;
+  return true;
+}
+
+// Bounds and means: the sums over a kv head's queries of dim d, 64 bits. (neg is 0 for means.)
+template <int KIND>
+__device__ __forceinline__ void query_sums(const SelectArgs& a, int token, int h, int d, double& pos,
+                                           double& neg) {
+  const uint16_t* q =
+      a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + d;
+  pos = neg = 0.0;
+#pragma unroll 4
+  for (int e = 0; e < a.q_heads; ++e) {
+    const double v = bf16_value(q[e * kIndexDims]);
+    if (KIND == HISPARSE_INDEX_BOUNDS && v < 0.0) neg += v;
+    else pos += v;
+  }
+}
+
+}  // namespace hisparse
