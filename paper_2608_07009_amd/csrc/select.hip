@@ -6,6 +6,8 @@
 //
 // Products from bf16 MFMAs, 16 query rows by 16 candidates, sums in fp32. Which candidates these choose is
 // settled in select_choose.hip.
+#include <algorithm>
+
 #include "select.h"
 
 namespace hisparse {
@@ -14,8 +16,9 @@ namespace {
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
-constexpr int kScoreThreads = 256;
 constexpr int kRowPad = 256;          // a row of scores is a multiple of this
+// New tokens of a request from which waves have new tokens of their own.
+constexpr int kTeamChunk = 5;
 constexpr size_t kMostScoreBytes = (size_t)1 << 30;
 
 __device__ __forceinline__ uint16_t to_bf16(float x) {
@@ -27,18 +30,55 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
 template <int KIND>
 struct Shape : IndexShape<KIND> {
   using IndexShape<KIND>::KEYS;
-  static constexpr int STEPS = IndexShape<KIND>::DIMS / 32;  // MFMAs of 16 rows x 16 candidates
-  static constexpr int ROWS = KEYS ? 1 : 4;        // new tokens of a workgroup
+  using IndexShape<KIND>::DIMS;
+  static constexpr int STEPS = DIMS / 32;          // MFMAs of 16 rows x 16 candidates
+  static constexpr int PIECES = DIMS / 8;          // 16-byte pieces of an index row
   static constexpr int TILE = KEYS ? 1024 : 512;   // candidates of a workgroup
 };
 
+// Sum of the squares of eight bf16 values, and acc.
+__device__ __forceinline__ float squares(u32x4_t x, float acc) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t b = x[i];
+    const bf16x2_t y = __builtin_bit_cast(bf16x2_t, b);
+    acc = __builtin_amdgcn_fdot2_f32_bf16(y, y, acc, false);
+  }
+  return acc;
+}
+// x, or 0 if that is more, without a rounding or a look for signalling NaN: by its sign.
+__device__ __forceinline__ float positive(float x) {
+  return __int_as_float(max(__float_as_int(x), 0));
+}
+// Over the 16 lanes of a row, in all of them.
+template <int CTRL>
+__device__ __forceinline__ float moved(float x) {
+  return __int_as_float(lane_moved<CTRL>(__float_as_int(x)));
+}
+__device__ __forceinline__ float sum16(float x) {
+  x += moved<0x128>(x);
+  x += moved<0x124>(x);
+  x += moved<0x122>(x);
+  return x + moved<0x121>(x);
+}
+// The totals over the four rows of 16 lanes of v0 .. v3: that of v_r in row r.
+__device__ __forceinline__ float totals(float v0, float v1, float v2, float v3) {
+  auto halves = [](float x, float y) {  // x's halves added in the lower half, y's in the upper
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  };
+  const float x = halves(v0, v2), y = halves(v1, v3);
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // Bounds and means: the sums over the heads of a token, exact in 64 bits, as three bf16 parts (24 bits:
 // off by 2^-25 of the value). Row 4 i + part of the A operand, i the token; the fourth is zero.
-template <int KIND>
-__device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int tokens, int h,
+template <int KIND, int T>
+__device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int tokens, int rows, int h,
                                             uint16_t* s_a) {
   constexpr int DIMS = Shape<KIND>::DIMS, PITCH = DIMS + 8;
-  for (int x = threadIdx.x; x < 4 * kIndexDims; x += kScoreThreads) {
+  for (int x = threadIdx.x; x < rows * kIndexDims; x += T) {
     const int i = x / kIndexDims, d = x % kIndexDims;
     double pos = 0.0, neg = 0.0;
     if (i < tokens) query_sums<KIND>(a, token0 + i, h, d, pos, neg);
@@ -56,19 +96,175 @@ __device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int
   }
 }
 
-template <int KIND, int MT>
-__global__ __launch_bounds__(kScoreThreads) void score_kernel(SelectArgs a) {
+// What a wave scores: keys, NT new tokens of MT tiles of 16 heads each; the others, 4 MT new tokens, four of
+// three rows (and an empty one) to a tile.
+template <int KIND, int MT, int NT>
+struct Wave {
   using S = Shape<KIND>;
+  static constexpr bool KEYS = S::KEYS;
+  static constexpr int TILES = KEYS ? MT * NT : MT, TOKENS = KEYS ? NT : 4 * MT;
+  // Sums of a lane: keys, of four values at a time (see `totals`) that are four new tokens, or fewer and
+  // several 16 candidates; the others, of the new token 4 m + group.
+  static constexpr int SETS = KEYS ? (NT + 3) / 4 : MT;
+  static constexpr int SPAN = KEYS && NT < 4 ? 64 / NT : 16;  // candidates of a lane's new token at a time
+  bf16x8_t A[TILES][S::STEPS];
+  float w[KEYS ? TILES * 4 : 1];
+  float least[SETS], most[SETS];
+
+  __device__ __forceinline__ void start() {
+#pragma unroll
+    for (int i = 0; i < SETS; ++i) {
+      least[i] = INFINITY;
+      most[i] = -INFINITY;
+    }
+  }
+  // keys: the queries of tokens token0 .. of kv head h
+  __device__ __forceinline__ void load(const SelectArgs& a, int token0, int tokens, int h) {
+    const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int64_t token = token0 + n;
+      const uint16_t* q = a.q + token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + group * 8;
+      const float* wr = a.weights ? a.weights + (token * a.heads + h) * a.q_heads : nullptr;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int e = m * 16 + col;
+#pragma unroll
+        for (int k = 0; k < S::STEPS; ++k) {
+          u32x4_t x = {};
+          if (n < tokens && e < a.q_heads)
+            x = *reinterpret_cast<const any_u32x4_t*>(q + e * kIndexDims + k * 32);
+          A[n * MT + m][k] = __builtin_bit_cast(bf16x8_t, x);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int y = m * 16 + group * 4 + i;
+          w[(n * MT + m) * 4 + i] = n < tokens && y < a.q_heads ? (wr ? wr[y] : 1.f) : 0.f;
+        }
+      }
+    }
+  }
+  // the others: rows of s_a from token `first` of the workgroup's on
+  __device__ __forceinline__ void load(const uint16_t* s_a, int first) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int k = 0; k < S::STEPS; ++k)
+        A[m][k] = *reinterpret_cast<const bf16x8_t*>(
+            s_a + (first * 4 + m * 16 + (lane & 15)) * (S::DIMS + 8) + k * 32 + (lane >> 4) * 8);
+  }
+
+  // Scores of 16 candidates: keys, this lane's share of each new token's; the others, whole.
+  __device__ __forceinline__ void score(const u32x4_t (&x)[S::STEPS], float (&v)[KEYS ? NT : MT]) {
+    f32x4_t acc[TILES];
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{};
+#pragma unroll
+    for (int k = 0; k < S::STEPS; ++k)
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t][k], __builtin_bit_cast(bf16x8_t, x[k]),
+                                                         acc[t], 0, 0, 0);
+    if constexpr (KEYS) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        v[n] = 0.f;
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            v[n] += w[(n * MT + m) * 4 + i] * positive(acc[n * MT + m][i]);
+        asm volatile("" : "+v"(v[n]));  // here, and not where it is used: the accumulators are free
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        v[m] = acc[m][0] + acc[m][1] + acc[m][2];
+        asm volatile("" : "+v"(v[m]));
+      }
+    }
+  }
+
+  // A set's scores to memory: this lane's is candidate j's, of its new token's row.
+  __device__ __forceinline__ void put(float s, int set, float* row, int j, int end, bool valid, bool live) {
+    if (j >= end || !live) return;
+    if (s != s) s = __uint_as_float(kNan);
+    if (valid) {
+      least[set] = fminf(least[set], s);  // (NaN is passed over)
+      most[set] = fmaxf(most[set], s);
+    }
+    row[j] = valid ? s : __uint_as_float(kPad);
+  }
+  // The workgroup's new token (from the wave's first) that this lane has in a set.
+  __device__ __forceinline__ int token_of(int set) const {
+    const int row = (threadIdx.x & 63) >> 4;
+    if (!KEYS) return 4 * set + row;
+    return NT >= 4 ? 4 * set + row : NT == 2 ? row >> 1 : 0;
+  }
+  // Scores of 64 candidates base .., v[sub] of each 16, written down. out: row of the wave's first token;
+  // mask: which are not padding.
+  __device__ __forceinline__ void put64(const float (&v)[4][KEYS ? NT : MT], float* out, int64_t pitch,
+                                        int tokens, int base, int end, uint64_t mask) {
+    const int lane = threadIdx.x & 63, col = lane & 15;
+    auto one = [&](float s, int set, int at) {
+      const int t = token_of(set);
+      put(s, set, out + t * pitch, base + at, end, mask >> at & 1, t < tokens);
+    };
+    if constexpr (!KEYS) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub) one(v[sub][m], m, sub * 16 + col);
+    } else if constexpr (NT == 1) {
+      one(totals(v[0][0], v[1][0], v[2][0], v[3][0]), 0, lane);
+    } else if constexpr (NT == 2) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        one(totals(v[2 * x][0], v[2 * x + 1][0], v[2 * x][1], v[2 * x + 1][1]), 0, x * 32 + (lane & 31));
+    } else {
+#pragma unroll
+      for (int set = 0; set < SETS; ++set)
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub)
+          one(totals(v[sub][4 * set], v[sub][4 * set + 1], v[sub][4 * set + 2], v[sub][4 * set + 3]),
+              set, sub * 16 + col);
+    }
+  }
+};
+
+// The table's entry for candidate j of [0, end), as it is; j past the end has the last one's.
+template <bool KEYS>
+__device__ __forceinline__ int entry_of(const SelectArgs& a, const int32_t* table, int j, int end) {
+  j = min(j, end - 1);
+  const int e = KEYS ? j >> a.tpr_shift : j;
+  return table ? table[e] : e;
+}
+
+// ROWS new tokens of a workgroup (of one or more requests, one after the other), a tile of candidates.
+//
+// TEAM: the waves have new tokens of their own and the same candidates, 64 at a time by way of LDS, the next
+// 64 on their way in registers meanwhile. Otherwise, and where there are no more new tokens than one wave
+// has, each wave has a quarter of the candidates and loads them as operands.
+template <int KIND, int MT, int NT, int WAVES, bool TEAM, int OCCUPANCY>
+__global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs a) {
+  using S = Shape<KIND>;
+  using W = Wave<KIND, MT, NT>;
   constexpr bool KEYS = S::KEYS;
-  __shared__ uint32_t s_norm[4];
-  __shared__ float s_least[4][S::ROWS], s_most[4][S::ROWS];
-  __shared__ __align__(16) uint16_t s_a[KEYS ? 8 : 16 * (S::DIMS + 8)];
+  constexpr int T = 64 * WAVES, ROWS = TEAM ? WAVES * W::TOKENS : 1;
+  constexpr int LOADS = 64 * S::PIECES / T;  // of a thread, for 64 rows
+  constexpr int A_ROWS = KEYS ? 0 : MT * (TEAM ? WAVES : 1);  // tiles
+  constexpr int TILE_BYTES = 64 * S::DIMS * 2, A_BYTES = 16 * A_ROWS * (S::DIMS + 8) * 2;
+  __shared__ __align__(16) uint8_t s_mem[std::max(TEAM ? 2 * TILE_BYTES : 16, A_BYTES)];
+  __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
+  __shared__ float s_least[WAVES][W::TOKENS], s_most[WAVES][W::TOKENS];
   const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t block = blockIdx.x, rest = block / (uint32_t)a.tiles;
   const int kt = (int)(block - rest * (uint32_t)a.tiles);
   const int tile = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)tile * a.heads);
-  const int row0 = a.row0 + tile * S::ROWS, row1 = min(row0 + S::ROWS, a.row0 + a.rows);
+  const int row0 = a.row0 + tile * ROWS, row1 = min(row0 + ROWS, a.row0 + a.rows);
+#pragma unroll 1
   for (int t = row0; t < row1;) {
     const int q = request_at(a, t);
     const RequestRows r = rows_of(a, q);
@@ -79,147 +275,195 @@ __global__ __launch_bounds__(kScoreThreads) void score_kernel(SelectArgs a) {
     const int token0 = t, tokens = min(row1, r.begin + r.n) - t;
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
-    if (seen <= a.top_k || kt * S::TILE >= seen) continue;
-    bf16x8_t A[MT][S::STEPS];
-    float w[KEYS ? MT * 4 : 1];
+    const int first = kt * S::TILE, end = min(first + S::TILE, seen);
+    if (seen <= a.top_k || first >= seen) continue;
+    const bool team = TEAM && tokens > W::TOKENS;
+    const int mine = team ? wave * W::TOKENS : 0;      // this wave's first new token
+    const int live = min(tokens - mine, W::TOKENS);    // and how many it has (0 or less: none)
+    const int32_t* table =
+        a.table ? a.table + q * a.table_request_stride + h * a.table_head_stride : nullptr;
+    const uint8_t* index = a.index + q * a.request_stride + h * a.head_stride;
+    // Padding is loaded as record 0 is, and left out of everything.
+    auto there = [&](int entry, int j, int stop) {
+      return j < stop && entry >= 0 && entry < a.num_records;
+    };
+    auto row_of = [&](int entry, bool valid, int j) {
+      return index + (uint64_t)(uint32_t)(valid ? entry : 0) * (uint32_t)a.record_stride +
+             (KEYS ? (j & ((1 << a.tpr_shift) - 1)) * kIndexRowBytes : 0);
+    };
+    W wv;
+    wv.start();
     if constexpr (KEYS) {
-      const uint16_t* qrow = a.q + (int64_t)token0 * a.q_stride +
-                             (int64_t)h * a.q_heads * kIndexDims + group * 8;
-      const float* wrow = a.weights ? a.weights + ((int64_t)token0 * a.heads + h) * a.q_heads
-                                    : nullptr;
+      wv.load(a, token0 + mine, live, h);
+    } else {
+      __syncthreads();  // what the last segment kept here is read
+      linear_rows<KIND, T>(a, token0, tokens, 4 * A_ROWS, h, reinterpret_cast<uint16_t*>(s_mem));
+      __syncthreads();
+      wv.load(reinterpret_cast<const uint16_t*>(s_mem), mine);
+      if (TEAM) __syncthreads();
+    }
+    const int64_t pitch = a.heads * a.row_pad;
+    float* out = a.scores + ((int64_t)(token0 + mine - a.row0) * a.heads + h) * a.row_pad;
+    float norm = 0.f;  // the largest sum of squares; NaN stays (its bits are above infinity's)
+    uint32_t bits = 0;
+    auto larger = [&](float sq) {
+      norm = __uint_as_float(max(__float_as_uint(norm), __float_as_uint(sq)));
+    };
+    if (team) {
+      // thread t: piece t % PIECES of rows t / PIECES + i * (T / PIECES); piece p of row r lies in slot
+      // p ^ (r & 15), so that 16 rows' pieces p are in 16 slots of the banks
+      constexpr int P = S::PIECES;
+      const int piece = threadIdx.x % P, row_first = threadIdx.x / P;
+      int entry = entry_of<KEYS>(a, table, first + lane, end);  // of candidate base + lane, one step ahead
+      u32x4_t x[LOADS];
+      uint64_t mask;  // which of 64 candidates are not padding
+      auto fetch = [&](int base) {
+        mask = __ballot(there(entry, base + lane, end));
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int e = m * 16 + col;
-#pragma unroll
-        for (int k = 0; k < S::STEPS; ++k) {
-          u32x4_t x = {};
-          if (e < a.q_heads)
-            x = *reinterpret_cast<const any_u32x4_t*>(qrow + e * kIndexDims + k * 32);
-          A[m][k] = __builtin_bit_cast(bf16x8_t, x);
+        for (int i = 0; i < LOADS; ++i) {
+          const int row = row_first + i * (T / P), e = __shfl(entry, row);
+          x[i] = *reinterpret_cast<const u32x4_t*>(row_of(e, mask >> row & 1, base + row) + piece * 16);
         }
+        entry = entry_of<KEYS>(a, table, base + 64 + lane, end);
+      };
+      auto store = [&](uint8_t* buf) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int y = m * 16 + group * 4 + i;
-          w[m * 4 + i] = y < a.q_heads ? (wrow ? wrow[y] : 1.f) : 0.f;
+        for (int i = 0; i < LOADS; ++i) {
+          const int row = row_first + i * (T / P);
+          const bool valid = mask >> row & 1;
+          *reinterpret_cast<u32x4_t*>(buf + row * (P * 16) + ((piece ^ (row & 15)) << 4)) = x[i];
+          bits |= valid ? (x[i][0] | x[i][1] | x[i][2] | x[i][3]) & 0x7fff7fffu : 0;
+          float sq = sum16(squares(x[i], 0.f));
+          if (P == 32) sq += __shfl_xor(sq, 16);
+          larger(valid ? sq : 0.f);
+          asm volatile("" : "+v"(bits), "+v"(norm));
         }
+      };
+      fetch(first);
+      store(s_mem);
+      __syncthreads();
+      int cur = 0;
+#pragma unroll 1
+      for (int base = first; base < end; base += 64) {
+        const uint64_t now = mask;
+        if (base + 64 < end) fetch(base + 64);
+        if (live > 0) {
+          float v[4][KEYS ? NT : MT];
+#pragma unroll
+          for (int sub = 0; sub < 4; ++sub) {
+            u32x4_t y[S::STEPS];
+            const uint8_t* row = s_mem + cur * TILE_BYTES + (sub * 16 + col) * (P * 16);
+#pragma unroll
+            for (int k = 0; k < S::STEPS; ++k)
+              y[k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
+            wv.score(y, v[sub]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          wv.put64(v, out, pitch, live, base, end, now);
+        }
+        cur ^= 1;
+        if (base + 64 < end) store(s_mem + cur * TILE_BYTES);
+        __syncthreads();
       }
     } else {
-      __syncthreads();  // the last segment's operands are read
-      linear_rows<KIND>(a, token0, tokens, h, s_a);
-      __syncthreads();
+      const int from = first + wave * (S::TILE / WAVES), to = min(from + S::TILE / WAVES, end);
+      u32x4_t x[2][S::STEPS];  // two times 16 candidates, the next ones on their way
+      int entry = 0, next = 0;  // of candidate base + lane, and of the next step's
+      auto fetch = [&](u32x4_t (&y)[S::STEPS], int entries, int base, int sub) {
+        const int j = base + sub * 16 + col, e = __shfl(entries, sub * 16 + col);
+        const uint8_t* row = row_of(e, there(e, j, to), min(j, to - 1)) + group * 16;
 #pragma unroll
-      for (int k = 0; k < S::STEPS; ++k)
-        A[0][k] = *reinterpret_cast<const bf16x8_t*>(s_a + col * (S::DIMS + 8) + k * 32 + group * 8);
-    }
-    float norm = 0.f;      // the largest sum of squares; NaN stays (its bits are above infinity's)
-    uint32_t bits = 0;
-    float least = INFINITY, most = -INFINITY;  // of this lane's row
-    const int64_t out = ((int64_t)(token0 - a.row0) * a.heads + h) * a.row_pad;
-    for (int base = kt * S::TILE + wave * (S::TILE / 4), end = min(base + S::TILE / 4, seen);
-         base < end; base += 64) {
-      u32x4_t x[4][S::STEPS];
-      bool valid[4];
-#pragma unroll
-      for (int sub = 0; sub < 4; ++sub) {
-        const int j = base + sub * 16 + col;
-        const uint8_t* row = nullptr;
-        int record;
-        valid[sub] = j < end && find_row<KEYS>(a, q, h, j, row, record);
-#pragma unroll
-        for (int k = 0; k < S::STEPS; ++k) {
-          x[sub][k] = u32x4_t{};
-          if (valid[sub]) x[sub][k] = *reinterpret_cast<const u32x4_t*>(row + k * 64 + group * 16);
-        }
+        for (int k = 0; k < S::STEPS; ++k) y[k] = *reinterpret_cast<const u32x4_t*>(row + k * 64);
+      };
+      if (from < to) {
+        entry = entry_of<KEYS>(a, table, from + lane, to);
+        next = entry_of<KEYS>(a, table, from + 64 + lane, to);
+        fetch(x[0], entry, from, 0);
+        fetch(x[1], entry, from, 1);
       }
-      float v[4];
+#pragma unroll 1
+      for (int base = from; base < to; base += 64) {
+        const uint64_t mask = __ballot(there(entry, base + lane, to));
+        const int after = entry_of<KEYS>(a, table, base + 128 + lane, to);
+        float v[4][KEYS ? NT : MT];
 #pragma unroll
-      for (int sub = 0; sub < 4; ++sub) {
-        float sq = 0.f, sum = 0.f;
+        for (int sub = 0; sub < 4; ++sub) {
+          float sq = 0.f;
+          uint32_t any = 0;
 #pragma unroll
-        for (int k = 0; k < S::STEPS; ++k)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t b = x[sub][k][i];
-            bits |= b & 0x7fff7fffu;
-            sq += low_half(b) * low_half(b) + high_half(b) * high_half(b);
+          for (int k = 0; k < S::STEPS; ++k) {
+            const u32x4_t y = x[sub & 1][k];
+            any |= (y[0] | y[1] | y[2] | y[3]) & 0x7fff7fffu;
+            sq = squares(y, sq);
           }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          f32x4_t acc = {};
-#pragma unroll
-          for (int k = 0; k < S::STEPS; ++k)
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                A[m][k], __builtin_bit_cast(bf16x8_t, x[sub][k]), acc, 0, 0, 0);
-          if constexpr (KEYS) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum += w[m * 4 + i] * fmaxf(acc[i], 0.f);
-          } else {
-            sum = acc[0] + acc[1] + acc[2];
-          }
+          sq += __shfl_xor(sq, 16);
+          sq += __shfl_xor(sq, 32);
+          const bool valid = mask >> (sub * 16 + col) & 1;
+          larger(valid ? sq : 0.f);
+          bits |= valid ? any : 0;
+          asm volatile("" : "+v"(bits), "+v"(norm));  // now: the operands' registers are loaded again
+          wv.score(x[sub & 1], v[sub]);
+          __builtin_amdgcn_sched_barrier(0);
+          // (past the end: the last candidate again)
+          if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);
+          else fetch(x[sub & 1], next, base + 64, sub - 2);
         }
-        if constexpr (KEYS) {
-          sum += __shfl_xor(sum, 16);
-          sum += __shfl_xor(sum, 32);
-        }
-        sq += __shfl_xor(sq, 16);
-        sq += __shfl_xor(sq, 32);
-        norm = __uint_as_float(max(__float_as_uint(norm), __float_as_uint(sq)));
-        if (sum != sum) sum = __uint_as_float(kNan);
-        v[sub] = valid[sub] ? sum : __uint_as_float(kPad);
-      }
-      if constexpr (KEYS) {
-        const float s = group == 0 ? v[0] : group == 1 ? v[1] : group == 2 ? v[2] : v[3];
-        if (base + lane < end) {
-          a.scores[out + base + lane] = s;
-          least = fminf(least, s);  // (a NaN, as padding is, is passed over)
-          most = fmaxf(most, s);
-        }
-      } else {
-        if (group < tokens)
-#pragma unroll
-          for (int sub = 0; sub < 4; ++sub)
-            if (base + sub * 16 + col < end) {
-              a.scores[out + group * a.heads * a.row_pad + base + sub * 16 + col] = v[sub];
-              least = fminf(least, v[sub]);
-              most = fmaxf(most, v[sub]);
-            }
+        wv.put64(v, out, pitch, live, base, to, mask);
+        entry = next;
+        next = after;
       }
     }
-    // Largest norm of this tile's rows: 0 only if all are zero. Squares below the float range are made
-    // up for.
+    // The tile's facts. The largest norm is 0 only if all rows are zero; squares below the float range are
+    // made up for.
     uint32_t nb = __float_as_uint(norm);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
       nb = max(nb, (uint32_t)__shfl_xor((int)nb, d));
       bits |= (uint32_t)__shfl_xor((int)bits, d);
-      if (KEYS || d < 16) {
-        least = fminf(least, __shfl_xor(least, d));
-        most = fmaxf(most, __shfl_xor(most, d));
-      }
     }
-    if (lane == 0)
-      s_norm[wave] =
-          bits ? __float_as_uint(sqrtf(__uint_as_float(nb)) * 1.01f + 0x1p-58f) : 0;
-    if (KEYS ? lane == 0 : col == 0) {
-      s_least[wave][KEYS ? 0 : group] = least;
-      s_most[wave][KEYS ? 0 : group] = most;
+    if (lane == 0) {
+      s_norm[wave] = nb;
+      s_bits[wave] = bits;
+    }
+#pragma unroll
+    for (int set = 0; set < W::SETS; ++set) {
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        // over the lanes that have the same new token
+        if (d >= (KEYS ? NT == 1 ? 64 : NT == 2 ? 32 : 16 : 16)) break;
+        wv.least[set] = fminf(wv.least[set], __shfl_xor(wv.least[set], d));
+        wv.most[set] = fmaxf(wv.most[set], __shfl_xor(wv.most[set], d));
+      }
+      if (col == 0) {
+        s_least[wave][wv.token_of(set)] = wv.least[set];
+        s_most[wave][wv.token_of(set)] = wv.most[set];
+      }
     }
     __syncthreads();
     if (threadIdx.x < (unsigned)tokens) {
-      uint32_t n = 0;
-      least = INFINITY, most = -INFINITY;
+      uint32_t n = 0, any = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < WAVES; ++i) {
         n = max(n, s_norm[i]);
-        least = fminf(least, s_least[i][threadIdx.x]);
-        most = fmaxf(most, s_most[i][threadIdx.x]);
+        any |= s_bits[i];
+      }
+      float least = INFINITY, most = -INFINITY;
+      if (team) {
+        least = s_least[threadIdx.x / W::TOKENS][threadIdx.x % W::TOKENS];
+        most = s_most[threadIdx.x / W::TOKENS][threadIdx.x % W::TOKENS];
+      } else {
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+          least = fminf(least, s_least[i][threadIdx.x]);
+          most = fmaxf(most, s_most[i][threadIdx.x]);
+        }
       }
       a.facts[((int64_t)(token0 + (int)threadIdx.x - a.row0) * a.heads + h) * a.tiles + kt] =
-          TileFacts{__uint_as_float(n), least, most};
+          TileFacts{any ? sqrtf(__uint_as_float(n)) * 1.01f + 0x1p-58f : 0.f, least, most};
     }
     if (a.hist && kt == 0)  // added to by the next kernel
       for (int i = 0; i < tokens; ++i)
-        for (int x = threadIdx.x; x < kLongBins; x += kScoreThreads)
+        for (int x = threadIdx.x; x < kLongBins; x += T)
           a.hist[((int64_t)(token0 + i - a.row0) * a.heads + h) * kLongBins + x] = 0;
     __syncthreads();
   }
@@ -231,7 +475,7 @@ struct SelectPlan {
   int64_t candidates, row_pad, tiles, parts;
   bool is_long;
   int64_t row_bytes;  // of a new token, all kv heads
-  int32_t tile_rows, tile_size;
+  int32_t tile_size;
 };
 
 int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -251,23 +495,36 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
   const int64_t words =
       p.row_pad + 3 * p.tiles + (big ? p.row_pad + kLongBins + p.parts + 3 : 0);
   p.row_bytes = words * 4 * b.kv_heads;
-  p.tile_rows = keys ? 1 : Shape<HISPARSE_INDEX_MEANS>::ROWS;
   return p;
 }
 
+template <int KIND, int MT, int NT, int WAVES, bool TEAM, int OCCUPANCY>
+void launch_score(const SelectArgs& a, hipStream_t s) {
+  constexpr int ROWS = TEAM ? WAVES * Wave<KIND, MT, NT>::TOKENS : 1;
+  const unsigned row_tiles = (unsigned)((a.rows + ROWS - 1) / ROWS);
+  hipLaunchKernelGGL((score_kernel<KIND, MT, NT, WAVES, TEAM, OCCUPANCY>),
+                     dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), dim3(64 * WAVES), 0, s, a);
+}
+
 hipError_t launch_select(const SelectArgs& a, int kind, const SelectPlan& p, hipStream_t s) {
-  const unsigned row_tiles = (unsigned)((a.rows + p.tile_rows - 1) / p.tile_rows);
-  const dim3 grid(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), block(kScoreThreads);
   constexpr int K = HISPARSE_INDEX_KEYS, B = HISPARSE_INDEX_BOUNDS, M = HISPARSE_INDEX_MEANS;
+  const bool team = a.max_chunk >= kTeamChunk;
   if (kind == B) {
-    hipLaunchKernelGGL((score_kernel<B, 1>), grid, block, 0, s, a);
+    if (team) launch_score<B, 1, 1, 4, true, 2>(a, s);
+    else launch_score<B, 1, 1, 4, false, 2>(a, s);
   } else if (kind == M) {
-    hipLaunchKernelGGL((score_kernel<M, 1>), grid, block, 0, s, a);
+    if (team) launch_score<M, 2, 1, 4, true, 2>(a, s);
+    else launch_score<M, 1, 1, 4, false, 2>(a, s);
+  } else if (team) {
+    if (a.q_heads <= 16) launch_score<K, 1, 4, 8, true, 2>(a, s);
+    else if (a.q_heads <= 32) launch_score<K, 2, 2, 8, true, 2>(a, s);
+    else if (a.q_heads <= 64) launch_score<K, 4, 1, 8, true, 2>(a, s);
+    else launch_score<K, 8, 1, 4, true, 1>(a, s);
   } else {
-    if (a.q_heads <= 16) hipLaunchKernelGGL((score_kernel<K, 1>), grid, block, 0, s, a);
-    else if (a.q_heads <= 32) hipLaunchKernelGGL((score_kernel<K, 2>), grid, block, 0, s, a);
-    else if (a.q_heads <= 64) hipLaunchKernelGGL((score_kernel<K, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((score_kernel<K, 8>), grid, block, 0, s, a);
+    if (a.q_heads <= 16) launch_score<K, 1, 1, 4, false, 3>(a, s);
+    else if (a.q_heads <= 32) launch_score<K, 2, 1, 4, false, 3>(a, s);
+    else if (a.q_heads <= 64) launch_score<K, 4, 1, 4, false, 2>(a, s);
+    else launch_score<K, 8, 1, 4, false, 1>(a, s);
   }
   return launch_choose(a, kind, p.candidates, s);
 }
@@ -303,10 +560,9 @@ size_t hisparse_select_workspace_bytes(const hisparse_index_desc_t* x,
   if (hisparse_validate_select(x, b, d) != HISPARSE_OK) return 0;
   const SelectPlan p = plan_select(*x, *b);
   const int64_t rows = b->total_tokens > 1 ? b->total_tokens : 1;
-  const size_t tile = (size_t)(p.tile_rows * p.row_bytes);
   size_t bytes = (size_t)rows <= kMostScoreBytes / (size_t)p.row_bytes ? (size_t)(rows * p.row_bytes)
                                                                       : kMostScoreBytes;
-  if (bytes < tile) bytes = tile;
+  if (bytes < (size_t)p.row_bytes) bytes = (size_t)p.row_bytes;
   return (bytes + 255) / 256 * 256;
 }
 
@@ -335,18 +591,17 @@ hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* x,
   if (b->total_tokens == 0) return HISPARSE_OK;
   const SelectPlan p = plan_select(*x, *b);
   if (!d_index || !d_q || !d_sel || !d_workspace ||
-      workspace_bytes < (size_t)(p.tile_rows * p.row_bytes))
+      workspace_bytes < (size_t)p.row_bytes)
     return HISPARSE_ERR_INVALID_ARG;
-  // rows of a step: what the workspace holds, in whole tiles, and a launch's 2^32 threads
+  // rows of a step: what the workspace holds, and a launch's 2^32 threads
   int64_t step = (int64_t)(workspace_bytes / (size_t)p.row_bytes);
   const int64_t blocks_of_tile = p.tiles * b->kv_heads;
-  const int64_t most = ((int64_t)UINT32_MAX / kScoreThreads / blocks_of_tile) * p.tile_rows;
+  const int64_t most = (int64_t)UINT32_MAX / 512 / blocks_of_tile;
   const int64_t most_chosen =
       (int64_t)UINT32_MAX / 1024 / ((p.is_long ? p.parts : 1) * b->kv_heads);
   if (step > most) step = most;
   if (step > most_chosen) step = most_chosen;
   if (step > b->total_tokens) step = b->total_tokens;
-  else step = step / p.tile_rows * p.tile_rows;
   if (step < 1) return HISPARSE_ERR_UNSUPPORTED;
   SelectArgs a{};
   static_cast<BatchArgs&>(a) = batch_args(*b, d_table, d_chunk_start, d_kv_len);
