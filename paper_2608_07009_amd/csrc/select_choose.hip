@@ -41,15 +41,20 @@ __device__ __forceinline__ double positive(double x) { return x > 0.0 ? x : x ==
 
 // T threads, of a kernel that chooses among up to CAP candidates at once.
 template <int KIND, int T, int BINS, int LIST, int CAP>
-struct Shared {
+struct alignas(16) Shared {
   static constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
   union {
-    uint32_t hist[BINS];
-    double part[KEYS ? 8 * kBatch : 1];  // keys: 16 heads' share of open candidates' scores
+    struct {
+      union {
+        uint32_t hist[BINS];
+        double part[KEYS ? 8 * kBatch : 1];  // keys: 16 heads' share of open candidates' scores
+      };
+      uint64_t score[LIST];
+      int list[LIST];        // open candidates, and each one's place among those looked at
+      uint16_t where[LIST];
+    };
+    int out[CAP < kMaxTopK ? CAP : kMaxTopK];  // at the end, the chosen ones
   };
-  uint64_t score[LIST];
-  int list[LIST];        // open candidates, and each one's place among those looked at
-  uint16_t where[LIST];
   uint32_t win[CAP / 32];  // chosen ones among the open, by place
   double q[KEYS ? 2 : 2 * kIndexDims];   // bounds and means: the sums over the heads
   uint32_t wave_a[T / 64], wave_b[T / 64], wave_c[T / 64];
@@ -58,18 +63,21 @@ struct Shared {
 };
 
 struct Add {
+  static constexpr uint32_t none = 0;
   __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return x + y; }
 };
 struct Most {
+  static constexpr uint32_t none = 0;
   __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return max(x, y); }
 };
 struct Least {
+  static constexpr uint32_t none = ~0u;
   __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return min(x, y); }
 };
 template <int T, class F>
 __device__ __forceinline__ uint32_t group_reduce(uint32_t x, uint32_t* waves, F f) {
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) x = f(x, (uint32_t)__shfl_xor((int)x, d));
+  x = wave_reduce(x, F::none, f);
+  if constexpr (T == 64) return x;
   __syncthreads();
   if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = x;
   __syncthreads();
@@ -189,8 +197,7 @@ struct Row {
           const double lo = low_half(x[i]), hi = high_half(x[i]);
           sq = fma(lo, lo, fma(hi, hi, sq));
         }
-#pragma unroll
-        for (int d = 1; d < 16; d *= 2) sq += __shfl_xor(sq, d);
+        sq = sum16_64(sq);
         if (c == 0) {
           const double n = sqrt(sq), w = wrow ? fabs((double)wrow[e]) : 1.0;
           A += w * n;
@@ -212,12 +219,9 @@ struct Row {
         Q = fma(pos, pos, fma(neg, neg, Q));
       }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      A += __shfl_xor(A, d);
-      W += __shfl_xor(W, d);
-      Q += __shfl_xor(Q, d);
-    }
+    A = wave_sum64(A);
+    W = wave_sum64(W);
+    Q = wave_sum64(Q);
     uint32_t norm = 0, least = ~0u, most = 0;
     const int tiles = (seen + (1 << a.tile_size) - 1) >> a.tile_size;
     for (int i = threadIdx.x; i < tiles; i += T) {
@@ -226,14 +230,11 @@ struct Row {
       least = min(least, ordered32(f.least));
       most = max(most, ordered32(f.most));
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      norm = max(norm, (uint32_t)__shfl_xor((int)norm, d));
-      least = min(least, (uint32_t)__shfl_xor((int)least, d));
-      most = max(most, (uint32_t)__shfl_xor((int)most, d));
-    }
+    norm = wave_reduce(norm, Most::none, Most());
+    least = wave_reduce(least, Least::none, Least());
+    most = wave_reduce(most, Most::none, Most());
     __syncthreads();
-    if (lane == 0) {
+    if (lane == 63) {
       s.wave_d[wave] = A;
       s.wave_e[wave] = W;
       s.wave_f[wave] = Q;
@@ -521,7 +522,8 @@ struct Stream {
     for (int base = lo; base < hi; base += 64) {
       const bool in = is_in(base + r.lane);
       const uint64_t mask = __ballot(in);
-      if (in) r.put(at + __popcll(mask & ((1ull << r.lane) - 1)), base + r.lane);
+      const int place = at + (int)__popcll(mask & ((1ull << r.lane) - 1));
+      if (in && place < r.a.top_k) r.put(place, base + r.lane);
       at += __popcll(mask);
     }
     r.finish(total);
@@ -600,8 +602,7 @@ __device__ __forceinline__ void score_open(const Row<KIND, T>& r, S& s, int n) {
         for (int z = 0; z < 4; ++z)
           sum = fma((double)high_half(y[z]), q[2 * z + 1], fma((double)low_half(y[z]), q[2 * z], sum));
       }
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) sum += __shfl_xor(sum, d);
+      sum = sum16_64(sum);
       if (c == 0) s.score[i] = ordered(sum);
     }
     __syncthreads();
@@ -648,7 +649,9 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
   if (listed) {
     if (!a.hist || !row.divisible()) return slow();
     const int parts = (r.seen + kPart - 1) / kPart;  // at most kMaxParts, T
-    const int mine = (int)threadIdx.x < parts ? a.part_count[slot * a.parts + threadIdx.x] : 0;
+    // (held to what can be: where starts do not ascend, a row may not have been scored)
+    const int mine = (int)threadIdx.x < parts
+                         ? min(max(a.part_count[slot * a.parts + threadIdx.x], 0), kPart) : 0;
     const int inc = wave_inclusive(mine);
     if (r.lane == 63) s.wave_a[r.wave] = (uint32_t)inc;
     __syncthreads();
@@ -688,6 +691,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
             else hi = mid;
           }
           j = a.survivors[slot * a.row_pad + (int64_t)lo * kPart + e - (int)s.win[lo]];
+          j = min(max(j, 0), r.seen - 1);
           y = r.scores[j];
           if (r.forced(j)) {
             y = __uint_as_float(kNan);
@@ -820,14 +824,18 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
     before += i < r.wave ? (int)s.wave_a[i] : 0;
     total += (int)s.wave_a[i];
   }
+  // by way of LDS: looked up and stored 64 at a time, and not where each lane finds its own
 #pragma unroll
   for (int v = 0; v < V; ++v) {
     int at = before + places[v];
     if (v < groups)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (in >> (4 * v + i) & 1) r.put(at++, position(4 * v + i));
+        if ((in >> (4 * v + i) & 1) && at < a.top_k) s.out[at++] = position(4 * v + i);
   }
+  __syncthreads();
+#pragma unroll 4
+  for (int i = threadIdx.x; i < min(total, a.top_k); i += T) r.put(i, s.out[i]);
   r.finish(total);
 }
 

@@ -421,11 +421,28 @@ def test_captured_and_replayed(kind):
         other.compare()
 
 
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("requests", [1, 3, 64, 65, 200])
+def test_rows_before_the_first_request_and_many_requests(kind, requests):
+    """Rows that no request starts at or before, empty requests, more requests than a wave has lanes."""
+    for chunk in (1, 6):
+        c = Case(kind, 4, [(i * 7) % (chunk + 1) for i in range(requests)],
+                 [(i * 37) % 400 for i in range(requests)], k=6, last=1, tail=3)
+        c.start = [x + 7 for x in c.start]
+        c.total += 7
+        g = torch.Generator().manual_seed(1)
+        c.q = torch.randn((c.total, c.q.shape[1]), generator=g).to(torch.bfloat16)
+        c.w = None if c.w is None else torch.randn((c.total, c.w.shape[1]), generator=g)
+        c.check()
+
+
 def test_starts_that_do_not_ascend_stay_in_bounds():
     """What the rows hold is unspecified; nothing outside the arrays is touched."""
     for kind in (KEYS, BOUNDS, MEANS):
         c = Case(kind, 4, [5, 5, 5], [300, 200, 100], k=8, last=1)
         c.device()
+        c.dv["start"].copy_(torch.tensor([0, 7, 3, 15], dtype=torch.int32))
+        c.call()
         room = torch.full((c.total + 4, 1, 8), MARK, dtype=torch.int32, device="cuda")
         c.dv["start"].copy_(torch.tensor([9, 2, 14, -3], dtype=torch.int32))
         c.call(sel=room[2:-2])
