@@ -155,9 +155,8 @@ struct Wave {
             s_a + (first * 4 + m * 16 + (lane & 15)) * (S::DIMS + 8) + k * 32 + (lane >> 4) * 8);
   }
 
-  // Scores of 16 candidates: keys, this lane's share of each new token's; the others, whole.
-  __device__ __forceinline__ void score(const u32x4_t (&x)[S::STEPS], float (&v)[KEYS ? NT : MT]) {
-    f32x4_t acc[TILES];
+  // Products with 16 candidates' rows.
+  __device__ __forceinline__ void multiply(const u32x4_t (&x)[S::STEPS], f32x4_t (&acc)[TILES]) const {
 #pragma unroll
     for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{};
 #pragma unroll
@@ -166,6 +165,9 @@ struct Wave {
       for (int t = 0; t < TILES; ++t)
         acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t][k], __builtin_bit_cast(bf16x8_t, x[k]),
                                                          acc[t], 0, 0, 0);
+  }
+  // Their scores: keys, this lane's share of each new token's; the others, whole.
+  __device__ __forceinline__ void add_up(const f32x4_t (&acc)[TILES], float (&v)[KEYS ? NT : MT]) const {
     if constexpr (KEYS) {
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
@@ -348,17 +350,31 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
         const uint64_t now = mask;
         if (base + 64 < end) fetch(base + 64);
         if (live > 0) {
+          // the products of 16 candidates while those of the 16 before are added up
           float v[4][KEYS ? NT : MT];
-#pragma unroll
-          for (int sub = 0; sub < 4; ++sub) {
-            u32x4_t y[S::STEPS];
+          u32x4_t y[2][S::STEPS];
+          f32x4_t acc[2][W::TILES];
+          auto read = [&](int sub) {
             const uint8_t* row = s_mem + cur * TILE_BYTES + (sub * 16 + col) * (P * 16);
 #pragma unroll
             for (int k = 0; k < S::STEPS; ++k)
-              y[k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
-            wv.score(y, v[sub]);
+              y[sub & 1][k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
+          };
+          read(0);
+#pragma unroll
+          for (int sub = 0; sub < 4; ++sub) {
+            if (sub < 3) read(sub + 1);
+            wv.multiply(y[sub & 1], acc[sub & 1]);
+            if (sub > 0) wv.add_up(acc[(sub - 1) & 1], v[sub - 1]);
+            if (KEYS)
+#pragma unroll
+              for (int i = 0; i < W::TILES * S::STEPS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // an MFMA
+                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);  // two vector instructions
+              }
             __builtin_amdgcn_sched_barrier(0);
           }
+          wv.add_up(acc[1], v[3]);
           wv.put64(v, out, pitch, live, base, end, now);
         }
         cur ^= 1;
@@ -402,7 +418,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
           larger(valid ? sq : 0.f);
           bits |= valid ? any : 0;
           asm volatile("" : "+v"(bits), "+v"(norm));  // now: the operands' registers are loaded again
-          wv.score(x[sub & 1], v[sub]);
+          f32x4_t acc[W::TILES];
+          wv.multiply(x[sub & 1], acc);
+          wv.add_up(acc, v[sub]);
           __builtin_amdgcn_sched_barrier(0);
           // (past the end: the last candidate again)
           if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);

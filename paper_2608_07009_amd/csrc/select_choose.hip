@@ -557,6 +557,12 @@ __device__ __forceinline__ void score_open(const Row<KIND, T>& r, S& s, int n) {
           for (int x = 0; x < 4; ++x)
             qx[x] = reinterpret_cast<const u32x4_t*>(r.s_q + e * kQPitch + 32 * g)[x];
         }
+        float w[4];  // a lane has heads g, g + 4, g + 8, g + 12 of the tile
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int head = tile * 16 + g + 4 * x;
+          w[x] = r.wrow && head < r.a.q_heads ? r.wrow[head] : 1.f;
+        }
         f64x4 acc = {};
 #pragma unroll
         for (int x = 0; x < 4; ++x)
@@ -567,13 +573,10 @@ __device__ __forceinline__ void score_open(const Row<KIND, T>& r, S& s, int n) {
             acc = __builtin_amdgcn_mfma_f64_16x16x4f64((double)high_half(qx[x][y]),
                                                        (double)high_half(kx[x][y]), acc, 0, 0, 0);
           }
-        double sum = 0.0;  // a lane has heads g, g + 4, g + 8, g + 12 of the tile
+        double sum = 0.0;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int head = tile * 16 + g + 4 * x;
-          if (head < r.a.q_heads)
-            sum = fma(r.wrow ? (double)r.wrow[head] : 1.0, positive(acc[x]), sum);
-        }
+        for (int x = 0; x < 4; ++x)
+          if (tile * 16 + g + 4 * x < r.a.q_heads) sum = fma((double)w[x], positive(acc[x]), sum);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (g == 0) s.part[tile * kBatch + i] = sum;
@@ -786,13 +789,16 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
         return slow();
       }
       score_open<KIND, T>(r, s, open);
-      for (int i = threadIdx.x; i < open; i += T) {
+      for (int i = r.wave; i < open; i += WAVES) {  // a wave looks at 64 others at a time
         const uint64_t y = s.score[i];
         const int e = s.where[i];
         int better = 0;
-        for (int z = 0; z < open; ++z)
-          better += s.score[z] > y || (s.score[z] == y && s.where[z] < e);
-        if (better < need) atomicOr(&s.win[e >> 5], 1u << (e & 31));
+        for (int z = r.lane; z - r.lane < open; z += 64) {
+          const int at = min(z, open - 1);
+          const uint64_t o = s.score[at];
+          better += (int)__popcll(__ballot(z < open && (o > y || (o == y && s.where[at] < e))));
+        }
+        if (better < need && r.lane == 0) atomicOr(&s.win[e >> 5], 1u << (e & 31));
       }
       __syncthreads();
       if (open_bits)
