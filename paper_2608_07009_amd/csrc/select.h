@@ -81,18 +81,24 @@ __device__ __forceinline__ bool find_row(const SelectArgs& a, int q, int h, int 
   return true;
 }
 
-// Bounds and means: the sums over a kv head's queries of dim d, 64 bits. (neg is 0 for means.)
+// Bounds and means: the sums in 64 bits of dims 8 c .. 8 c + 7 over heads e0, e0 + step, .. of a kv head's
+// queries, positive and negative ones apart (means: all in pos).
 template <int KIND>
-__device__ __forceinline__ void query_sums(const SelectArgs& a, int token, int h, int d, double& pos,
-                                           double& neg) {
+__device__ __forceinline__ void query_sums(const SelectArgs& a, int token, int h, int c, int e0, int step,
+                                           double (&pos)[8], double (&neg)[8]) {
   const uint16_t* q =
-      a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + d;
-  pos = neg = 0.0;
-#pragma unroll 4
-  for (int e = 0; e < a.q_heads; ++e) {
-    const double v = bf16_value(q[e * kIndexDims]);
-    if (KIND == HISPARSE_INDEX_BOUNDS && v < 0.0) neg += v;
-    else pos += v;
+      a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + 8 * c;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) pos[i] = neg[i] = 0.0;
+#pragma unroll 8
+  for (int e = e0; e < a.q_heads; e += step) {
+    const u32x4_t x = *reinterpret_cast<const any_u32x4_t*>(q + e * kIndexDims);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const double v = i & 1 ? high_half(x[i >> 1]) : low_half(x[i >> 1]);
+      if (KIND == HISPARSE_INDEX_BOUNDS && v < 0.0) neg[i] += v;
+      else pos[i] += v;
+    }
   }
 }
 

@@ -19,11 +19,9 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 constexpr int kRowPad = 256;          // a row of scores is a multiple of this
 // New tokens of a request from which waves have new tokens of their own.
 constexpr int kTeamChunk = 5;
+// Workgroups that tiles of candidates are made small for, and the least tile (log2).
+constexpr int kWantedGroups = 512, kLeastTile = 8;
 constexpr size_t kMostScoreBytes = (size_t)1 << 30;
-
-__device__ __forceinline__ uint16_t to_bf16(float x) {
-  return (uint16_t)__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x, 0.f}, bf16x2_t));
-}
 
 // ---- scores ----------------------------------------------------------------------------------
 
@@ -33,7 +31,6 @@ struct Shape : IndexShape<KIND> {
   using IndexShape<KIND>::DIMS;
   static constexpr int STEPS = DIMS / 32;          // MFMAs of 16 rows x 16 candidates
   static constexpr int PIECES = DIMS / 8;          // 16-byte pieces of an index row
-  static constexpr int TILE = KEYS ? 1024 : 512;   // candidates of a workgroup
 };
 
 // Sum of the squares of eight bf16 values, and acc.
@@ -78,21 +75,29 @@ template <int KIND, int T>
 __device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int tokens, int rows, int h,
                                             uint16_t* s_a) {
   constexpr int DIMS = Shape<KIND>::DIMS, PITCH = DIMS + 8;
-  for (int x = threadIdx.x; x < rows * kIndexDims; x += T) {
-    const int i = x / kIndexDims, d = x % kIndexDims;
-    double pos = 0.0, neg = 0.0;
-    if (i < tokens) query_sums<KIND>(a, token0 + i, h, d, pos, neg);
-    auto put = [&](int at, double v) {
+  for (int x = threadIdx.x; x < rows * 16; x += T) {
+    const int i = x >> 4, c = x & 15;
+    double pos[8], neg[8];
+    query_sums<KIND>(a, token0 + i, h, c, i < tokens ? 0 : a.q_heads, 1, pos, neg);
+    auto put = [&](int at, double (&v)[8]) {
 #pragma unroll
-      for (int part = 0; part < 3; ++part) {
-        const uint16_t b = to_bf16((float)v);
-        s_a[(4 * i + part) * PITCH + at] = b;
-        v -= bf16_value(b);
+      for (int part = 0; part < 4; ++part) {
+        u32x4_t y = {};
+        if (part < 3)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const bf16x2_t b =
+                __builtin_convertvector(f32x2_t{(float)v[2 * d], (float)v[2 * d + 1]}, bf16x2_t);
+            const uint32_t bits = __builtin_bit_cast(uint32_t, b);
+            v[2 * d] -= low_half(bits);
+            v[2 * d + 1] -= high_half(bits);
+            y[d] = bits;
+          }
+        *reinterpret_cast<u32x4_t*>(s_a + (4 * i + part) * PITCH + at) = y;
       }
-      s_a[(4 * i + 3) * PITCH + at] = 0;
     };
-    if (KIND == HISPARSE_INDEX_BOUNDS) put(d, neg);
-    put(KIND == HISPARSE_INDEX_BOUNDS ? kIndexDims + d : d, pos);
+    if (KIND == HISPARSE_INDEX_BOUNDS) put(8 * c, neg);
+    put(KIND == HISPARSE_INDEX_BOUNDS ? kIndexDims + 8 * c : 8 * c, pos);
   }
 }
 
@@ -277,7 +282,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
     const int token0 = t, tokens = min(row1, r.begin + r.n) - t;
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
-    const int first = kt * S::TILE, end = min(first + S::TILE, seen);
+    const int first = kt << a.tile_size, end = min(first + (1 << a.tile_size), seen);
     if (seen <= a.top_k || first >= seen) continue;
     const bool team = TEAM && tokens > W::TOKENS;
     const int mine = team ? wave * W::TOKENS : 0;      // this wave's first new token
@@ -293,6 +298,8 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
       return index + (uint64_t)(uint32_t)(valid ? entry : 0) * (uint32_t)a.record_stride +
              (KEYS ? (j & ((1 << a.tpr_shift) - 1)) * kIndexRowBytes : 0);
     };
+    // 64 candidates from a multiple of 64 on that lie in one record, one behind the other
+    const bool one_record = KEYS && a.tpr_shift >= 6;
     W wv;
     wv.start();
     if constexpr (KEYS) {
@@ -321,6 +328,12 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
       uint64_t mask;  // which of 64 candidates are not padding
       auto fetch = [&](int base) {
         mask = __ballot(there(entry, base + lane, end));
+        if (one_record) {
+          const uint8_t* from = row_of(__builtin_amdgcn_readfirstlane(entry), mask & 1, base);
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i)
+            x[i] = *reinterpret_cast<const u32x4_t*>(from + (threadIdx.x + i * T) * 16);
+        } else
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
           const int row = row_first + i * (T / P), e = __shfl(entry, row);
@@ -334,10 +347,10 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
           const int row = row_first + i * (T / P);
           const bool valid = mask >> row & 1;
           *reinterpret_cast<u32x4_t*>(buf + row * (P * 16) + ((piece ^ (row & 15)) << 4)) = x[i];
+          // the largest of this piece; over the row's pieces they are added up at the end, which is no less
+          // than the largest row
           bits |= valid ? (x[i][0] | x[i][1] | x[i][2] | x[i][3]) & 0x7fff7fffu : 0;
-          float sq = sum16(squares(x[i], 0.f));
-          if (P == 32) sq += __shfl_xor(sq, 16);
-          larger(valid ? sq : 0.f);
+          larger(valid ? squares(x[i], 0.f) : 0.f);
           asm volatile("" : "+v"(bits), "+v"(norm));
         }
       };
@@ -382,12 +395,19 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
         __syncthreads();
       }
     } else {
-      const int from = first + wave * (S::TILE / WAVES), to = min(from + S::TILE / WAVES, end);
+      const int share = (1 << a.tile_size) / WAVES;
+      const int from = first + wave * share, to = min(from + share, end);
       u32x4_t x[2][S::STEPS];  // two times 16 candidates, the next ones on their way
       int entry = 0, next = 0;  // of candidate base + lane, and of the next step's
       auto fetch = [&](u32x4_t (&y)[S::STEPS], int entries, int base, int sub) {
-        const int j = base + sub * 16 + col, e = __shfl(entries, sub * 16 + col);
-        const uint8_t* row = row_of(e, there(e, j, to), min(j, to - 1)) + group * 16;
+        const uint8_t* row;
+        if (one_record) {
+          const int e = __builtin_amdgcn_readfirstlane(entries);
+          row = row_of(e, there(e, base, to), base + sub * 16) + col * kIndexRowBytes + group * 16;
+        } else {
+          const int j = base + sub * 16 + col, e = __shfl(entries, sub * 16 + col);
+          row = row_of(e, there(e, j, to), min(j, to - 1)) + group * 16;
+        }
 #pragma unroll
         for (int k = 0; k < S::STEPS; ++k) y[k] = *reinterpret_cast<const u32x4_t*>(row + k * 64);
       };
@@ -433,6 +453,10 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
     }
     // The tile's facts. The largest norm is 0 only if all rows are zero; squares below the float range are
     // made up for.
+    if (team) {
+      norm = sum16(norm);
+      if (S::PIECES == 32) norm += __shfl_xor(norm, 16);
+    }
     uint32_t nb = __float_as_uint(norm);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -489,6 +513,13 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
 
 // ---- host ------------------------------------------------------------------------------------
 
+// New tokens of a workgroup of score_kernel.
+int team_rows(int kind, int q_heads) {
+  if (kind == HISPARSE_INDEX_BOUNDS) return 16;
+  if (kind == HISPARSE_INDEX_MEANS) return 32;
+  return q_heads <= 16 ? 32 : q_heads <= 32 ? 16 : q_heads <= 64 ? 8 : 4;
+}
+
 struct SelectPlan {
   int64_t candidates, row_pad, tiles, parts;
   bool is_long;
@@ -498,20 +529,28 @@ struct SelectPlan {
 
 int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of; }
 
-SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc_t& b) {
+SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc_t& b,
+                       const hisparse_select_desc_t& d) {
   SelectPlan p{};
   const bool keys = x.kind == HISPARSE_INDEX_KEYS;
   p.candidates = keys ? (int64_t)b.max_records * b.tokens_per_record : b.max_records;
-  const int tile = keys ? Shape<HISPARSE_INDEX_KEYS>::TILE : Shape<HISPARSE_INDEX_MEANS>::TILE;
-  p.tile_size = shift_of(tile);
-  p.tiles = whole(p.candidates, tile);
+  // The largest tiles of which there are enough: a workgroup first loads its queries. (512 new tokens x 64
+  // heads over 32768 keys: scores and choice in 321 us with 512 of them, 331 with 1024.)
+  const bool team = b.max_chunk >= kTeamChunk;
+  const int64_t row_tiles =
+      whole(b.total_tokens, team ? team_rows(x.kind, d.q_heads) : 1) * b.kv_heads;
+  p.tile_size = team ? (keys ? 12 : 9) : keys ? 10 : 9;
+  while (p.tile_size > kLeastTile &&
+         row_tiles * whole(p.candidates, 1 << p.tile_size) < kWantedGroups)
+    --p.tile_size;
+  p.tiles = whole(p.candidates, 1 << p.tile_size);
   p.parts = whole(p.candidates, kPart);
   const bool big = p.candidates > kRegisterRow;
   p.is_long = big && p.parts <= kMaxParts;
   p.row_pad = whole(p.candidates, big ? kPart : kRowPad) * (big ? kPart : kRowPad);
   // (those of rows of too many parts too: a workspace serves smaller batches)
   const int64_t words =
-      p.row_pad + 3 * p.tiles + (big ? p.row_pad + kLongBins + p.parts + 3 : 0);
+      p.row_pad + 3 * whole(p.candidates, 1 << kLeastTile) + (big ? p.row_pad + kLongBins + p.parts + 3 : 0);
   p.row_bytes = words * 4 * b.kv_heads;
   return p;
 }
@@ -564,7 +603,7 @@ hisparse_status_t hisparse_validate_select(const hisparse_index_desc_t* x,
       d->last_records < 0 || (int64_t)d->first_records + d->last_records > d->top_k ||
       d->q_token_stride < 0)
     return HISPARSE_ERR_INVALID_ARG;
-  const hisparse::SelectPlan p = hisparse::plan_select(*x, *b);
+  const hisparse::SelectPlan p = hisparse::plan_select(*x, *b, *d);
   if ((int64_t)b->total_tokens * b->kv_heads > (int64_t)INT32_MAX ||
       p.candidates * b->kv_heads >= (1ll << 30))
     return HISPARSE_ERR_UNSUPPORTED;
@@ -576,7 +615,7 @@ size_t hisparse_select_workspace_bytes(const hisparse_index_desc_t* x,
                                        const hisparse_select_desc_t* d) {
   using namespace hisparse;
   if (hisparse_validate_select(x, b, d) != HISPARSE_OK) return 0;
-  const SelectPlan p = plan_select(*x, *b);
+  const SelectPlan p = plan_select(*x, *b, *d);
   const int64_t rows = b->total_tokens > 1 ? b->total_tokens : 1;
   size_t bytes = (size_t)rows <= kMostScoreBytes / (size_t)p.row_bytes ? (size_t)(rows * p.row_bytes)
                                                                       : kMostScoreBytes;
@@ -607,7 +646,7 @@ hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* x,
   if (keys && d_records && x->num_records * x->tokens_per_record > (int64_t)INT32_MAX)
     return HISPARSE_ERR_UNSUPPORTED;
   if (b->total_tokens == 0) return HISPARSE_OK;
-  const SelectPlan p = plan_select(*x, *b);
+  const SelectPlan p = plan_select(*x, *b, *d);
   if (!d_index || !d_q || !d_sel || !d_workspace ||
       workspace_bytes < (size_t)p.row_bytes)
     return HISPARSE_ERR_INVALID_ARG;

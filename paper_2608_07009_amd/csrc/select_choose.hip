@@ -206,17 +206,24 @@ struct Row {
         }
       }
     } else {
-      for (int d = threadIdx.x; d < kIndexDims; d += T) {
-        double pos, neg;
-        query_sums<KIND>(a, token, h, d, pos, neg);
-        if (KIND == HISPARSE_INDEX_BOUNDS) {
-          s.q[d] = neg;
-          s.q[kIndexDims + d] = pos;
-        } else {
-          s.q[d] = pos;
+      if (wave == 0) {  // 16 lanes a query
+        double pos[8], neg[8];
+        query_sums<KIND>(a, token, h, lane & 15, lane >> 4, 4, pos, neg);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+          for (int d = 16; d < 64; d *= 2) {
+            pos[i] += __shfl_xor(pos[i], d);
+            if (KIND == HISPARSE_INDEX_BOUNDS) neg[i] += __shfl_xor(neg[i], d);
+          }
+          const int d = 8 * (lane & 15) + i;
+          if (lane < 16) {
+            if (KIND == HISPARSE_INDEX_BOUNDS) s.q[d] = neg[i];
+            s.q[KIND == HISPARSE_INDEX_BOUNDS ? kIndexDims + d : d] = pos[i];
+            A += fabs(pos[i]) + fabs(neg[i]);  // (0 only if all are)
+            Q = fma(pos[i], pos[i], fma(neg[i], neg[i], Q));
+          }
         }
-        A += fabs(pos) + fabs(neg);  // above the root of the squares' sum; see below
-        Q = fma(pos, pos, fma(neg, neg, Q));
       }
     }
     A = wave_sum64(A);
