@@ -83,14 +83,14 @@ __device__ __forceinline__ bool find_row(const SelectArgs& a, int q, int h, int 
 
 // Bounds and means: the sums in 64 bits of dims 8 c .. 8 c + 7 over heads e0, e0 + step, .. of a kv head's
 // queries, positive and negative ones apart (means: all in pos).
-template <int KIND>
+template <int KIND, int UNROLL>
 __device__ __forceinline__ void query_sums(const SelectArgs& a, int token, int h, int c, int e0, int step,
                                            double (&pos)[8], double (&neg)[8]) {
   const uint16_t* q =
       a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + 8 * c;
 #pragma unroll
   for (int i = 0; i < 8; ++i) pos[i] = neg[i] = 0.0;
-#pragma unroll 8
+#pragma unroll UNROLL
   for (int e = e0; e < a.q_heads; e += step) {
     const u32x4_t x = *reinterpret_cast<const any_u32x4_t*>(q + e * kIndexDims);
 #pragma unroll

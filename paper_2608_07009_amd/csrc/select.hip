@@ -58,6 +58,18 @@ __device__ __forceinline__ float sum16(float x) {
   x += moved<0x122>(x);
   return x + moved<0x121>(x);
 }
+__device__ __forceinline__ float least16(float x) {
+  x = fminf(x, moved<0x128>(x));
+  x = fminf(x, moved<0x124>(x));
+  x = fminf(x, moved<0x122>(x));
+  return fminf(x, moved<0x121>(x));
+}
+struct Largest {
+  __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return max(x, y); }
+};
+struct Either {
+  __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return x | y; }
+};
 // The totals over the four rows of 16 lanes of v0 .. v3: that of v_r in row r.
 __device__ __forceinline__ float totals(float v0, float v1, float v2, float v3) {
   auto halves = [](float x, float y) {  // x's halves added in the lower half, y's in the upper
@@ -78,7 +90,7 @@ __device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int
   for (int x = threadIdx.x; x < rows * 16; x += T) {
     const int i = x >> 4, c = x & 15;
     double pos[8], neg[8];
-    query_sums<KIND>(a, token0 + i, h, c, i < tokens ? 0 : a.q_heads, 1, pos, neg);
+    query_sums<KIND, 16>(a, token0 + i, h, c, i < tokens ? 0 : a.q_heads, 1, pos, neg);
     auto put = [&](int at, double (&v)[8]) {
 #pragma unroll
       for (int part = 0; part < 4; ++part) {
@@ -276,6 +288,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
     const int q = request_at(a, t);
     const RequestRows r = rows_of(a, q);
     if (t < r.begin || t >= r.begin + r.n) {
+      if (ROWS == 1) return;
       ++t;
       continue;
     }
@@ -283,7 +296,10 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
     const int first = kt << a.tile_size, end = min(first + (1 << a.tile_size), seen);
-    if (seen <= a.top_k || first >= seen) continue;
+    if (seen <= a.top_k || first >= seen) {
+      if (ROWS == 1) return;
+      continue;
+    }
     const bool team = TEAM && tokens > W::TOKENS;
     const int mine = team ? wave * W::TOKENS : 0;      // this wave's first new token
     const int live = min(tokens - mine, W::TOKENS);    // and how many it has (0 or less: none)
@@ -416,39 +432,39 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
         next = entry_of<KEYS>(a, table, from + 64 + lane, to);
         fetch(x[0], entry, from, 0);
         fetch(x[1], entry, from, 1);
-      }
 #pragma unroll 1
-      for (int base = from; base < to; base += 64) {
-        const uint64_t mask = __ballot(there(entry, base + lane, to));
-        const int after = entry_of<KEYS>(a, table, base + 128 + lane, to);
-        float v[4][KEYS ? NT : MT];
+        for (int base = from; base < to; base += 64) {
+          const uint64_t mask = __ballot(there(entry, base + lane, to));
+          const int after = entry_of<KEYS>(a, table, base + 128 + lane, to);
+          float v[4][KEYS ? NT : MT];
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) {
-          float sq = 0.f;
-          uint32_t any = 0;
+          for (int sub = 0; sub < 4; ++sub) {
+            float sq = 0.f;
+            uint32_t any = 0;
 #pragma unroll
-          for (int k = 0; k < S::STEPS; ++k) {
-            const u32x4_t y = x[sub & 1][k];
-            any |= (y[0] | y[1] | y[2] | y[3]) & 0x7fff7fffu;
-            sq = squares(y, sq);
+            for (int k = 0; k < S::STEPS; ++k) {
+              const u32x4_t y = x[sub & 1][k];
+              any |= (y[0] | y[1] | y[2] | y[3]) & 0x7fff7fffu;
+              sq = squares(y, sq);
+            }
+            sq += __shfl_xor(sq, 16);
+            sq += __shfl_xor(sq, 32);
+            const bool valid = mask >> (sub * 16 + col) & 1;
+            larger(valid ? sq : 0.f);
+            bits |= valid ? any : 0;
+            asm volatile("" : "+v"(bits), "+v"(norm));  // now: the operands' registers are loaded again
+            f32x4_t acc[W::TILES];
+            wv.multiply(x[sub & 1], acc);
+            wv.add_up(acc, v[sub]);
+            __builtin_amdgcn_sched_barrier(0);
+            // (past the end: the last candidate again)
+            if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);
+            else fetch(x[sub & 1], next, base + 64, sub - 2);
           }
-          sq += __shfl_xor(sq, 16);
-          sq += __shfl_xor(sq, 32);
-          const bool valid = mask >> (sub * 16 + col) & 1;
-          larger(valid ? sq : 0.f);
-          bits |= valid ? any : 0;
-          asm volatile("" : "+v"(bits), "+v"(norm));  // now: the operands' registers are loaded again
-          f32x4_t acc[W::TILES];
-          wv.multiply(x[sub & 1], acc);
-          wv.add_up(acc, v[sub]);
-          __builtin_amdgcn_sched_barrier(0);
-          // (past the end: the last candidate again)
-          if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);
-          else fetch(x[sub & 1], next, base + 64, sub - 2);
+          wv.put64(v, out, pitch, live, base, to, mask);
+          entry = next;
+          next = after;
         }
-        wv.put64(v, out, pitch, live, base, to, mask);
-        entry = next;
-        next = after;
       }
     }
     // The tile's facts. The largest norm is 0 only if all rows are zero; squares below the float range are
@@ -457,28 +473,26 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
       norm = sum16(norm);
       if (S::PIECES == 32) norm += __shfl_xor(norm, 16);
     }
-    uint32_t nb = __float_as_uint(norm);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      nb = max(nb, (uint32_t)__shfl_xor((int)nb, d));
-      bits |= (uint32_t)__shfl_xor((int)bits, d);
-    }
+    const uint32_t nb = wave_reduce(__float_as_uint(norm), 0u, Largest());
+    bits = wave_reduce(bits, 0u, Either());
     if (lane == 0) {
       s_norm[wave] = nb;
       s_bits[wave] = bits;
     }
 #pragma unroll
-    for (int set = 0; set < W::SETS; ++set) {
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        // over the lanes that have the same new token
-        if (d >= (KEYS ? NT == 1 ? 64 : NT == 2 ? 32 : 16 : 16)) break;
-        wv.least[set] = fminf(wv.least[set], __shfl_xor(wv.least[set], d));
-        wv.most[set] = fmaxf(wv.most[set], __shfl_xor(wv.most[set], d));
+    for (int set = 0; set < W::SETS; ++set) {  // over the lanes that have the same new token
+      float lo = least16(wv.least[set]), hi = -least16(-wv.most[set]);
+      if (KEYS && NT <= 2) {
+        lo = fminf(lo, __shfl_xor(lo, 16));
+        hi = fmaxf(hi, __shfl_xor(hi, 16));
+      }
+      if (KEYS && NT == 1) {
+        lo = fminf(lo, __shfl_xor(lo, 32));
+        hi = fmaxf(hi, __shfl_xor(hi, 32));
       }
       if (col == 0) {
-        s_least[wave][wv.token_of(set)] = wv.least[set];
-        s_most[wave][wv.token_of(set)] = wv.most[set];
+        s_least[wave][wv.token_of(set)] = lo;
+        s_most[wave][wv.token_of(set)] = hi;
       }
     }
     __syncthreads();
@@ -507,6 +521,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
       for (int i = 0; i < tokens; ++i)
         for (int x = threadIdx.x; x < kLongBins; x += T)
           a.hist[((int64_t)(token0 + i - a.row0) * a.heads + h) * kLongBins + x] = 0;
+    if (ROWS == 1) return;
     __syncthreads();
   }
 }
@@ -515,8 +530,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs
 
 // New tokens of a workgroup of score_kernel.
 int team_rows(int kind, int q_heads) {
-  if (kind == HISPARSE_INDEX_BOUNDS) return 16;
-  if (kind == HISPARSE_INDEX_MEANS) return 32;
+  if (kind != HISPARSE_INDEX_KEYS) return 16;
   return q_heads <= 16 ? 32 : q_heads <= 32 ? 16 : q_heads <= 64 ? 8 : 4;
 }
 
@@ -539,7 +553,7 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
   const bool team = b.max_chunk >= kTeamChunk;
   const int64_t row_tiles =
       whole(b.total_tokens, team ? team_rows(x.kind, d.q_heads) : 1) * b.kv_heads;
-  p.tile_size = team ? (keys ? 12 : 9) : keys ? 10 : 9;
+  p.tile_size = !keys ? 9 : team ? 12 : 11;
   while (p.tile_size > kLeastTile &&
          row_tiles * whole(p.candidates, 1 << p.tile_size) < kWantedGroups)
     --p.tile_size;
@@ -570,7 +584,7 @@ hipError_t launch_select(const SelectArgs& a, int kind, const SelectPlan& p, hip
     if (team) launch_score<B, 1, 1, 4, true, 2>(a, s);
     else launch_score<B, 1, 1, 4, false, 2>(a, s);
   } else if (kind == M) {
-    if (team) launch_score<M, 2, 1, 4, true, 2>(a, s);
+    if (team) launch_score<M, 1, 1, 4, true, 2>(a, s);
     else launch_score<M, 1, 1, 4, false, 2>(a, s);
   } else if (team) {
     if (a.q_heads <= 16) launch_score<K, 1, 4, 8, true, 2>(a, s);

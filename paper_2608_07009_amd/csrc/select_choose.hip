@@ -208,7 +208,7 @@ struct Row {
     } else {
       if (wave == 0) {  // 16 lanes a query
         double pos[8], neg[8];
-        query_sums<KIND>(a, token, h, lane & 15, lane >> 4, 4, pos, neg);
+        query_sums<KIND, 4>(a, token, h, lane & 15, lane >> 4, 4, pos, neg);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
 #pragma unroll
