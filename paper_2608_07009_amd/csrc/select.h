@@ -45,6 +45,7 @@ struct SelectArgs : BatchArgs {
   int32_t tile_size;      // candidates of a tile (log2)
   int32_t q_heads, top_k, first, last;
   int32_t cand_shift;     // tokens of a candidate (log2)
+  int32_t tokens_of_request;  // that are scored one by one, at most
 };
 
 // Chooses from the scores of the step's rows; `candidates`: the most that a row has.

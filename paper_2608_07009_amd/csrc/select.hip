@@ -15,12 +15,14 @@ namespace {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRowPad = 256;          // a row of scores is a multiple of this
-// New tokens of a request from which waves have new tokens of their own.
+// New tokens of a request from which waves have new tokens of their own; fewer are scored one by one.
 constexpr int kTeamChunk = 5;
 // Workgroups that tiles of candidates are made small for, and the least tile (log2).
 constexpr int kWantedGroups = 512, kLeastTile = 8;
+constexpr int64_t kMostGroups = (1 << 23) - 1;
 constexpr size_t kMostScoreBytes = (size_t)1 << 30;
 
 // ---- scores ----------------------------------------------------------------------------------
@@ -70,12 +72,13 @@ struct Largest {
 struct Either {
   __device__ __forceinline__ uint32_t operator()(uint32_t x, uint32_t y) const { return x | y; }
 };
+// x's halves added in the lower half of the wave, y's in the upper.
+__device__ __forceinline__ float halves(float x, float y) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
 // The totals over the four rows of 16 lanes of v0 .. v3: that of v_r in row r.
 __device__ __forceinline__ float totals(float v0, float v1, float v2, float v3) {
-  auto halves = [](float x, float y) {  // x's halves added in the lower half, y's in the upper
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
-    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-  };
   const float x = halves(v0, v2), y = halves(v1, v3);
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
@@ -113,422 +116,567 @@ __device__ __forceinline__ void linear_rows(const SelectArgs& a, int token0, int
   }
 }
 
-// What a wave scores: keys, NT new tokens of MT tiles of 16 heads each; the others, 4 MT new tokens, four of
-// three rows (and an empty one) to a tile.
-template <int KIND, int MT, int NT>
-struct Wave {
+// A tile of candidates, first .. end - 1, that a workgroup scores for new tokens of one request and kv head.
+template <int KIND>
+struct Tile {
+  static constexpr bool KEYS = Shape<KIND>::KEYS;
+  const SelectArgs& a;
+  const int32_t* table;
+  const uint8_t* index;
+  int kt, first, end;
+
+  __device__ __forceinline__ Tile(const SelectArgs& args, int q, int h, int tile, int seen)
+      : a(args),
+        table(args.table ? args.table + q * args.table_request_stride + h * args.table_head_stride : nullptr),
+        index(args.index + q * args.request_stride + h * args.head_stride),
+        kt(tile),
+        first(tile << args.tile_size),
+        end(min(first + (1 << args.tile_size), seen)) {}
+  // The table's entry for candidate j, as it is; j past the last (of [.., stop)) has the last one's.
+  __device__ __forceinline__ int entry_of(int j, int stop) const {
+    j = min(j, stop - 1);
+    const int e = KEYS ? j >> a.tpr_shift : j;
+    return table ? table[e] : e;
+  }
+  // Padding is loaded as record 0 is, and left out of everything.
+  __device__ __forceinline__ bool there(int entry, int j, int stop) const {
+    return j < stop && entry >= 0 && entry < a.num_records;
+  }
+  __device__ __forceinline__ const uint8_t* row_of(int entry, bool valid, int j) const {
+    return index + (uint64_t)(uint32_t)(valid ? entry : 0) * (uint32_t)a.record_stride +
+           (KEYS ? (j & ((1 << a.tpr_shift) - 1)) * kIndexRowBytes : 0);
+  }
+  // Whether 64 candidates from a multiple of 64 on lie in one record, one behind the other.
+  __device__ __forceinline__ bool one_record() const { return KEYS && a.tpr_shift >= 6; }
+};
+
+// The largest sum of squares of index rows (NaN stays: its bits are above infinity's), and all their bits.
+struct Norm {
+  float largest = 0.f;
+  uint32_t bits = 0;
+  __device__ __forceinline__ void add(float squares, uint32_t row_bits, bool valid) {
+    const uint32_t sq = valid ? __float_as_uint(squares) : 0;
+    largest = __uint_as_float(max(__float_as_uint(largest), sq));
+    bits |= valid ? row_bits & 0x7fff7fffu : 0;
+    // now, and not where they are used: the rows' registers are loaded again
+    asm volatile("" : "+v"(bits), "+v"(largest));
+  }
+};
+__device__ __forceinline__ uint32_t any_bits(u32x4_t x) { return x[0] | x[1] | x[2] | x[3]; }
+
+// Writes down score s of candidate j, and takes it into the least and the largest.
+__device__ __forceinline__ void put_score(float s, bool valid, float* row, int j, float& least, float& most) {
+  if (s != s) s = __uint_as_float(kNan);
+  if (valid) {
+    least = fminf(least, s);  // (NaN is passed over)
+    most = fmaxf(most, s);
+  }
+  row[j] = valid ? s : __uint_as_float(kPad);
+}
+
+// The tile's facts, of the `tokens` new tokens from token0 on. least, most: of the workgroup's token threadIdx.x.
+// The largest norm is 0 only if all rows are zero; squares below the float range are made up for.
+template <int WAVES>
+__device__ __forceinline__ void put_facts(const SelectArgs& a, int token0, int tokens, int h, int kt,
+                                          const uint32_t* norms, const uint32_t* bits, float least,
+                                          float most) {
+  if (threadIdx.x < (unsigned)tokens) {
+    uint32_t n = 0, any = 0;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      n = max(n, norms[i]);
+      any |= bits[i];
+    }
+    a.facts[((int64_t)(token0 + (int)threadIdx.x - a.row0) * a.heads + h) * a.tiles + kt] =
+        TileFacts{any ? sqrtf(__uint_as_float(n)) * 1.01f + 0x1p-58f : 0.f, least, most};
+  }
+  if (a.hist && kt == 0)  // added to by the next kernel
+    for (int i = 0; i < tokens; ++i)
+      for (int x = threadIdx.x; x < kLongBins; x += 64 * WAVES)
+        a.hist[((int64_t)(token0 + i - a.row0) * a.heads + h) * kLongBins + x] = 0;
+}
+
+// ---- one new token at a time -------------------------------------------------------------------
+
+// A operands of 16 rows: keys, MT tiles of 16 queries of a new token and their weights; the others, of the
+// sums of four new tokens (linear_rows).
+template <int KIND, int MT>
+struct Rows16 {
   using S = Shape<KIND>;
   static constexpr bool KEYS = S::KEYS;
-  static constexpr int TILES = KEYS ? MT * NT : MT, TOKENS = KEYS ? NT : 4 * MT;
-  // Sums of a lane: keys, of four values at a time (see `totals`) that are four new tokens, or fewer and
-  // several 16 candidates; the others, of the new token 4 m + group.
-  static constexpr int SETS = KEYS ? (NT + 3) / 4 : MT;
-  static constexpr int SPAN = KEYS && NT < 4 ? 64 / NT : 16;  // candidates of a lane's new token at a time
-  bf16x8_t A[TILES][S::STEPS];
-  float w[KEYS ? TILES * 4 : 1];
-  float least[SETS], most[SETS];
+  bf16x8_t A[MT][S::STEPS];
+  float w[KEYS ? MT * 4 : 1];
 
-  __device__ __forceinline__ void start() {
-#pragma unroll
-    for (int i = 0; i < SETS; ++i) {
-      least[i] = INFINITY;
-      most[i] = -INFINITY;
-    }
-  }
-  // keys: the queries of tokens token0 .. of kv head h
-  __device__ __forceinline__ void load(const SelectArgs& a, int token0, int tokens, int h) {
+  __device__ __forceinline__ void load(const SelectArgs& a, int token, int h) {  // keys
     const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
+    const uint16_t* q = a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + group * 8;
+    const float* wr = a.weights ? a.weights + ((int64_t)token * a.heads + h) * a.q_heads : nullptr;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const int64_t token = token0 + n;
-      const uint16_t* q = a.q + token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims + group * 8;
-      const float* wr = a.weights ? a.weights + (token * a.heads + h) * a.q_heads : nullptr;
+    for (int m = 0; m < MT; ++m) {
+      const int e = m * 16 + col;
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const int e = m * 16 + col;
+      for (int k = 0; k < S::STEPS; ++k) {
+        u32x4_t x = {};
+        if (e < a.q_heads) x = *reinterpret_cast<const any_u32x4_t*>(q + e * kIndexDims + k * 32);
+        A[m][k] = __builtin_bit_cast(bf16x8_t, x);
+      }
 #pragma unroll
-        for (int k = 0; k < S::STEPS; ++k) {
-          u32x4_t x = {};
-          if (n < tokens && e < a.q_heads)
-            x = *reinterpret_cast<const any_u32x4_t*>(q + e * kIndexDims + k * 32);
-          A[n * MT + m][k] = __builtin_bit_cast(bf16x8_t, x);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int y = m * 16 + group * 4 + i;
-          w[(n * MT + m) * 4 + i] = n < tokens && y < a.q_heads ? (wr ? wr[y] : 1.f) : 0.f;
-        }
+      for (int i = 0; i < 4; ++i) {
+        const int y = m * 16 + group * 4 + i;
+        w[m * 4 + i] = y < a.q_heads ? (wr ? wr[y] : 1.f) : 0.f;
       }
     }
   }
-  // the others: rows of s_a from token `first` of the workgroup's on
-  __device__ __forceinline__ void load(const uint16_t* s_a, int first) {
+  __device__ __forceinline__ void load(const uint16_t* s_a, int tile) {  // the others
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int k = 0; k < S::STEPS; ++k)
-        A[m][k] = *reinterpret_cast<const bf16x8_t*>(
-            s_a + (first * 4 + m * 16 + (lane & 15)) * (S::DIMS + 8) + k * 32 + (lane >> 4) * 8);
+    for (int k = 0; k < S::STEPS; ++k)
+      A[0][k] = *reinterpret_cast<const bf16x8_t*>(s_a + (tile * 16 + (lane & 15)) * (S::DIMS + 8) +
+                                                   k * 32 + (lane >> 4) * 8);
   }
-
-  // Products with 16 candidates' rows.
-  __device__ __forceinline__ void multiply(const u32x4_t (&x)[S::STEPS], f32x4_t (&acc)[TILES]) const {
+  // Scores of 16 candidates, x their rows: keys, this lane's four heads' share of a tile's; the others, of
+  // new token group and candidate col, whole.
+  __device__ __forceinline__ float score(const u32x4_t (&x)[S::STEPS]) const {
+    f32x4_t acc[MT];
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) acc[t] = f32x4_t{};
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4_t{};
 #pragma unroll
     for (int k = 0; k < S::STEPS; ++k)
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[t][k], __builtin_bit_cast(bf16x8_t, x[k]),
-                                                         acc[t], 0, 0, 0);
-  }
-  // Their scores: keys, this lane's share of each new token's; the others, whole.
-  __device__ __forceinline__ void add_up(const f32x4_t (&acc)[TILES], float (&v)[KEYS ? NT : MT]) const {
+      for (int m = 0; m < MT; ++m)
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A[m][k], __builtin_bit_cast(bf16x8_t, x[k]),
+                                                         acc[m], 0, 0, 0);
+    float v = 0.f;
     if constexpr (KEYS) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        v[n] = 0.f;
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            v[n] += w[(n * MT + m) * 4 + i] * positive(acc[n * MT + m][i]);
-        asm volatile("" : "+v"(v[n]));  // here, and not where it is used: the accumulators are free
-      }
-    } else {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        v[m] = acc[m][0] + acc[m][1] + acc[m][2];
-        asm volatile("" : "+v"(v[m]));
-      }
-    }
-  }
-
-  // A set's scores to memory: this lane's is candidate j's, of its new token's row.
-  __device__ __forceinline__ void put(float s, int set, float* row, int j, int end, bool valid, bool live) {
-    if (j >= end || !live) return;
-    if (s != s) s = __uint_as_float(kNan);
-    if (valid) {
-      least[set] = fminf(least[set], s);  // (NaN is passed over)
-      most[set] = fmaxf(most[set], s);
-    }
-    row[j] = valid ? s : __uint_as_float(kPad);
-  }
-  // The workgroup's new token (from the wave's first) that this lane has in a set.
-  __device__ __forceinline__ int token_of(int set) const {
-    const int row = (threadIdx.x & 63) >> 4;
-    if (!KEYS) return 4 * set + row;
-    return NT >= 4 ? 4 * set + row : NT == 2 ? row >> 1 : 0;
-  }
-  // Scores of 64 candidates base .., v[sub] of each 16, written down. out: row of the wave's first token;
-  // mask: which are not padding.
-  __device__ __forceinline__ void put64(const float (&v)[4][KEYS ? NT : MT], float* out, int64_t pitch,
-                                        int tokens, int base, int end, uint64_t mask) {
-    const int lane = threadIdx.x & 63, col = lane & 15;
-    auto one = [&](float s, int set, int at) {
-      const int t = token_of(set);
-      put(s, set, out + t * pitch, base + at, end, mask >> at & 1, t < tokens);
-    };
-    if constexpr (!KEYS) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub) one(v[sub][m], m, sub * 16 + col);
-    } else if constexpr (NT == 1) {
-      one(totals(v[0][0], v[1][0], v[2][0], v[3][0]), 0, lane);
-    } else if constexpr (NT == 2) {
+        for (int i = 0; i < 4; ++i) v += w[m * 4 + i] * positive(acc[m][i]);
+    } else {
+      v = acc[0][0] + acc[0][1] + acc[0][2];
+    }
+    asm volatile("" : "+v"(v));  // here, and not where it is used: the accumulators are free
+    return v;
+  }
+};
+
+// New token i of request q (of those with fewer than kTeamChunk), a tile of candidates: each wave has a
+// quarter of it and loads rows as operands, 32 ahead. HBM-bound from a few requests on: 32 requests of up to
+// 32768 tokens, 64 heads, 200 MB of keys in 40 us.
+template <int KIND, int MT, int OCCUPANCY>
+__global__ __launch_bounds__(256, OCCUPANCY) void score_token_kernel(SelectArgs a) {
+  using S = Shape<KIND>;
+  constexpr bool KEYS = S::KEYS;
+  constexpr int WAVES = 4, T = 64 * WAVES;
+  __shared__ __align__(16) uint16_t s_a[KEYS ? 8 : 16 * (S::DIMS + 8)];
+  __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
+  __shared__ float s_least[WAVES], s_most[WAVES];
+  const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // request and token first: workgroups of one request are far apart
+  const uint32_t per = (uint32_t)a.tokens_of_request;
+  const uint32_t n_rows = (uint32_t)a.requests * per;
+  const uint32_t rest = blockIdx.x / n_rows, row = blockIdx.x - rest * n_rows;
+  const int q = (int)(row / per), i = (int)(row - (uint32_t)q * per);
+  const int kt = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)kt * a.heads);
+  const RequestRows r = rows_of(a, q);
+  const int token = r.begin + i;
+  if (i >= r.n || r.n >= kTeamChunk || token < a.row0 || token >= a.row0 + a.rows) return;
+  const int seen = seen_at(a, r.len - r.n + i);
+  const Tile<KIND> tile(a, q, h, kt, seen);
+  if (seen <= a.top_k || tile.first >= seen) return;
+  Rows16<KIND, MT> rows;
+  if constexpr (KEYS) {
+    rows.load(a, token, h);
+  } else {
+    linear_rows<KIND, T>(a, token, 1, 4, h, s_a);
+    __syncthreads();
+    rows.load(s_a, 0);
+  }
+  float* out = a.scores + ((int64_t)(token - a.row0) * a.heads + h) * a.row_pad;
+  float least = INFINITY, most = -INFINITY;
+  Norm norm;
+  const int share = (1 << a.tile_size) / WAVES;
+  const int from = tile.first + wave * share, to = min(from + share, tile.end);
+  if (from < to) {
+    const bool one_record = tile.one_record();
+    auto fetch = [&](u32x4_t (&y)[S::STEPS], int entries, int base, int sub) {
+      const uint8_t* x;
+      if (one_record) {
+        const int e = __builtin_amdgcn_readfirstlane(entries);
+        x = tile.row_of(e, tile.there(e, base, to), base + sub * 16) + col * kIndexRowBytes;
+      } else {
+        const int j = base + sub * 16 + col, e = __shfl(entries, sub * 16 + col);
+        x = tile.row_of(e, tile.there(e, j, to), min(j, to - 1));
+      }
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-        one(totals(v[2 * x][0], v[2 * x + 1][0], v[2 * x][1], v[2 * x + 1][1]), 0, x * 32 + (lane & 31));
+      for (int k = 0; k < S::STEPS; ++k)
+        y[k] = *reinterpret_cast<const u32x4_t*>(x + k * 64 + group * 16);
+    };
+    u32x4_t x[2][S::STEPS];  // two times 16 candidates, the next ones on their way
+    int entry = tile.entry_of(from + lane, to);      // of candidate base + lane
+    int next = tile.entry_of(from + 64 + lane, to);  // and of the next step's
+    fetch(x[0], entry, from, 0);
+    fetch(x[1], entry, from, 1);
+#pragma unroll 1
+    for (int base = from; base < to; base += 64) {
+      const uint64_t mask = __ballot(tile.there(entry, base + lane, to));
+      const int after = tile.entry_of(base + 128 + lane, to);
+      float v[4];
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub) {
+        float sq = 0.f;
+        uint32_t bits = 0;
+#pragma unroll
+        for (int k = 0; k < S::STEPS; ++k) {
+          bits |= any_bits(x[sub & 1][k]);
+          sq = squares(x[sub & 1][k], sq);
+        }
+        sq += __shfl_xor(sq, 16);
+        sq += __shfl_xor(sq, 32);
+        norm.add(sq, bits, mask >> (sub * 16 + col) & 1);
+        v[sub] = rows.score(x[sub & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        // (past the end: the last candidate again)
+        if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);
+        else fetch(x[sub & 1], next, base + 64, sub - 2);
+      }
+      // keys: a lane has candidate base + lane; the others: the first 16 lanes have the new token's
+      if constexpr (KEYS) {
+        const float s = totals(v[0], v[1], v[2], v[3]);
+        if (base + lane < to) put_score(s, mask >> lane & 1, out, base + lane, least, most);
+      } else {
+#pragma unroll
+        for (int sub = 0; sub < 4; ++sub) {
+          const int at = sub * 16 + col;
+          if (group == 0 && base + at < to)
+            put_score(v[sub], mask >> at & 1, out, base + at, least, most);
+        }
+      }
+      entry = next;
+      next = after;
+    }
+  }
+  const uint32_t nb = wave_reduce(__float_as_uint(norm.largest), 0u, Largest());
+  const uint32_t bits = wave_reduce(norm.bits, 0u, Either());
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    least = fminf(least, __shfl_xor(least, d));
+    most = fmaxf(most, __shfl_xor(most, d));
+  }
+  if (lane == 0) {
+    s_norm[wave] = nb;
+    s_bits[wave] = bits;
+    s_least[wave] = least;
+    s_most[wave] = most;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < WAVES; ++x) {
+    least = fminf(least, s_least[x]);
+    most = fmaxf(most, s_most[x]);
+  }
+  put_facts<WAVES>(a, token, 1, h, kt, s_norm, s_bits, least, most);
+}
+
+// ---- chunks of new tokens ----------------------------------------------------------------------
+
+// The workgroup's candidates, 64 at a time, on their way from memory to one of two buffers in LDS by way of
+// registers. Thread t has piece t % PIECES of rows t / PIECES + i * (T / PIECES); piece p of row r lies in
+// slot p ^ (r & 15), so that 16 rows' pieces p are in 16 slots of the banks.
+template <int KIND, int T>
+struct Stage {
+  static constexpr int P = Shape<KIND>::PIECES, LOADS = 64 * P / T, BYTES = 64 * P * 16;
+  const Tile<KIND>& tile;
+  u32x4_t x[LOADS];
+  uint64_t mask;  // which of the 64 are not padding
+  int entry;      // of candidate base + lane of the next 64
+  Norm norm;
+
+  __device__ __forceinline__ explicit Stage(const Tile<KIND>& t) : tile(t) {
+    entry = tile.entry_of(tile.first + (threadIdx.x & 63), tile.end);
+  }
+  __device__ __forceinline__ void fetch(int base) {
+    const int lane = threadIdx.x & 63, piece = threadIdx.x % P;
+    mask = __ballot(tile.there(entry, base + lane, tile.end));
+    if (tile.one_record()) {
+      const uint8_t* from = tile.row_of(__builtin_amdgcn_readfirstlane(entry), mask & 1, base);
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i)
+        x[i] = *reinterpret_cast<const u32x4_t*>(from + (threadIdx.x + i * T) * 16);
     } else {
 #pragma unroll
-      for (int set = 0; set < SETS; ++set)
+      for (int i = 0; i < LOADS; ++i) {
+        const int row = threadIdx.x / P + i * (T / P), e = __shfl(entry, row);
+        x[i] = *reinterpret_cast<const u32x4_t*>(tile.row_of(e, mask >> row & 1, base + row) + piece * 16);
+      }
+    }
+    entry = tile.entry_of(base + 64 + lane, tile.end);
+  }
+  __device__ __forceinline__ void store(uint8_t* buf) {
+    const int piece = threadIdx.x % P;
 #pragma unroll
-        for (int sub = 0; sub < 4; ++sub)
-          one(totals(v[sub][4 * set], v[sub][4 * set + 1], v[sub][4 * set + 2], v[sub][4 * set + 3]),
-              set, sub * 16 + col);
+    for (int i = 0; i < LOADS; ++i) {
+      const int row = threadIdx.x / P + i * (T / P);
+      *reinterpret_cast<u32x4_t*>(buf + row * (P * 16) + ((piece ^ (row & 15)) << 4)) = x[i];
+      float sq = sum16(squares(x[i], 0.f));
+      if (P == 32) sq += __shfl_xor(sq, 16);
+      norm.add(sq, any_bits(x[i]), mask >> row & 1);
     }
   }
 };
 
-// The table's entry for candidate j of [0, end), as it is; j past the end has the last one's.
-template <bool KEYS>
-__device__ __forceinline__ int entry_of(const SelectArgs& a, const int32_t* table, int j, int end) {
-  j = min(j, end - 1);
-  const int e = KEYS ? j >> a.tpr_shift : j;
-  return table ? table[e] : e;
-}
+// Keys: the queries of TOKENS new tokens as 32-row A operands, HEADS rows each (16, 32, 64 or 128).
+template <int HEADS>
+struct Rows32 {
+  static constexpr int TILES = HEADS == 128 ? 4 : 2, TOKENS = 32 * TILES / HEADS, STEPS = kIndexDims / 16;
+  bf16x8_t A[TILES][STEPS];
+  float w[TILES][16];
 
-// ROWS new tokens of a workgroup (of one or more requests, one after the other), a tile of candidates.
-//
-// TEAM: the waves have new tokens of their own and the same candidates, 64 at a time by way of LDS, the next
-// 64 on their way in registers meanwhile. Otherwise, and where there are no more new tokens than one wave
-// has, each wave has a quarter of the candidates and loads them as operands.
-template <int KIND, int MT, int NT, int WAVES, bool TEAM, int OCCUPANCY>
-__global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_kernel(SelectArgs a) {
-  using S = Shape<KIND>;
-  using W = Wave<KIND, MT, NT>;
-  constexpr bool KEYS = S::KEYS;
-  constexpr int T = 64 * WAVES, ROWS = TEAM ? WAVES * W::TOKENS : 1;
-  constexpr int LOADS = 64 * S::PIECES / T;  // of a thread, for 64 rows
-  constexpr int A_ROWS = KEYS ? 0 : MT * (TEAM ? WAVES : 1);  // tiles
-  constexpr int TILE_BYTES = 64 * S::DIMS * 2, A_BYTES = 16 * A_ROWS * (S::DIMS + 8) * 2;
-  __shared__ __align__(16) uint8_t s_mem[std::max(TEAM ? 2 * TILE_BYTES : 16, A_BYTES)];
+  // The row of a tile that accumulator i of this lane has.
+  static __device__ __forceinline__ int row_of(int i) {
+    return 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5) + (i & 3);
+  }
+  __device__ __forceinline__ void load(const SelectArgs& a, int token0, int live, int h) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const int row = t * 32 + (lane & 31), n = row / HEADS, e = row % HEADS;
+      const bool there = n < live && e < a.q_heads;
+      const uint16_t* q = a.q + (int64_t)(token0 + n) * a.q_stride +
+                          ((int64_t)h * a.q_heads + e) * kIndexDims + (lane >> 5) * 8;
+#pragma unroll
+      for (int k = 0; k < STEPS; ++k) {
+        u32x4_t x = {};
+        if (there) x = *reinterpret_cast<const any_u32x4_t*>(q + k * 16);
+        A[t][k] = __builtin_bit_cast(bf16x8_t, x);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int y = t * 32 + row_of(i), m = y / HEADS, f = y % HEADS;
+        float x = 0.f;
+        if (m < live && f < a.q_heads)
+          x = a.weights ? a.weights[((int64_t)(token0 + m) * a.heads + h) * a.q_heads + f] : 1.f;
+        w[t][i] = x;
+      }
+    }
+  }
+  // Tile t's products with 32 candidates.
+  __device__ __forceinline__ f32x16_t multiply(int t, const u32x4_t (&x)[STEPS]) const {
+    f32x16_t acc = {};
+#pragma unroll
+    for (int k = 0; k < STEPS; ++k)
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(A[t][k], __builtin_bit_cast(bf16x8_t, x[k]), acc, 0,
+                                                    0, 0);
+    return acc;
+  }
+  // What they add to this lane's share (half of the heads) of its new tokens' scores.
+  __device__ __forceinline__ void add_up(int t, const f32x16_t& acc, float (&v)[TOKENS]) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      v[(t * 32 + 8 * (i >> 2)) / HEADS] += w[t][i] * positive(acc[i]);
+#pragma unroll
+    for (int n = 0; n < TOKENS; ++n) asm volatile("" : "+v"(v[n]));
+  }
+};
+
+// WAVES times Rows32::TOKENS new tokens (of one or more requests that have kTeamChunk or more, one after the
+// other), a tile of candidates: each wave has new tokens of its own, all have the same candidates, 64 at a
+// time in LDS. The products of 32 candidates with one tile of queries run beside the sums of those before.
+template <int HEADS, int WAVES, int OCCUPANCY>
+__global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(SelectArgs a) {
+  constexpr int KIND = HISPARSE_INDEX_KEYS, T = 64 * WAVES;
+  using R = Rows32<HEADS>;
+  using St = Stage<KIND, T>;
+  constexpr int ROWS = WAVES * R::TOKENS;
+  __shared__ __align__(16) uint8_t s_mem[2 * St::BYTES];
   __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
-  __shared__ float s_least[WAVES][W::TOKENS], s_most[WAVES][W::TOKENS];
-  const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
+  __shared__ float s_least[ROWS], s_most[ROWS];
+  const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const uint32_t block = blockIdx.x, rest = block / (uint32_t)a.tiles;
-  const int kt = (int)(block - rest * (uint32_t)a.tiles);
-  const int tile = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)tile * a.heads);
-  const int row0 = a.row0 + tile * ROWS, row1 = min(row0 + ROWS, a.row0 + a.rows);
+  const uint32_t rest = blockIdx.x / (uint32_t)a.tiles;
+  const int kt = (int)(blockIdx.x - rest * (uint32_t)a.tiles);
+  const int row_tile = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)row_tile * a.heads);
+  const int row0 = a.row0 + row_tile * ROWS, row1 = min(row0 + ROWS, a.row0 + a.rows);
 #pragma unroll 1
   for (int t = row0; t < row1;) {
     const int q = request_at(a, t);
     const RequestRows r = rows_of(a, q);
     if (t < r.begin || t >= r.begin + r.n) {
-      if (ROWS == 1) return;
       ++t;
       continue;
     }
     const int token0 = t, tokens = min(row1, r.begin + r.n) - t;
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
-    const int first = kt << a.tile_size, end = min(first + (1 << a.tile_size), seen);
-    if (seen <= a.top_k || first >= seen) {
-      if (ROWS == 1) return;
-      continue;
-    }
-    const bool team = TEAM && tokens > W::TOKENS;
-    const int mine = team ? wave * W::TOKENS : 0;      // this wave's first new token
-    const int live = min(tokens - mine, W::TOKENS);    // and how many it has (0 or less: none)
-    const int32_t* table =
-        a.table ? a.table + q * a.table_request_stride + h * a.table_head_stride : nullptr;
-    const uint8_t* index = a.index + q * a.request_stride + h * a.head_stride;
-    // Padding is loaded as record 0 is, and left out of everything.
-    auto there = [&](int entry, int j, int stop) {
-      return j < stop && entry >= 0 && entry < a.num_records;
-    };
-    auto row_of = [&](int entry, bool valid, int j) {
-      return index + (uint64_t)(uint32_t)(valid ? entry : 0) * (uint32_t)a.record_stride +
-             (KEYS ? (j & ((1 << a.tpr_shift) - 1)) * kIndexRowBytes : 0);
-    };
-    // 64 candidates from a multiple of 64 on that lie in one record, one behind the other
-    const bool one_record = KEYS && a.tpr_shift >= 6;
-    W wv;
-    wv.start();
-    if constexpr (KEYS) {
-      wv.load(a, token0 + mine, live, h);
-    } else {
-      __syncthreads();  // what the last segment kept here is read
-      linear_rows<KIND, T>(a, token0, tokens, 4 * A_ROWS, h, reinterpret_cast<uint16_t*>(s_mem));
-      __syncthreads();
-      wv.load(reinterpret_cast<const uint16_t*>(s_mem), mine);
-      if (TEAM) __syncthreads();
-    }
+    const Tile<KIND> tile(a, q, h, kt, seen);
+    if (r.n < kTeamChunk || seen <= a.top_k || tile.first >= seen) continue;
+    const int mine = wave * R::TOKENS;                     // this wave's first new token
+    const int live = min(tokens - mine, (int)R::TOKENS);  // and how many it has (0 or less: none)
+    R rows;
+    rows.load(a, token0 + mine, live, h);
     const int64_t pitch = a.heads * a.row_pad;
     float* out = a.scores + ((int64_t)(token0 + mine - a.row0) * a.heads + h) * a.row_pad;
-    float norm = 0.f;  // the largest sum of squares; NaN stays (its bits are above infinity's)
-    uint32_t bits = 0;
-    auto larger = [&](float sq) {
-      norm = __uint_as_float(max(__float_as_uint(norm), __float_as_uint(sq)));
-    };
-    if (team) {
-      // thread t: piece t % PIECES of rows t / PIECES + i * (T / PIECES); piece p of row r lies in slot
-      // p ^ (r & 15), so that 16 rows' pieces p are in 16 slots of the banks
-      constexpr int P = S::PIECES;
-      const int piece = threadIdx.x % P, row_first = threadIdx.x / P;
-      int entry = entry_of<KEYS>(a, table, first + lane, end);  // of candidate base + lane, one step ahead
-      u32x4_t x[LOADS];
-      uint64_t mask;  // which of 64 candidates are not padding
-      auto fetch = [&](int base) {
-        mask = __ballot(there(entry, base + lane, end));
-        if (one_record) {
-          const uint8_t* from = row_of(__builtin_amdgcn_readfirstlane(entry), mask & 1, base);
+    float least[R::TOKENS], most[R::TOKENS];
 #pragma unroll
-          for (int i = 0; i < LOADS; ++i)
-            x[i] = *reinterpret_cast<const u32x4_t*>(from + (threadIdx.x + i * T) * 16);
-        } else
+    for (int n = 0; n < R::TOKENS; ++n) {
+      least[n] = INFINITY;
+      most[n] = -INFINITY;
+    }
+    St stage(tile);
+    stage.fetch(tile.first);
+    stage.store(s_mem);
+    __syncthreads();
+    int cur = 0;
+#pragma unroll 1
+    for (int base = tile.first; base < tile.end; base += 64) {
+      const uint64_t mask = stage.mask;
+      if (base + 64 < tile.end) stage.fetch(base + 64);
+      if (live > 0) {
+        float v[2][R::TOKENS] = {};
+        u32x4_t y[2][R::STEPS];
+        f32x16_t acc[2];
+        auto read = [&](int g) {
+          const int row = g * 32 + (lane & 31);
+          const uint8_t* at = s_mem + cur * St::BYTES + row * kIndexRowBytes;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          const int row = row_first + i * (T / P), e = __shfl(entry, row);
-          x[i] = *reinterpret_cast<const u32x4_t*>(row_of(e, mask >> row & 1, base + row) + piece * 16);
+          for (int k = 0; k < R::STEPS; ++k)
+            y[g][k] = *reinterpret_cast<const u32x4_t*>(at + (((k * 2 + (lane >> 5)) ^ (row & 15)) << 4));
+        };
+        read(0);
+#pragma unroll
+        for (int u = 0; u < 2 * R::TILES; ++u) {
+          if (u == R::TILES - 1) read(1);
+          acc[u & 1] = rows.multiply(u % R::TILES, y[u / R::TILES]);
+          if (u > 0) rows.add_up((u - 1) % R::TILES, acc[(u - 1) & 1], v[(u - 1) / R::TILES]);
+#pragma unroll
+          for (int i = 0; i < R::STEPS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // an MFMA
+            __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);  // four vector instructions
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-        entry = entry_of<KEYS>(a, table, base + 64 + lane, end);
-      };
-      auto store = [&](uint8_t* buf) {
+        rows.add_up(R::TILES - 1, acc[1], v[1]);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          const int row = row_first + i * (T / P);
-          const bool valid = mask >> row & 1;
-          *reinterpret_cast<u32x4_t*>(buf + row * (P * 16) + ((piece ^ (row & 15)) << 4)) = x[i];
-          // the largest of this piece; over the row's pieces they are added up at the end, which is no less
-          // than the largest row
-          bits |= valid ? (x[i][0] | x[i][1] | x[i][2] | x[i][3]) & 0x7fff7fffu : 0;
-          larger(valid ? squares(x[i], 0.f) : 0.f);
-          asm volatile("" : "+v"(bits), "+v"(norm));
+        for (int n = 0; n < R::TOKENS; ++n) {
+          const float s = halves(v[0][n], v[1][n]);
+          if (n < live && base + lane < tile.end)
+            put_score(s, mask >> lane & 1, out + n * pitch, base + lane, least[n], most[n]);
         }
-      };
-      fetch(first);
-      store(s_mem);
+      }
+      cur ^= 1;
+      if (base + 64 < tile.end) stage.store(s_mem + cur * St::BYTES);
       __syncthreads();
-      int cur = 0;
-#pragma unroll 1
-      for (int base = first; base < end; base += 64) {
-        const uint64_t now = mask;
-        if (base + 64 < end) fetch(base + 64);
-        if (live > 0) {
-          // the products of 16 candidates while those of the 16 before are added up
-          float v[4][KEYS ? NT : MT];
-          u32x4_t y[2][S::STEPS];
-          f32x4_t acc[2][W::TILES];
-          auto read = [&](int sub) {
-            const uint8_t* row = s_mem + cur * TILE_BYTES + (sub * 16 + col) * (P * 16);
-#pragma unroll
-            for (int k = 0; k < S::STEPS; ++k)
-              y[sub & 1][k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
-          };
-          read(0);
-#pragma unroll
-          for (int sub = 0; sub < 4; ++sub) {
-            if (sub < 3) read(sub + 1);
-            wv.multiply(y[sub & 1], acc[sub & 1]);
-            if (sub > 0) wv.add_up(acc[(sub - 1) & 1], v[sub - 1]);
-            if (KEYS)
-#pragma unroll
-              for (int i = 0; i < W::TILES * S::STEPS; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // an MFMA
-                __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);  // two vector instructions
-              }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-          wv.add_up(acc[1], v[3]);
-          wv.put64(v, out, pitch, live, base, end, now);
-        }
-        cur ^= 1;
-        if (base + 64 < end) store(s_mem + cur * TILE_BYTES);
-        __syncthreads();
-      }
-    } else {
-      const int share = (1 << a.tile_size) / WAVES;
-      const int from = first + wave * share, to = min(from + share, end);
-      u32x4_t x[2][S::STEPS];  // two times 16 candidates, the next ones on their way
-      int entry = 0, next = 0;  // of candidate base + lane, and of the next step's
-      auto fetch = [&](u32x4_t (&y)[S::STEPS], int entries, int base, int sub) {
-        const uint8_t* row;
-        if (one_record) {
-          const int e = __builtin_amdgcn_readfirstlane(entries);
-          row = row_of(e, there(e, base, to), base + sub * 16) + col * kIndexRowBytes + group * 16;
-        } else {
-          const int j = base + sub * 16 + col, e = __shfl(entries, sub * 16 + col);
-          row = row_of(e, there(e, j, to), min(j, to - 1)) + group * 16;
-        }
-#pragma unroll
-        for (int k = 0; k < S::STEPS; ++k) y[k] = *reinterpret_cast<const u32x4_t*>(row + k * 64);
-      };
-      if (from < to) {
-        entry = entry_of<KEYS>(a, table, from + lane, to);
-        next = entry_of<KEYS>(a, table, from + 64 + lane, to);
-        fetch(x[0], entry, from, 0);
-        fetch(x[1], entry, from, 1);
-#pragma unroll 1
-        for (int base = from; base < to; base += 64) {
-          const uint64_t mask = __ballot(there(entry, base + lane, to));
-          const int after = entry_of<KEYS>(a, table, base + 128 + lane, to);
-          float v[4][KEYS ? NT : MT];
-#pragma unroll
-          for (int sub = 0; sub < 4; ++sub) {
-            float sq = 0.f;
-            uint32_t any = 0;
-#pragma unroll
-            for (int k = 0; k < S::STEPS; ++k) {
-              const u32x4_t y = x[sub & 1][k];
-              any |= (y[0] | y[1] | y[2] | y[3]) & 0x7fff7fffu;
-              sq = squares(y, sq);
-            }
-            sq += __shfl_xor(sq, 16);
-            sq += __shfl_xor(sq, 32);
-            const bool valid = mask >> (sub * 16 + col) & 1;
-            larger(valid ? sq : 0.f);
-            bits |= valid ? any : 0;
-            asm volatile("" : "+v"(bits), "+v"(norm));  // now: the operands' registers are loaded again
-            f32x4_t acc[W::TILES];
-            wv.multiply(x[sub & 1], acc);
-            wv.add_up(acc, v[sub]);
-            __builtin_amdgcn_sched_barrier(0);
-            // (past the end: the last candidate again)
-            if (sub < 2) fetch(x[sub & 1], entry, base, sub + 2);
-            else fetch(x[sub & 1], next, base + 64, sub - 2);
-          }
-          wv.put64(v, out, pitch, live, base, to, mask);
-          entry = next;
-          next = after;
-        }
-      }
     }
-    // The tile's facts. The largest norm is 0 only if all rows are zero; squares below the float range are
-    // made up for.
-    if (team) {
-      norm = sum16(norm);
-      if (S::PIECES == 32) norm += __shfl_xor(norm, 16);
-    }
-    const uint32_t nb = wave_reduce(__float_as_uint(norm), 0u, Largest());
-    bits = wave_reduce(bits, 0u, Either());
+    const uint32_t nb = wave_reduce(__float_as_uint(stage.norm.largest), 0u, Largest());
+    const uint32_t bits = wave_reduce(stage.norm.bits, 0u, Either());
     if (lane == 0) {
       s_norm[wave] = nb;
       s_bits[wave] = bits;
     }
 #pragma unroll
-    for (int set = 0; set < W::SETS; ++set) {  // over the lanes that have the same new token
-      float lo = least16(wv.least[set]), hi = -least16(-wv.most[set]);
-      if (KEYS && NT <= 2) {
-        lo = fminf(lo, __shfl_xor(lo, 16));
-        hi = fmaxf(hi, __shfl_xor(hi, 16));
+    for (int n = 0; n < R::TOKENS; ++n) {
+#pragma unroll
+      for (int d = 1; d < 64; d *= 2) {
+        least[n] = fminf(least[n], __shfl_xor(least[n], d));
+        most[n] = fmaxf(most[n], __shfl_xor(most[n], d));
       }
-      if (KEYS && NT == 1) {
-        lo = fminf(lo, __shfl_xor(lo, 32));
-        hi = fmaxf(hi, __shfl_xor(hi, 32));
-      }
-      if (col == 0) {
-        s_least[wave][wv.token_of(set)] = lo;
-        s_most[wave][wv.token_of(set)] = hi;
+      if (lane == 0) {
+        s_least[mine + n] = least[n];
+        s_most[mine + n] = most[n];
       }
     }
     __syncthreads();
-    if (threadIdx.x < (unsigned)tokens) {
-      uint32_t n = 0, any = 0;
-#pragma unroll
-      for (int i = 0; i < WAVES; ++i) {
-        n = max(n, s_norm[i]);
-        any |= s_bits[i];
-      }
-      float least = INFINITY, most = -INFINITY;
-      if (team) {
-        least = s_least[threadIdx.x / W::TOKENS][threadIdx.x % W::TOKENS];
-        most = s_most[threadIdx.x / W::TOKENS][threadIdx.x % W::TOKENS];
-      } else {
-#pragma unroll
-        for (int i = 0; i < WAVES; ++i) {
-          least = fminf(least, s_least[i][threadIdx.x]);
-          most = fmaxf(most, s_most[i][threadIdx.x]);
-        }
-      }
-      a.facts[((int64_t)(token0 + (int)threadIdx.x - a.row0) * a.heads + h) * a.tiles + kt] =
-          TileFacts{any ? sqrtf(__uint_as_float(n)) * 1.01f + 0x1p-58f : 0.f, least, most};
+    put_facts<WAVES>(a, token0, tokens, h, kt, s_norm, s_bits, s_least[threadIdx.x % ROWS],
+                     s_most[threadIdx.x % ROWS]);
+    __syncthreads();
+  }
+}
+
+// The same for bounds and means, four new tokens a wave.
+template <int KIND>
+__global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a) {
+  using S = Shape<KIND>;
+  constexpr int WAVES = 4, T = 64 * WAVES, TOKENS = 4, ROWS = WAVES * TOKENS;
+  using St = Stage<KIND, T>;
+  constexpr int A_BYTES = 16 * WAVES * (S::DIMS + 8) * 2;
+  __shared__ __align__(16) uint8_t s_mem[std::max(2 * St::BYTES, A_BYTES)];
+  __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
+  __shared__ float s_least[ROWS], s_most[ROWS];
+  const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t rest = blockIdx.x / (uint32_t)a.tiles;
+  const int kt = (int)(blockIdx.x - rest * (uint32_t)a.tiles);
+  const int row_tile = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)row_tile * a.heads);
+  const int row0 = a.row0 + row_tile * ROWS, row1 = min(row0 + ROWS, a.row0 + a.rows);
+#pragma unroll 1
+  for (int t = row0; t < row1;) {
+    const int q = request_at(a, t);
+    const RequestRows r = rows_of(a, q);
+    if (t < r.begin || t >= r.begin + r.n) {
+      ++t;
+      continue;
     }
-    if (a.hist && kt == 0)  // added to by the next kernel
-      for (int i = 0; i < tokens; ++i)
-        for (int x = threadIdx.x; x < kLongBins; x += T)
-          a.hist[((int64_t)(token0 + i - a.row0) * a.heads + h) * kLongBins + x] = 0;
-    if (ROWS == 1) return;
+    const int token0 = t, tokens = min(row1, r.begin + r.n) - t;
+    t += tokens;
+    const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
+    const Tile<KIND> tile(a, q, h, kt, seen);
+    if (r.n < kTeamChunk || seen <= a.top_k || tile.first >= seen) continue;
+    Rows16<KIND, 1> rows;
+    linear_rows<KIND, T>(a, token0, tokens, ROWS, h, reinterpret_cast<uint16_t*>(s_mem));
+    __syncthreads();
+    rows.load(reinterpret_cast<const uint16_t*>(s_mem), wave);
+    __syncthreads();
+    const int mine = wave * TOKENS + group;  // this lane's new token
+    float* out = a.scores + ((int64_t)(token0 + mine - a.row0) * a.heads + h) * a.row_pad;
+    float least = INFINITY, most = -INFINITY;
+    St stage(tile);
+    stage.fetch(tile.first);
+    stage.store(s_mem);
+    __syncthreads();
+    int cur = 0;
+#pragma unroll 1
+    for (int base = tile.first; base < tile.end; base += 64) {
+      const uint64_t mask = stage.mask;
+      if (base + 64 < tile.end) stage.fetch(base + 64);
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub) {
+        u32x4_t y[S::STEPS];
+        const int at = sub * 16 + col;
+        const uint8_t* row = s_mem + cur * St::BYTES + at * (S::PIECES * 16);
+#pragma unroll
+        for (int k = 0; k < S::STEPS; ++k)
+          y[k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
+        const float s = rows.score(y);
+        if (mine < tokens && base + at < tile.end)
+          put_score(s, mask >> at & 1, out, base + at, least, most);
+      }
+      cur ^= 1;
+      if (base + 64 < tile.end) stage.store(s_mem + cur * St::BYTES);
+      __syncthreads();
+    }
+    const uint32_t nb = wave_reduce(__float_as_uint(stage.norm.largest), 0u, Largest());
+    const uint32_t bits = wave_reduce(stage.norm.bits, 0u, Either());
+    least = least16(least);
+    most = -least16(-most);
+    if (lane == 0) {
+      s_norm[wave] = nb;
+      s_bits[wave] = bits;
+    }
+    if (col == 0) {
+      s_least[mine] = least;
+      s_most[mine] = most;
+    }
+    __syncthreads();
+    put_facts<WAVES>(a, token0, tokens, h, kt, s_norm, s_bits, s_least[threadIdx.x % ROWS],
+                     s_most[threadIdx.x % ROWS]);
     __syncthreads();
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------
 
-// New tokens of a workgroup of score_kernel.
+// New tokens of a workgroup that has a chunk's.
 int team_rows(int kind, int q_heads) {
   if (kind != HISPARSE_INDEX_KEYS) return 16;
   return q_heads <= 16 ? 32 : q_heads <= 32 ? 16 : q_heads <= 64 ? 8 : 4;
@@ -538,7 +686,9 @@ struct SelectPlan {
   int64_t candidates, row_pad, tiles, parts;
   bool is_long;
   int64_t row_bytes;  // of a new token, all kv heads
+  int64_t token_rows;  // workgroups of single tokens, for each tile
   int32_t tile_size;
+  bool team;          // chunks of kTeamChunk or more new tokens can occur
 };
 
 int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -550,13 +700,18 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
   p.candidates = keys ? (int64_t)b.max_records * b.tokens_per_record : b.max_records;
   // The largest tiles of which there are enough: a workgroup first loads its queries. (512 new tokens x 64
   // heads over 32768 keys: scores and choice in 321 us with 512 of them, 331 with 1024.)
-  const bool team = b.max_chunk >= kTeamChunk;
+  p.team = b.max_chunk >= kTeamChunk;
   const int64_t row_tiles =
-      whole(b.total_tokens, team ? team_rows(x.kind, d.q_heads) : 1) * b.kv_heads;
-  p.tile_size = !keys ? 9 : team ? 12 : 11;
+      (p.team ? whole(b.total_tokens, team_rows(x.kind, d.q_heads))
+              : std::min<int64_t>(b.total_tokens, (int64_t)b.num_requests * b.max_chunk)) * b.kv_heads;
+  p.tile_size = !keys ? 9 : p.team ? 12 : 11;
   while (p.tile_size > kLeastTile &&
          row_tiles * whole(p.candidates, 1 << p.tile_size) < kWantedGroups)
     --p.tile_size;
+  // (a launch's workgroups are counted in 32 bits, with all their threads)
+  p.token_rows = (int64_t)b.num_requests * std::min(b.max_chunk, kTeamChunk - 1) * b.kv_heads;
+  while (p.tile_size < 30 && p.token_rows * whole(p.candidates, 1 << p.tile_size) > kMostGroups)
+    ++p.tile_size;
   p.tiles = whole(p.candidates, 1 << p.tile_size);
   p.parts = whole(p.candidates, kPart);
   const bool big = p.candidates > kRegisterRow;
@@ -569,33 +724,43 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
   return p;
 }
 
-template <int KIND, int MT, int NT, int WAVES, bool TEAM, int OCCUPANCY>
-void launch_score(const SelectArgs& a, hipStream_t s) {
-  constexpr int ROWS = TEAM ? WAVES * Wave<KIND, MT, NT>::TOKENS : 1;
+template <int KIND, int MT, int OCCUPANCY>
+void launch_tokens(const SelectArgs& a, const SelectPlan& p, hipStream_t s) {
+  hipLaunchKernelGGL((score_token_kernel<KIND, MT, OCCUPANCY>), dim3((unsigned)(p.token_rows * p.tiles)),
+                     dim3(256), 0, s, a);
+}
+template <int HEADS, int WAVES, int OCCUPANCY>
+void launch_keys(const SelectArgs& a, hipStream_t s) {
+  constexpr int ROWS = WAVES * Rows32<HEADS>::TOKENS;
   const unsigned row_tiles = (unsigned)((a.rows + ROWS - 1) / ROWS);
-  hipLaunchKernelGGL((score_kernel<KIND, MT, NT, WAVES, TEAM, OCCUPANCY>),
+  hipLaunchKernelGGL((score_keys_kernel<HEADS, WAVES, OCCUPANCY>),
                      dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), dim3(64 * WAVES), 0, s, a);
+}
+template <int KIND>
+void launch_rows(const SelectArgs& a, hipStream_t s) {
+  const unsigned row_tiles = (unsigned)((a.rows + 15) / 16);
+  hipLaunchKernelGGL(score_rows_kernel<KIND>,
+                     dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), dim3(256), 0, s, a);
 }
 
 hipError_t launch_select(const SelectArgs& a, int kind, const SelectPlan& p, hipStream_t s) {
   constexpr int K = HISPARSE_INDEX_KEYS, B = HISPARSE_INDEX_BOUNDS, M = HISPARSE_INDEX_MEANS;
-  const bool team = a.max_chunk >= kTeamChunk;
-  if (kind == B) {
-    if (team) launch_score<B, 1, 1, 4, true, 2>(a, s);
-    else launch_score<B, 1, 1, 4, false, 2>(a, s);
-  } else if (kind == M) {
-    if (team) launch_score<M, 1, 1, 4, true, 2>(a, s);
-    else launch_score<M, 1, 1, 4, false, 2>(a, s);
-  } else if (team) {
-    if (a.q_heads <= 16) launch_score<K, 1, 4, 8, true, 2>(a, s);
-    else if (a.q_heads <= 32) launch_score<K, 2, 2, 8, true, 2>(a, s);
-    else if (a.q_heads <= 64) launch_score<K, 4, 1, 8, true, 2>(a, s);
-    else launch_score<K, 8, 1, 4, true, 1>(a, s);
-  } else {
-    if (a.q_heads <= 16) launch_score<K, 1, 1, 4, false, 3>(a, s);
-    else if (a.q_heads <= 32) launch_score<K, 2, 1, 4, false, 3>(a, s);
-    else if (a.q_heads <= 64) launch_score<K, 4, 1, 4, false, 2>(a, s);
-    else launch_score<K, 8, 1, 4, false, 1>(a, s);
+  const bool tokens = a.start || !p.team;  // (without starts all chunks are max_chunk)
+  if (tokens) {
+    if (kind == B) launch_tokens<B, 1, 2>(a, p, s);
+    else if (kind == M) launch_tokens<M, 1, 2>(a, p, s);
+    else if (a.q_heads <= 16) launch_tokens<K, 1, 3>(a, p, s);
+    else if (a.q_heads <= 32) launch_tokens<K, 2, 3>(a, p, s);
+    else if (a.q_heads <= 64) launch_tokens<K, 4, 3>(a, p, s);
+    else launch_tokens<K, 8, 1>(a, p, s);
+  }
+  if (p.team) {
+    if (kind == B) launch_rows<B>(a, s);
+    else if (kind == M) launch_rows<M>(a, s);
+    else if (a.q_heads <= 16) launch_keys<16, 8, 2>(a, s);
+    else if (a.q_heads <= 32) launch_keys<32, 8, 2>(a, s);
+    else if (a.q_heads <= 64) launch_keys<64, 8, 2>(a, s);
+    else launch_keys<128, 4, 1>(a, s);
   }
   return launch_choose(a, kind, p.candidates, s);
 }
@@ -673,7 +838,7 @@ hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* x,
   if (step > most) step = most;
   if (step > most_chosen) step = most_chosen;
   if (step > b->total_tokens) step = b->total_tokens;
-  if (step < 1) return HISPARSE_ERR_UNSUPPORTED;
+  if (step < 1 || p.token_rows * p.tiles > kMostGroups) return HISPARSE_ERR_UNSUPPORTED;
   SelectArgs a{};
   static_cast<BatchArgs&>(a) = batch_args(*b, d_table, d_chunk_start, d_kv_len);
   a.index = reinterpret_cast<const uint8_t*>(d_index);
@@ -696,6 +861,7 @@ hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* x,
   a.cand_shift = keys ? 0 : a.tpr_shift;
   a.tile_size = p.tile_size;
   a.parts = (int32_t)p.parts;
+  a.tokens_of_request = std::min(b->max_chunk, kTeamChunk - 1);
   const int64_t n = step * b->kv_heads;  // rows of scores
   a.scores = reinterpret_cast<float*>(d_workspace);
   a.facts = reinterpret_cast<TileFacts*>(a.scores + n * p.row_pad);
