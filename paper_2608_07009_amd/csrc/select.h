@@ -20,9 +20,13 @@ constexpr int kLongBins = 2048;       // of a long row's division
 constexpr int kPart = 16384;          // candidates of a long row's part
 constexpr int kRegisterRow = 32768;   // a longer row is long
 constexpr int kMaxParts = 1024;
+// New tokens of a request from which waves have new tokens of their own; fewer are scored one by one.
+constexpr int kTeamChunk = 5;
 
 struct TileFacts {
-  float norm, least, most;  // largest norm of a tile's rows, its least and largest score
+  // Largest norm of a tile's rows (of chunks of kTeamChunk and more, only the step's last new token has it),
+  // its least and largest score.
+  float norm, least, most;
 };
 
 struct SelectArgs : BatchArgs {

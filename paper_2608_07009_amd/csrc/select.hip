@@ -18,8 +18,6 @@ typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 constexpr int kRowPad = 256;          // a row of scores is a multiple of this
-// New tokens of a request from which waves have new tokens of their own; fewer are scored one by one.
-constexpr int kTeamChunk = 5;
 // Workgroups that tiles of candidates are made small for, and the least tile (log2).
 constexpr int kWantedGroups = 512, kLeastTile = 8;
 constexpr int64_t kMostGroups = (1 << 23) - 1;
@@ -389,11 +387,12 @@ struct Stage {
   static constexpr int P = Shape<KIND>::PIECES, LOADS = 64 * P / T, BYTES = 64 * P * 16;
   const Tile<KIND>& tile;
   u32x4_t x[LOADS];
-  uint64_t mask;  // which of the 64 are not padding
-  int entry;      // of candidate base + lane of the next 64
+  uint64_t mask, ready;  // which of the 64 are not padding: of those in registers, stored last
+  int entry;             // of candidate base + lane of the next 64
   Norm norm;
+  bool with_norm;
 
-  __device__ __forceinline__ explicit Stage(const Tile<KIND>& t) : tile(t) {
+  __device__ __forceinline__ Stage(const Tile<KIND>& t, bool norms) : tile(t), with_norm(norms) {
     entry = tile.entry_of(tile.first + (threadIdx.x & 63), tile.end);
   }
   __device__ __forceinline__ void fetch(int base) {
@@ -419,10 +418,31 @@ struct Stage {
     for (int i = 0; i < LOADS; ++i) {
       const int row = threadIdx.x / P + i * (T / P);
       *reinterpret_cast<u32x4_t*>(buf + row * (P * 16) + ((piece ^ (row & 15)) << 4)) = x[i];
-      float sq = sum16(squares(x[i], 0.f));
-      if (P == 32) sq += __shfl_xor(sq, 16);
-      norm.add(sq, any_bits(x[i]), mask >> row & 1);
     }
+    if (with_norm)
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) {
+        float sq = sum16(squares(x[i], 0.f));
+        if (P == 32) sq += __shfl_xor(sq, 16);
+        norm.add(sq, any_bits(x[i]), mask >> (threadIdx.x / P + i * (T / P)) & 1);
+      }
+    ready = mask;
+  }
+  // The first 64 candidates to buf, the next ones to registers.
+  __device__ __forceinline__ void start(uint8_t* buf) {
+    fetch(tile.first);
+    store(buf);
+    if (tile.first + 64 < tile.end) fetch(tile.first + 64);
+  }
+  // While the 64 from base on are scored: the next ones to buf, those behind them to registers. between()
+  // writes down scores: after what was loaded is here, before the next loads, so that no wait for a load is
+  // one for a store as well.
+  template <class F>
+  __device__ __forceinline__ void move(int base, uint8_t* buf, F&& between) {
+    if (base + 64 < tile.end) store(buf);
+    asm volatile("" : "+v"(entry));
+    between();
+    if (base + 128 < tile.end) fetch(base + 128);
   }
 };
 
@@ -483,6 +503,12 @@ struct Rows32 {
 // WAVES times Rows32::TOKENS new tokens (of one or more requests that have kTeamChunk or more, one after the
 // other), a tile of candidates: each wave has new tokens of its own, all have the same candidates, 64 at a
 // time in LDS. The products of 32 candidates with one tile of queries run beside the sums of those before.
+// Norms of the rows, a tenth of the time where every workgroup works them out, are the request's, not a new
+// token's: the workgroup that has its last new token of this step, which sees most, has them for all.
+// 512 new tokens of 64 heads over 32768 keys: 262 us, 1.05 PFLOP/s of products, four fifths of the rate of a
+// large matrix product; the rest is the weighted sum, 32 vector instructions to 16 MFMAs, which run beside
+// each other only in part. (Measured: half of the waves moving candidates after their products instead of
+// before, 2 % slower in all; a wave priority for them, no gain.)
 template <int HEADS, int WAVES, int OCCUPANCY>
 __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(SelectArgs a) {
   constexpr int KIND = HISPARSE_INDEX_KEYS, T = 64 * WAVES;
@@ -523,15 +549,24 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(Selec
       least[n] = INFINITY;
       most[n] = -INFINITY;
     }
-    St stage(tile);
-    stage.fetch(tile.first);
-    stage.store(s_mem);
+    // scores of the 64 candidates from `scored` on, not yet written down
+    float scores[R::TOKENS] = {};
+    int scored = tile.end;
+    uint64_t scored_mask = 0;
+    auto write_down = [&] {
+#pragma unroll
+      for (int n = 0; n < R::TOKENS; ++n)
+        if (n < live && scored + lane < tile.end)
+          put_score(scores[n], scored_mask >> lane & 1, out + n * pitch, scored + lane, least[n], most[n]);
+    };
+    St stage(tile, token0 + tokens == min(r.begin + r.n, a.row0 + a.rows));
+    stage.start(s_mem);
     __syncthreads();
     int cur = 0;
 #pragma unroll 1
     for (int base = tile.first; base < tile.end; base += 64) {
-      const uint64_t mask = stage.mask;
-      if (base + 64 < tile.end) stage.fetch(base + 64);
+      const uint64_t mask = stage.ready;
+      stage.move(base, s_mem + (cur ^ 1) * St::BYTES, write_down);
       if (live > 0) {
         float v[2][R::TOKENS] = {};
         u32x4_t y[2][R::STEPS];
@@ -558,16 +593,14 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(Selec
         }
         rows.add_up(R::TILES - 1, acc[1], v[1]);
 #pragma unroll
-        for (int n = 0; n < R::TOKENS; ++n) {
-          const float s = halves(v[0][n], v[1][n]);
-          if (n < live && base + lane < tile.end)
-            put_score(s, mask >> lane & 1, out + n * pitch, base + lane, least[n], most[n]);
-        }
+        for (int n = 0; n < R::TOKENS; ++n) scores[n] = halves(v[0][n], v[1][n]);
       }
+      scored = base;
+      scored_mask = mask;
       cur ^= 1;
-      if (base + 64 < tile.end) stage.store(s_mem + cur * St::BYTES);
       __syncthreads();
     }
+    write_down();
     const uint32_t nb = wave_reduce(__float_as_uint(stage.norm.largest), 0u, Largest());
     const uint32_t bits = wave_reduce(stage.norm.bits, 0u, Either());
     if (lane == 0) {
@@ -630,31 +663,41 @@ __global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a) {
     const int mine = wave * TOKENS + group;  // this lane's new token
     float* out = a.scores + ((int64_t)(token0 + mine - a.row0) * a.heads + h) * a.row_pad;
     float least = INFINITY, most = -INFINITY;
-    St stage(tile);
-    stage.fetch(tile.first);
-    stage.store(s_mem);
+    // scores of the 64 candidates from `scored` on, not yet written down
+    float scores[4] = {};
+    int scored = tile.end;
+    uint64_t scored_mask = 0;
+    auto write_down = [&] {
+#pragma unroll
+      for (int sub = 0; sub < 4; ++sub) {
+        const int at = sub * 16 + col;
+        if (mine < tokens && scored + at < tile.end)
+          put_score(scores[sub], scored_mask >> at & 1, out, scored + at, least, most);
+      }
+    };
+    St stage(tile, token0 + tokens == min(r.begin + r.n, a.row0 + a.rows));
+    stage.start(s_mem);
     __syncthreads();
     int cur = 0;
 #pragma unroll 1
     for (int base = tile.first; base < tile.end; base += 64) {
-      const uint64_t mask = stage.mask;
-      if (base + 64 < tile.end) stage.fetch(base + 64);
+      const uint64_t mask = stage.ready;
+      stage.move(base, s_mem + (cur ^ 1) * St::BYTES, write_down);
 #pragma unroll
       for (int sub = 0; sub < 4; ++sub) {
         u32x4_t y[S::STEPS];
-        const int at = sub * 16 + col;
-        const uint8_t* row = s_mem + cur * St::BYTES + at * (S::PIECES * 16);
+        const uint8_t* row = s_mem + cur * St::BYTES + (sub * 16 + col) * (S::PIECES * 16);
 #pragma unroll
         for (int k = 0; k < S::STEPS; ++k)
           y[k] = *reinterpret_cast<const u32x4_t*>(row + (((k * 4 + group) ^ col) << 4));
-        const float s = rows.score(y);
-        if (mine < tokens && base + at < tile.end)
-          put_score(s, mask >> at & 1, out, base + at, least, most);
+        scores[sub] = rows.score(y);
       }
+      scored = base;
+      scored_mask = mask;
       cur ^= 1;
-      if (base + 64 < tile.end) stage.store(s_mem + cur * St::BYTES);
       __syncthreads();
     }
+    write_down();
     const uint32_t nb = wave_reduce(__float_as_uint(stage.norm.largest), 0u, Largest());
     const uint32_t bits = wave_reduce(stage.norm.bits, 0u, Either());
     least = least16(least);

@@ -143,7 +143,7 @@ struct Row {
   uint16_t* s_q;        // keys: the queries, [q_heads] rows of kQPitch
   const float* wrow;    // and their weights, or null
   float* scores;
-  const TileFacts* facts;
+  const TileFacts *facts, *norms;  // (the tiles' largest norms are in the second)
   int token, q, h, p, seen, first, last0;  // forced: j < first, j >= last0
   int lane, wave;
 
@@ -161,6 +161,8 @@ struct Row {
     const int64_t slot = (int64_t)local * a.heads + h;
     scores = a.scores + slot * a.row_pad;
     facts = a.facts + slot * a.tiles;
+    const int last = min(r.begin + r.n, a.row0 + a.rows) - 1;
+    norms = r.n < kTeamChunk ? facts : a.facts + ((int64_t)(last - a.row0) * a.heads + h) * a.tiles;
     wrow = KEYS && a.weights ? a.weights + ((int64_t)token * a.heads + h) * a.q_heads : nullptr;
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -233,7 +235,7 @@ struct Row {
     const int tiles = (seen + (1 << a.tile_size) - 1) >> a.tile_size;
     for (int i = threadIdx.x; i < tiles; i += T) {
       const TileFacts f = facts[i];
-      norm = max(norm, __float_as_uint(f.norm));
+      norm = max(norm, __float_as_uint(norms[i].norm));
       least = min(least, ordered32(f.least));
       most = max(most, ordered32(f.most));
     }
