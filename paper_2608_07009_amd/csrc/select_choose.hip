@@ -2,9 +2,10 @@
 //
 // The choice is that of scores in 64 bits, which the fp32 scores of select.hip settle but for a few:
 // with
-//   |s_j - exact| <= eps = 1.25 * 2^-15 A N,  A = sum_e |w_e| |q_e|, N = the largest |k_j| seen
-// (keys: sums of 128 products, each step off by at most 2^-23, and of up to 128 heads, 2^-24 a step:
-// 2^-16 + 2^-17; the others: 256 products, 2^-15, their three parts and what is left of q+ and q-, 2^-22)
+//   |s_j - exact| <= eps = 1.25 c A N,  A = sum_e |w_e| |q_e|, N = the largest |k_j| seen
+// (keys: sums of 128 products, each step off by at most 2^-23, and of the heads, 2^-24 a step and the
+// weight's product: c = 2^-16 + (heads + 1) 2^-24; the others: c = 2^-15, 256 products, their three parts and
+// what is left of q+ and q-, 2^-22, being less than the quarter added)
 // and with the m-th largest s in [lo, hi], candidates above hi + 2 eps are among the best m, those below
 // lo - 2 eps are not, and those between ("open") are scored again in 64 bits.
 //
@@ -273,7 +274,8 @@ struct Row {
     if (N == 0.f && A < INFINITY) return 0.f;
     // the last term: what inputs and sums below the normal range are off by
     const float AN = (float)A * 1.01f * N;
-    return AN * 0x1.4p-15f + (float)W * (N + (float)Q + 1.f) * 0x1p-118f;
+    const float c = KEYS ? 0x1.4p-16f + (float)(a.q_heads + 1) * 0x1.4p-24f : 0x1.4p-15f;
+    return AN * c + (float)W * (N + (float)Q + 1.f) * 0x1p-118f;
   }
 
   // Writes candidate j (-1: none) to a place of the list.
@@ -688,31 +690,43 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
   const int e0 = r.wave * span + r.lane * 4;
   if (listed) {
     const int parts = (r.seen + kPart - 1) / kPart;
+    const int32_t* survivors = a.survivors + slot * a.row_pad;
 #pragma unroll
-    for (int v = 0; v < V; ++v)
+    for (int v = 0; v < V; ++v) {
+      int at[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int e = e0 + v * 256 + i;
-        int j = -1;
-        float y = __uint_as_float(kNan);
-        if (v < groups && e < n) {
-          int lo = 0, hi = parts;  // the last part that begins at or before e
-          while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if ((int)s.win[mid] <= e) lo = mid;
-            else hi = mid;
-          }
-          j = a.survivors[slot * a.row_pad + (int64_t)lo * kPart + e - (int)s.win[lo]];
-          j = min(max(j, 0), r.seen - 1);
-          y = r.scores[j];
-          if (r.forced(j)) {
-            y = __uint_as_float(kNan);
-            in |= 1u << (4 * v + i);
-          }
-        }
-        x[v][i] = y;
-        pos[LONG ? 4 * v + i : 0] = j;
+        x[v][i] = __uint_as_float(kNan);
+        pos[LONG ? 4 * v + i : 0] = -1;
       }
+      if (v >= groups || e0 + v * 256 >= n) continue;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // (past the last one: the last one, for four loads at a time)
+        const int e = min(e0 + v * 256 + i, n - 1);
+        int lo = 0, hi = parts;  // the last part that begins at or before e
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if ((int)s.win[mid] <= e) lo = mid;
+          else hi = mid;
+        }
+        at[i] = lo * kPart + e - (int)s.win[lo];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) at[i] = survivors[at[i]];
+      float y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        at[i] = min(max(at[i], 0), r.seen - 1);
+        y[i] = r.scores[at[i]];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (e0 + v * 256 + i < n) {
+          pos[LONG ? 4 * v + i : 0] = at[i];
+          if (r.forced(at[i])) in |= 1u << (4 * v + i);
+          else x[v][i] = y[i];
+        }
+    }
     __syncthreads();
   } else {
 #pragma unroll
