@@ -23,6 +23,7 @@ namespace {
 typedef double f64x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kQPitch = kIndexDims + 8;  // keys: a query's row in LDS (16-byte pieces, banks apart)
+constexpr int kCUs = 256;
 constexpr int kBatch = 128;              // open candidates scored at a time
 
 // 64-bit scores in the order of the choice: NaN above everything, -0 as 0.
@@ -211,7 +212,7 @@ struct Row {
     } else {
       if (wave == 0) {  // 16 lanes a query
         double pos[8], neg[8];
-        query_sums<KIND, 4>(a, token, h, lane & 15, lane >> 4, 4, pos, neg);
+        query_sums<KIND, 2>(a, token, h, lane & 15, lane >> 4, 4, pos, neg);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
 #pragma unroll
@@ -632,11 +633,12 @@ struct LongRow {
 };
 
 template <int KIND, int T, int V, int BINS, int LIST, bool LONG>
-__global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
+__global__ __launch_bounds__(T, T == 512 ? 4 : 1) void choose_kernel(SelectArgs a) {
   constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
   constexpr int WAVES = T / 64, CAP = T * V * 4;
   using S = Shared<KIND, T, BINS, LIST, CAP>;
-  static_assert(V * 4 <= 32 && CAP <= 65536, "a bit for each of a thread's candidates; 16-bit places");
+  using Bits = std::conditional_t<V * 4 <= 32, uint32_t, uint64_t>;  // one for each of a thread's candidates
+  static_assert(V * 4 <= 64 && CAP <= 65536, "bits; 16-bit places");
   static_assert(sizeof(S) + (KEYS ? 128 * kQPitch * 2 : 0) <= 65536, "LDS of a launch");
   extern __shared__ __align__(16) uint8_t s_mem[];
   S& s = *reinterpret_cast<S*>(s_mem);
@@ -685,7 +687,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
   const int span = (((n + WAVES - 1) / WAVES) + 255) & ~255, groups = span >> 8;
   f32x4_t x[V];
   int pos[LONG ? V * 4 : 1];
-  uint32_t in = 0;  // the chosen ones: bit 4 v + i
+  Bits in = 0;  // the chosen ones: bit 4 v + i
   const int own = r.own();
   const int e0 = r.wave * span + r.lane * 4;
   if (listed) {
@@ -723,7 +725,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
       for (int i = 0; i < 4; ++i)
         if (e0 + v * 256 + i < n) {
           pos[LONG ? 4 * v + i : 0] = at[i];
-          if (r.forced(at[i])) in |= 1u << (4 * v + i);
+          if (r.forced(at[i])) in |= Bits(1) << (4 * v + i);
           else x[v][i] = y[i];
         }
     }
@@ -738,7 +740,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
       for (int i = 0; i < 4; ++i) {
         const int j = base + i;
         const bool dead = j >= n || y[i] == kPad, kept = !dead && r.forced(j);
-        if (kept && j != own) in |= 1u << (4 * v + i);
+        if (kept && j != own) in |= Bits(1) << (4 * v + i);
         x[v][i] = dead || kept ? __uint_as_float(kNan) : __uint_as_float(y[i]);
         if (LONG) pos[LONG ? 4 * v + i : 0] = j;
       }
@@ -756,7 +758,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
   auto position = [&](int bit) {
     return LONG ? pos[LONG ? bit : 0] : e0 + (bit >> 2) * 256 + (bit & 3);
   };
-  const int m = a.top_k - (a.last > 0) - (int)group_reduce<T>(__popc(in), s.wave_b, Add());
+  const int m = a.top_k - (a.last > 0) - (int)group_reduce<T>((uint32_t)__popcll(in), s.wave_b, Add());
 
   float sure = INFINITY, maybe = INFINITY;
   if (m > 0) {
@@ -788,13 +790,14 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
     // rounded outwards
     sure = any ? -INFINITY : nextafterf(to + 2.f * row.eps, INFINITY);
     maybe = any ? -INFINITY : nextafterf(from - 2.f * row.eps, -INFINITY);
-    uint32_t n_sure = 0, open_bits = 0;
+    uint32_t n_sure = 0;
+    Bits open_bits = 0;
     each([&](int bit, float y) {
       if (y > sure) {
-        in |= 1u << bit;
+        in |= Bits(1) << bit;
         ++n_sure;
       } else if (y >= maybe) {
-        open_bits |= 1u << bit;
+        open_bits |= Bits(1) << bit;
         const int at = atomicAdd(&s.count, 1);
         if (at < LIST) {
           s.list[at] = position(bit);
@@ -828,7 +831,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int e = e0 + v * 256;
-          if (v < groups) in |= ((s.win[e >> 5] >> (e & 31)) & 15u) << (4 * v);
+          if (v < groups) in |= (Bits)((s.win[e >> 5] >> (e & 31)) & 15u) << (4 * v);
         }
     }
   }
@@ -839,7 +842,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
   for (int v = 0; v < V; ++v) {
     places[v] = 0;
     if (v < groups) {
-      const int c = __popc((in >> (4 * v)) & 15u), inc = wave_inclusive(c);
+      const int c = __popc((uint32_t)(in >> (4 * v)) & 15u), inc = wave_inclusive(c);
       places[v] = mine + inc - c;
       mine += last_lane(inc);
     }
@@ -860,7 +863,7 @@ __global__ __launch_bounds__(T) void choose_kernel(SelectArgs a) {
     if (v < groups)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if ((in >> (4 * v + i) & 1) && at < a.top_k) s.out[at++] = position(4 * v + i);
+        if (((uint32_t)(in >> (4 * v + i)) & 1) && at < a.top_k) s.out[at++] = position(4 * v + i);
   }
   __syncthreads();
 #pragma unroll 4
@@ -983,6 +986,7 @@ template <int KIND>
 void launch_kind(const SelectArgs& a, int64_t candidates, hipStream_t s) {
   if (candidates <= 1024) launch<KIND, 64, 4, 256, 256, false>(a, s);
   else if (candidates <= 4096) launch<KIND, 256, 4, 1024, 512, false>(a, s);
+  else if (candidates <= kRegisterRow && (int64_t)a.rows * a.heads > kCUs) launch<KIND, 512, 16, 2048, 1024, false>(a, s);
   else if (candidates <= kRegisterRow) launch<KIND, 1024, 8, 2048, 1024, false>(a, s);
   else launch<KIND, 1024, 8, 2048, 1024, true>(a, s);
 }

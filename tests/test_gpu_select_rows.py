@@ -118,6 +118,29 @@ def test_chunks_of_every_length_side_by_side(kind, q_heads):
 
 
 @pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("cand,k", [(4100, 2048), (32768, 300), (20011, 7)])
+def test_more_rows_than_the_chip_has_workgroups_for(kind, cand, k):
+    """Rows that many choose with half the threads, as all others do."""
+    t = 4 if kind == KEYS else 1
+    c = Case(kind, t, [129, 1, 2], [cand, cand - 9, cand // 2], k=k, heads=2, q_heads=3, last=2, first=1,
+             data=long_data(kind), tail=3)
+    c.table[0, 0, 5], c.table[1, 0, 70] = -1, c.index.shape[0]
+    c.check(rows=[0, 1, 63, 64, 127, 128, 129, 130, 131])
+    whole = c.dv["sel"].clone()
+    c.device(ws=lambda n: (n // c.total + 1) * 100 + 64)
+    c.call()
+    assert torch.equal(c.dv["sel"], whole)
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_equal_scores_in_many_rows(kind):
+    c = Case(kind, 1, [300], [9000], k=900, q_heads=2, last=1, weights=False, data=small_whole(-1, 1, 0.9))
+    c.q = torch.randint(-1, 2, c.q.shape, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    c.q[7], c.q[8] = 0, c.q[9]
+    c.check(rows=[0, 7, 8, 150, 299])
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
 @pytest.mark.parametrize("max_chunk", [4, 5, 40])
 def test_uniform_chunks(kind, max_chunk):
     t = 4
