@@ -261,12 +261,12 @@ struct Rows16 {
 // New token i of request q (of those with fewer than kTeamChunk), a tile of candidates: each wave has a
 // quarter of it and loads rows as operands, 32 ahead. HBM-bound from a few requests on: 32 requests of up to
 // 32768 tokens, 64 heads, 200 MB of keys in 40 us.
-template <int KIND, int MT, int OCCUPANCY>
-__global__ __launch_bounds__(256, OCCUPANCY) void score_token_kernel(SelectArgs a) {
+// s_a: 16 rows of an operand, not used for keys.
+template <int KIND, int MT>
+__device__ __forceinline__ void score_token(const SelectArgs& a, uint32_t block, uint16_t* s_a) {
   using S = Shape<KIND>;
   constexpr bool KEYS = S::KEYS;
   constexpr int WAVES = 4, T = 64 * WAVES;
-  __shared__ __align__(16) uint16_t s_a[KEYS ? 8 : 16 * (S::DIMS + 8)];
   __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
   __shared__ float s_least[WAVES], s_most[WAVES];
   const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
@@ -274,7 +274,7 @@ __global__ __launch_bounds__(256, OCCUPANCY) void score_token_kernel(SelectArgs 
   // request and token first: workgroups of one request are far apart
   const uint32_t per = (uint32_t)a.tokens_of_request;
   const uint32_t n_rows = (uint32_t)a.requests * per;
-  const uint32_t rest = blockIdx.x / n_rows, row = blockIdx.x - rest * n_rows;
+  const uint32_t rest = block / n_rows, row = block - rest * n_rows;
   const int q = (int)(row / per), i = (int)(row - (uint32_t)q * per);
   const int kt = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)kt * a.heads);
   const RequestRows r = rows_of(a, q);
@@ -375,6 +375,12 @@ __global__ __launch_bounds__(256, OCCUPANCY) void score_token_kernel(SelectArgs 
     most = fmaxf(most, s_most[x]);
   }
   put_facts<WAVES>(a, token, 1, h, kt, s_norm, s_bits, least, most);
+}
+
+template <int KIND, int MT, int OCCUPANCY>
+__global__ __launch_bounds__(256, OCCUPANCY) void score_token_kernel(SelectArgs a) {
+  __shared__ __align__(16) uint16_t s_a[Shape<KIND>::KEYS ? 8 : 16 * (Shape<KIND>::DIMS + 8)];
+  score_token<KIND, MT>(a, blockIdx.x, s_a);
 }
 
 // ---- chunks of new tokens ----------------------------------------------------------------------
@@ -626,14 +632,17 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(Selec
   }
 }
 
-// The same for bounds and means, four new tokens a wave.
+// The same for bounds and means, four new tokens a wave. The last token_blocks workgroups are those of single
+// tokens. (A launch of their own took 2.5 us where none were due.)
 template <int KIND>
-__global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a) {
+__global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a, uint32_t token_blocks) {
   using S = Shape<KIND>;
   constexpr int WAVES = 4, T = 64 * WAVES, TOKENS = 4, ROWS = WAVES * TOKENS;
   using St = Stage<KIND, T>;
   constexpr int A_BYTES = 16 * WAVES * (S::DIMS + 8) * 2;
   __shared__ __align__(16) uint8_t s_mem[std::max(2 * St::BYTES, A_BYTES)];
+  if (blockIdx.x >= gridDim.x - token_blocks)
+    return score_token<KIND, 1>(a, blockIdx.x - (gridDim.x - token_blocks), reinterpret_cast<uint16_t*>(s_mem));
   __shared__ uint32_t s_norm[WAVES], s_bits[WAVES];
   __shared__ float s_least[ROWS], s_most[ROWS];
   const int lane = threadIdx.x & 63, col = lane & 15, group = lane >> 4;
@@ -780,16 +789,17 @@ void launch_keys(const SelectArgs& a, hipStream_t s) {
                      dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), dim3(64 * WAVES), 0, s, a);
 }
 template <int KIND>
-void launch_rows(const SelectArgs& a, hipStream_t s) {
+void launch_rows(const SelectArgs& a, unsigned token_blocks, hipStream_t s) {
   const unsigned row_tiles = (unsigned)((a.rows + 15) / 16);
   hipLaunchKernelGGL(score_rows_kernel<KIND>,
-                     dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles), dim3(256), 0, s, a);
+                     dim3(row_tiles * (unsigned)a.heads * (unsigned)a.tiles + token_blocks), dim3(256), 0, s, a,
+                     token_blocks);
 }
 
 hipError_t launch_select(const SelectArgs& a, int kind, const SelectPlan& p, hipStream_t s) {
   constexpr int K = HISPARSE_INDEX_KEYS, B = HISPARSE_INDEX_BOUNDS, M = HISPARSE_INDEX_MEANS;
   const bool tokens = a.start || !p.team;  // (without starts all chunks are max_chunk)
-  if (tokens) {
+  if (tokens && (kind == K || !p.team)) {
     if (kind == B) launch_tokens<B, 1, 2>(a, p, s);
     else if (kind == M) launch_tokens<M, 1, 2>(a, p, s);
     else if (a.q_heads <= 16) launch_tokens<K, 1, 3>(a, p, s);
@@ -798,8 +808,9 @@ hipError_t launch_select(const SelectArgs& a, int kind, const SelectPlan& p, hip
     else launch_tokens<K, 8, 1>(a, p, s);
   }
   if (p.team) {
-    if (kind == B) launch_rows<B>(a, s);
-    else if (kind == M) launch_rows<M>(a, s);
+    const unsigned token_blocks = tokens ? (unsigned)(p.token_rows * p.tiles) : 0u;
+    if (kind == B) launch_rows<B>(a, token_blocks, s);
+    else if (kind == M) launch_rows<M>(a, token_blocks, s);
     else if (a.q_heads <= 16) launch_keys<16, 8, 2>(a, s);
     else if (a.q_heads <= 32) launch_keys<32, 8, 2>(a, s);
     else if (a.q_heads <= 64) launch_keys<64, 8, 2>(a, s);
