@@ -262,7 +262,8 @@ hisparse_status_t hisparse_rotate_tokens(const hisparse_rotary_desc_t* d, int32_
     s.items = (uint32_t)((int64_t)r.heads * s.per_head);
   }
   a.items = (uint32_t)items;
-  // Four items a thread where there is enough to fill the chip, one workgroup of a token otherwise.
+  // Four items a thread where there is enough to fill the chip, one workgroup of a token otherwise. (16384
+  // tokens of 32 + 8 heads of 128: 61.0 us; with one item a thread 71.4, two 61.6, eight 63.5.)
   constexpr int kItems = 4 * kThreads;
   a.slice = (uint32_t)std::min<int64_t>(items, kItems);
   a.group_tokens = 1;

@@ -20,11 +20,14 @@ constexpr int kLongBins = 2048;       // of a long row's division
 constexpr int kPart = 16384;          // candidates of a long row's part
 constexpr int kRegisterRow = 32768;   // a longer row is long
 constexpr int kMaxParts = 1024;
-// New tokens of a request from which waves have new tokens of their own; fewer are scored one by one.
-constexpr int kTeamChunk = 5;
+// New tokens of a request from which waves have new tokens of their own; fewer are scored one by one, which
+// reads the index for each. (Eight requests, 64 heads over 32768 keys: chunks of 3 take 69 us one by one and
+// 86 by teams, of 4, 79 and 75. Bounds of 8192 pages, 4 requests x 8 kv heads: 2, 65 and 70; 4, 102 and 70.)
+template <int KIND>
+constexpr int kTeamChunk = KIND == HISPARSE_INDEX_KEYS ? 4 : 3;
 
 struct TileFacts {
-  // Largest norm of a tile's rows (of chunks of kTeamChunk and more, only the step's last new token has it),
+  // Largest norm of a tile's rows (of chunks of teams, only the step's last new token has it),
   // its least and largest score.
   float norm, least, most;
 };

@@ -279,7 +279,7 @@ __device__ __forceinline__ void score_token(const SelectArgs& a, uint32_t block,
   const int kt = (int)(rest / (uint32_t)a.heads), h = (int)(rest - (uint32_t)kt * a.heads);
   const RequestRows r = rows_of(a, q);
   const int token = r.begin + i;
-  if (i >= r.n || r.n >= kTeamChunk || token < a.row0 || token >= a.row0 + a.rows) return;
+  if (i >= r.n || r.n >= kTeamChunk<KIND> || token < a.row0 || token >= a.row0 + a.rows) return;
   const int seen = seen_at(a, r.len - r.n + i);
   const Tile<KIND> tile(a, q, h, kt, seen);
   if (seen <= a.top_k || tile.first >= seen) return;
@@ -542,7 +542,7 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(Selec
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
     const Tile<KIND> tile(a, q, h, kt, seen);
-    if (r.n < kTeamChunk || seen <= a.top_k || tile.first >= seen) continue;
+    if (r.n < kTeamChunk<KIND> || seen <= a.top_k || tile.first >= seen) continue;
     const int mine = wave * R::TOKENS;                     // this wave's first new token
     const int live = min(tokens - mine, (int)R::TOKENS);  // and how many it has (0 or less: none)
     R rows;
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a, uint32
     t += tokens;
     const int seen = seen_at(a, r.len - r.n + token0 + tokens - 1 - r.begin);
     const Tile<KIND> tile(a, q, h, kt, seen);
-    if (r.n < kTeamChunk || seen <= a.top_k || tile.first >= seen) continue;
+    if (r.n < kTeamChunk<KIND> || seen <= a.top_k || tile.first >= seen) continue;
     Rows16<KIND, 1> rows;
     linear_rows<KIND, T>(a, token0, tokens, ROWS, h, reinterpret_cast<uint16_t*>(s_mem));
     __syncthreads();
@@ -741,6 +741,7 @@ struct SelectPlan {
   int64_t token_rows;  // workgroups of single tokens, for each tile
   int32_t tile_size;
   bool team;          // chunks of kTeamChunk or more new tokens can occur
+  int32_t alone;      // the most new tokens of a request that are scored one by one
 };
 
 int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of; }
@@ -750,9 +751,12 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
   SelectPlan p{};
   const bool keys = x.kind == HISPARSE_INDEX_KEYS;
   p.candidates = keys ? (int64_t)b.max_records * b.tokens_per_record : b.max_records;
-  // The largest tiles of which there are enough: a workgroup first loads its queries. (512 new tokens x 64
-  // heads over 32768 keys: scores and choice in 321 us with 512 of them, 331 with 1024.)
-  p.team = b.max_chunk >= kTeamChunk;
+  // The largest tiles of which there are enough: a workgroup first loads its queries. (64 heads, all of a call:
+  // 128 new tokens over 32768 keys, 101 us with 512 workgroups, 114 with 1024, 98 with 256; a new token of 32
+  // requests over 8192, 39, 45 and 38; means of 512 blocks for 1024 new tokens, 34.3 with 512, 36.1 with 256.)
+  const int team = keys ? kTeamChunk<HISPARSE_INDEX_KEYS> : kTeamChunk<HISPARSE_INDEX_MEANS>;
+  p.team = b.max_chunk >= team;
+  p.alone = std::min(b.max_chunk, team - 1);
   const int64_t row_tiles =
       (p.team ? whole(b.total_tokens, team_rows(x.kind, d.q_heads))
               : std::min<int64_t>(b.total_tokens, (int64_t)b.num_requests * b.max_chunk)) * b.kv_heads;
@@ -761,7 +765,7 @@ SelectPlan plan_select(const hisparse_index_desc_t& x, const hisparse_batch_desc
          row_tiles * whole(p.candidates, 1 << p.tile_size) < kWantedGroups)
     --p.tile_size;
   // (a launch's workgroups are counted in 32 bits, with all their threads)
-  p.token_rows = (int64_t)b.num_requests * std::min(b.max_chunk, kTeamChunk - 1) * b.kv_heads;
+  p.token_rows = (int64_t)b.num_requests * p.alone * b.kv_heads;
   while (p.tile_size < 30 && p.token_rows * whole(p.candidates, 1 << p.tile_size) > kMostGroups)
     ++p.tile_size;
   p.tiles = whole(p.candidates, 1 << p.tile_size);
@@ -915,7 +919,7 @@ hisparse_status_t hisparse_select_records(const hisparse_index_desc_t* x,
   a.cand_shift = keys ? 0 : a.tpr_shift;
   a.tile_size = p.tile_size;
   a.parts = (int32_t)p.parts;
-  a.tokens_of_request = std::min(b->max_chunk, kTeamChunk - 1);
+  a.tokens_of_request = p.alone;
   const int64_t n = step * b->kv_heads;  // rows of scores
   a.scores = reinterpret_cast<float*>(d_workspace);
   a.facts = reinterpret_cast<TileFacts*>(a.scores + n * p.row_pad);

@@ -10,7 +10,7 @@
 // lo - 2 eps are not, and those between ("open") are scored again in 64 bits.
 //
 // [lo, hi] is a bin of a histogram between the least and the largest score. A row of up to 32768 scores
-// is held in the registers of one workgroup (64 to 1024 threads), loaded once. Longer rows are cut down
+// is held in the registers of one workgroup, loaded once. Longer rows are cut down
 // first: narrow_kernel's workgroups add up the row's histogram, keep_kernel's write down the candidates
 // that its bin leaves in question or in, a part of the row each, and those few are chosen from. Rows
 // that neither way settles (thousands of open candidates, no error bound because of infinities) go over
@@ -164,7 +164,7 @@ struct Row {
     scores = a.scores + slot * a.row_pad;
     facts = a.facts + slot * a.tiles;
     const int last = min(r.begin + r.n, a.row0 + a.rows) - 1;
-    norms = r.n < kTeamChunk ? facts : a.facts + ((int64_t)(last - a.row0) * a.heads + h) * a.tiles;
+    norms = r.n < kTeamChunk<KIND> ? facts : a.facts + ((int64_t)(last - a.row0) * a.heads + h) * a.tiles;
     wrow = KEYS && a.weights ? a.weights + ((int64_t)token * a.heads + h) * a.q_heads : nullptr;
     lane = threadIdx.x & 63;
     wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -981,12 +981,25 @@ void launch(const SelectArgs& a, hipStream_t s) {
                      sizeof(Shared<KIND, T, BINS, LIST, T * V * 4>) + queries, s, a);
 }
 
-// A workgroup holds a row in 16 or 32 registers a thread; the smallest that do.
+// The workgroups that hold a row, 16 to 64 scores a thread. Few threads have less to agree on, many get through
+// their own sooner, and where rows are more than compute units, small workgroups share them. Keys of 64 heads
+// and bounds, all of a call:
+//   1 row of 8192     512 threads, not 1024: 23.4 us, not 26.2      21.1, not 22.9
+//   600 rows of 8192  256, not 512:          130, not 138           63, not 71
+//   600 rows of 16000 512, not 1024:         225, not 234           94, not 101
+//   600 rows of 4096  256, not 1024:         85, not 105            41, not 58
+//   4000 rows of 512  64, not 256:           (keys: always 256)     27, not 40 (means; 300 rows: 19.5, 18.4)
 template <int KIND>
 void launch_kind(const SelectArgs& a, int64_t candidates, hipStream_t s) {
-  if (candidates <= 1024) launch<KIND, 64, 4, 256, 256, false>(a, s);
-  else if (candidates <= 4096) launch<KIND, 256, 4, 1024, 512, false>(a, s);
-  else if (candidates <= kRegisterRow && (int64_t)a.rows * a.heads > kCUs) launch<KIND, 512, 16, 2048, 1024, false>(a, s);
+  constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
+  const int64_t rows = (int64_t)a.rows * a.heads;
+  if constexpr (!KEYS) {
+    if (candidates <= 1024 && rows > 8 * kCUs) return launch<KIND, 64, 4, 256, 256, false>(a, s);
+  }
+  if (candidates <= 4096) launch<KIND, 256, 4, 1024, 512, false>(a, s);
+  else if (candidates <= 8192 && rows > kCUs) launch<KIND, 256, 8, 1024, 512, false>(a, s);
+  else if (candidates <= 16384) launch<KIND, 512, 8, 2048, 1024, false>(a, s);
+  else if (candidates <= kRegisterRow && rows > kCUs) launch<KIND, 512, 16, 2048, 1024, false>(a, s);
   else if (candidates <= kRegisterRow) launch<KIND, 1024, 8, 2048, 1024, false>(a, s);
   else launch<KIND, 1024, 8, 2048, 1024, true>(a, s);
 }

@@ -133,6 +133,27 @@ def test_more_rows_than_the_chip_has_workgroups_for(kind, cand, k):
 
 
 @pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+def test_thousands_of_short_rows(kind):
+    for cand, k in ((1024, 100), (513, 24), (300, 1)):
+        t = 4
+        c = Case(kind, t, [700, 2], [cand * (1 if kind == KEYS else t), cand - 7], k=k, heads=3, q_heads=3,
+                 first=int(k > 1), last=int(k > 2), tail=1)
+        c.table[0, 0, 5], c.table[0, 0, 70] = -1, c.index.shape[0]
+        c.check(rows=[0, 1, 350, 699, 700, 701])
+
+
+@pytest.mark.parametrize("kind", [BOUNDS, MEANS])
+def test_equal_scores_in_thousands_of_short_rows(kind):
+    c = Case(kind, 1, [2100], [1000 + 2100], k=90, q_heads=2, last=1, weights=False, data=small_whole(-1, 1, 0.98))
+    c.per = 1024
+    c.table = c.table[:, :, :1024].contiguous()
+    c.lens = [1024]
+    c.q = torch.randint(-1, 2, c.q.shape, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
+    c.q[2007] = 0
+    c.check(rows=[0, 1075, 1076, 1500, 2007, 2099])
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
 def test_equal_scores_in_many_rows(kind):
     c = Case(kind, 1, [300], [9000], k=900, q_heads=2, last=1, weights=False, data=small_whole(-1, 1, 0.9))
     c.q = torch.randint(-1, 2, c.q.shape, generator=torch.Generator().manual_seed(8)).to(torch.bfloat16)
