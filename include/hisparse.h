@@ -907,9 +907,9 @@ hisparse_status_t hisparse_validate_select(const hisparse_index_desc_t* index,
 
 /* [pure host] Bytes of device scratch for the call; 0 for invalid descriptors. A workspace of this size serves
  * every call of at most as many tokens and records with the same index kind and select and as many or
- * fewer kv heads. (The scores of all new tokens, held to 1 GiB or the scores of one tile of them: a call
- * goes over its tokens in as many steps as its workspace takes, and smaller workspaces, down to one tile's,
- * are accepted too. Results do not depend on it.) */
+ * fewer kv heads. (The scores of all new tokens, held to 1 GiB or to one new token's: a call goes over its
+ * tokens in as many steps as its workspace takes, and smaller workspaces, down to one new token's, are
+ * accepted too. Results do not depend on it.) */
 size_t hisparse_select_workspace_bytes(const hisparse_index_desc_t* index,
                                        const hisparse_batch_desc_t* batch,
                                        const hisparse_select_desc_t* select);
@@ -940,7 +940,8 @@ size_t hisparse_select_workspace_bytes(const hisparse_index_desc_t* index,
  *                request per row, chunks of 1, this and d_sel_len are d_table and d_kv_len of
  *                hisparse_chunk_attention over the selected records.
  *   d_sel_len    int32 [total_tokens] or NULL, out: tokens up to the row's own in those tables (0 for a token
- *                that sees nothing). Needs last_records > 0.
+ *                that sees nothing). Needs last_records > 0. Rows outside every chunk keep theirs: a caller
+ *                that attends to all rows of a padded batch clears them first.
  *   d_workspace  a multiple of 16; calls that may overlap need one each.
  * HISPARSE_ERR_INVALID_ARG for bad descriptors (tokens_per_record of index and batch alike), null or
  * misaligned pointers (d_index and d_workspace 16 bytes), d_weights with another kind than KEYS, d_sel_len

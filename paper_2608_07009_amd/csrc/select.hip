@@ -632,7 +632,9 @@ __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(Selec
   }
 }
 
-// The same for bounds and means, four new tokens a wave. The last token_blocks workgroups are those of single
+// The same for bounds and means, four new tokens a wave. 1024 new tokens of 4 x 16 heads over 512 means: 17 us,
+// of which 6 go into the sums over the heads (each of the two tiles of candidates reads all 17 MB of queries)
+// and 4 into the scores: one round of workgroups, each a chain of loads. The last token_blocks workgroups are those of single
 // tokens. (A launch of their own took 2.5 us where none were due.)
 template <int KIND>
 __global__ __launch_bounds__(256, 2) void score_rows_kernel(SelectArgs a, uint32_t token_blocks) {

@@ -57,7 +57,8 @@ struct alignas(16) Shared {
     };
     int out[CAP < kMaxTopK ? CAP : kMaxTopK];  // at the end, the chosen ones
   };
-  uint32_t win[CAP / 32];  // chosen ones among the open, by place
+  uint32_t win[CAP < 8192 ? 256 : CAP / 32];  // chosen ones among the open, by place
+  unsigned long long least, most;
   double q[KEYS ? 2 : 2 * kIndexDims];   // bounds and means: the sums over the heads
   uint32_t wave_a[T / 64], wave_b[T / 64], wave_c[T / 64];
   double wave_d[T / 64], wave_e[T / 64], wave_f[T / 64];
@@ -303,245 +304,6 @@ struct Row {
   }
 };
 
-// The choice from scores in memory, whatever they are: a few passes where 64 bits settle few candidates,
-// and where they have to settle many, the scores worked out anew in each of eight passes.
-template <int KIND, int T, int BINS, int LIST, class S>
-struct Stream {
-  static constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
-  static constexpr int WAVES = T / 64;
-  const Row<KIND, T>& r;
-  S& s;
-  int lo, hi;           // this wave's candidates
-  bool all, zero;       // every candidate is open; every score is 0
-  float sure, maybe;    // above sure: chosen; below maybe: not
-
-  __device__ Stream(const Row<KIND, T>& row, S& shared) : r(row), s(shared) {
-    const int span = (((r.seen + WAVES - 1) / WAVES) + 255) & ~255;
-    lo = (int)min((int64_t)r.wave * span, (int64_t)r.seen);
-    hi = (int)min((int64_t)(r.wave + 1) * span, (int64_t)r.seen);
-    all = zero = false;
-    sure = maybe = INFINITY;
-  }
-  __device__ __forceinline__ bool rankable(int j, float x) const {
-    return __float_as_uint(x) != kPad && !r.forced(j);
-  }
-  __device__ __forceinline__ bool is_sure(float x) const { return !all && x > sure; }
-  __device__ __forceinline__ bool is_open(float x) const { return all || (x >= maybe && !(x > sure)); }
-
-  // f(j, score) for this wave's candidates, four in a row per lane.
-  template <class F>
-  __device__ __forceinline__ void each(F&& f) const {
-    for (int base = lo + r.lane * 4; base < hi; base += 256) {
-      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(r.scores + base);
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (base + i < hi) f(base + i, x[i]);
-    }
-  }
-
-  // The score of candidate j in 64 bits. j is the same in all lanes, and so is the result.
-  __device__ __forceinline__ uint64_t exact(int j) const {
-    const uint8_t* key = nullptr;
-    int record;
-    find_row<KEYS>(r.a, r.q, r.h, j, key, record);
-    double sum = 0.0;
-    if constexpr (KEYS) {
-      const u32x4_t* k = reinterpret_cast<const u32x4_t*>(key);
-      for (int e = r.lane; e < r.a.q_heads; e += 64) {
-        double dot = 0.0;
-#pragma unroll 4
-        for (int p = 0; p < kIndexDims / 8; ++p) {
-          const u32x4_t kx = k[p];
-          const uint16_t* qe = r.s_q + e * kQPitch + p * 8;
-          const u32x4_t qx = *reinterpret_cast<const u32x4_t*>(qe);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            dot = fma((double)low_half(kx[i]), (double)low_half(qx[i]), dot);
-            dot = fma((double)high_half(kx[i]), (double)high_half(qx[i]), dot);
-          }
-        }
-        sum += (r.wrow ? (double)r.wrow[e] : 1.0) * positive(dot);
-      }
-    } else {
-      constexpr int PER = IndexShape<KIND>::DIMS / 64;
-#pragma unroll
-      for (int i = 0; i < PER / 2; ++i) {
-        const int d = r.lane * PER + 2 * i;
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(key + 2 * d);
-        sum = fma((double)low_half(x), s.q[d], sum);
-        sum = fma((double)high_half(x), s.q[d + 1], sum);
-      }
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-    return ordered(sum);
-  }
-
-  // Marks the m best of the rankable candidates: those above `sure`, and others by marks in their scores.
-  __device__ void choose(int m, float eps) {
-    zero = eps == 0.f;
-    all = zero || !(eps < INFINITY);
-    if (!all) {
-      uint32_t least = ~0u, most = 0, count = 0;
-      each([&](int j, float x) {
-        if (!rankable(j, x)) return;
-        ++count;
-        least = min(least, ordered32(x));
-        most = max(most, ordered32(x));
-      });
-      float from = unordered32(group_reduce<T>(least, s.wave_a, Least()));
-      float to = unordered32(group_reduce<T>(most, s.wave_b, Most()));
-      const int rankables = (int)group_reduce<T>(count, s.wave_a, Add());
-      all = rankables <= m;  // nothing to choose
-      int need = m;
-      for (int round = 0; round < 4 && from < to && !all; ++round) {
-        const float scale = (float)BINS / (to - from);
-        auto bin_of = [&](float x) { return min((int)((x - from) * scale), BINS - 1); };
-        for (int i = threadIdx.x; i < BINS; i += T) s.hist[i] = 0;
-        __syncthreads();
-        each([&](int j, float x) {
-          if (rankable(j, x) && x >= from && x <= to) atomicAdd(&s.hist[bin_of(x)], 1u);
-        });
-        __syncthreads();
-        find_bin<T, BINS>(s, s.hist, need);
-        const int bin = s.bin, in_bin = s.in_bin;
-        need -= s.above;
-        least = ~0u;
-        most = 0;
-        each([&](int j, float x) {
-          if (!rankable(j, x) || !(x >= from && x <= to) || bin_of(x) != bin) return;
-          least = min(least, ordered32(x));
-          most = max(most, ordered32(x));
-        });
-        from = unordered32(group_reduce<T>(least, s.wave_a, Least()));
-        to = unordered32(group_reduce<T>(most, s.wave_b, Most()));
-        if (in_bin <= LIST / 4) break;
-      }
-      // rounded outwards
-      sure = nextafterf(to + 2.f * eps, INFINITY);
-      maybe = nextafterf(from - 2.f * eps, -INFINITY);
-    }
-    // how many are sure, which are open
-    if (threadIdx.x == 0) s.count = 0;
-    __syncthreads();
-    uint32_t n_sure = 0;
-    each([&](int j, float x) {
-      if (!rankable(j, x)) return;
-      if (is_sure(x)) {
-        ++n_sure;
-      } else if (is_open(x)) {
-        const int at = atomicAdd(&s.count, 1);
-        if (at < LIST) s.list[at] = j;
-      }
-    });
-    const int need = m - (int)group_reduce<T>(n_sure, s.wave_a, Add());
-    const int open = s.count;
-    __syncthreads();
-    if (need >= open) {  // (all of them: fewer rankable candidates than asked for)
-      each([&](int j, float x) {
-        if (rankable(j, x) && is_open(x)) r.scores[j] = __uint_as_float(kWin);
-      });
-    } else if (open <= LIST && !zero) {
-      for (int i = r.wave; i < open; i += WAVES) {
-        const uint64_t x = exact(s.list[i]);
-        if (r.lane == 0) s.score[i] = x;
-      }
-      __syncthreads();
-      for (int i = threadIdx.x; i < open; i += T) {
-        const uint64_t x = s.score[i];
-        const int j = s.list[i];
-        int better = 0;
-        for (int y = 0; y < open; ++y)
-          better += s.score[y] > x || (s.score[y] == x && s.list[y] < j);
-        if (better < need) r.scores[j] = __uint_as_float(kWin);
-      }
-    } else {
-      choose_many(need);
-    }
-    __syncthreads();  // the marks are read by other waves
-  }
-
-  // More open candidates than the list holds (thousands of equal scores, or no error bound): the need-th
-  // largest in 64 bits is found 8 bits at a time, the scores worked out anew each time.
-  __device__ void choose_many(int need) {
-    uint64_t prefix = zero ? ordered(0.0) : 0;
-    for (int shift = 56; shift >= 0 && !zero; shift -= 8) {
-      for (int i = threadIdx.x; i < BINS; i += T) s.hist[i] = 0;
-      __syncthreads();
-      open_ones([&](int j) {
-        const uint64_t x = exact(j);
-        if (r.lane == 0 && (shift == 56 || x >> (shift + 8) == prefix))
-          atomicAdd(&s.hist[(int)(x >> shift) & 255], 1u);
-      });
-      __syncthreads();
-      find_bin<T, BINS>(s, s.hist, need);
-      prefix = prefix << 8 | (uint64_t)s.bin;
-      need -= s.above;
-      __syncthreads();
-    }
-    const int equal = need;  // of the need-th score, how many are wanted
-    uint32_t mine = 0;
-    open_ones([&](int j) { mine += zero || exact(j) == prefix; });
-    if (r.lane == 0) s.wave_b[r.wave] = mine;
-    __syncthreads();
-    int before = 0;
-    for (int i = 0; i < r.wave; ++i) before += (int)s.wave_b[i];
-    open_ones([&](int j) {
-      const uint64_t x = zero ? prefix : exact(j);
-      const bool wins = x > prefix || (x == prefix && before < equal);
-      before += x == prefix;
-      if (wins && r.lane == 0) r.scores[j] = __uint_as_float(kWin);
-    });
-  }
-  // f(j) for this wave's open candidates in ascending order, j the same in all lanes.
-  template <class F>
-  __device__ __forceinline__ void open_ones(F&& f) const {
-    for (int base = lo; base < hi; base += 64) {
-      const int j = base + r.lane;
-      const float x = j < hi ? r.scores[j] : 0.f;
-      uint64_t todo = __ballot(j < hi && rankable(j, x) && is_open(x));
-      while (todo) {
-        f(base + __builtin_ctzll(todo));
-        todo &= todo - 1;
-      }
-    }
-  }
-
-  // The marked and the sure ones in ascending order (scored false: all that are not padding).
-  __device__ __forceinline__ void write(bool scored) const {
-    const int own = r.own();
-    auto is_in = [&](int j) {
-      if (j >= hi || j == own) return false;
-      if (!scored) {
-        const uint8_t* at;
-        int record;
-        return find_row<KEYS>(r.a, r.q, r.h, j, at, record);
-      }
-      const float x = r.scores[j];
-      const uint32_t b = __float_as_uint(x);
-      return b != kPad && (b == kWin || r.forced(j) || is_sure(x));
-    };
-    int mine = 0;
-    for (int base = lo; base < hi; base += 64) mine += __popcll(__ballot(is_in(base + r.lane)));
-    __syncthreads();
-    if (r.lane == 0) s.wave_a[r.wave] = (uint32_t)mine;
-    __syncthreads();
-    int at = 0, total = 0;
-    for (int i = 0; i < WAVES; ++i) {
-      if (i < r.wave) at += (int)s.wave_a[i];
-      total += (int)s.wave_a[i];
-    }
-    for (int base = lo; base < hi; base += 64) {
-      const bool in = is_in(base + r.lane);
-      const uint64_t mask = __ballot(in);
-      const int place = at + (int)__popcll(mask & ((1ull << r.lane) - 1));
-      if (in && place < r.a.top_k) r.put(place, base + r.lane);
-      at += __popcll(mask);
-    }
-    r.finish(total);
-  }
-};
-
 // Scores of the open candidates s.list[0 .. n) in 64 bits, to s.score.
 //
 // Keys: fp64 MFMAs, 16 heads by 16 candidates: a wave has a tile of heads and 16 candidates; a lane holds
@@ -623,6 +385,268 @@ __device__ __forceinline__ void score_open(const Row<KIND, T>& r, S& s, int n) {
     __syncthreads();
   }
 }
+
+// The choice from scores in memory, whatever they are: a few passes where 64 bits settle few candidates,
+// and where they have to settle many, the scores worked out anew in each of up to nine passes.
+template <int KIND, int T, int BINS, int LIST, class S>
+struct Stream {
+  static constexpr bool KEYS = KIND == HISPARSE_INDEX_KEYS;
+  static constexpr int WAVES = T / 64;
+  const Row<KIND, T>& r;
+  S& s;
+  int lo, hi;           // this wave's candidates
+  bool all, zero;       // every candidate is open; every score is 0
+  float sure, maybe;    // above sure: chosen; below maybe: not
+
+  __device__ Stream(const Row<KIND, T>& row, S& shared) : r(row), s(shared) {
+    const int span = (((r.seen + WAVES - 1) / WAVES) + 255) & ~255;
+    lo = (int)min((int64_t)r.wave * span, (int64_t)r.seen);
+    hi = (int)min((int64_t)(r.wave + 1) * span, (int64_t)r.seen);
+    all = zero = false;
+    sure = maybe = INFINITY;
+  }
+  __device__ __forceinline__ bool rankable(int j, float x) const {
+    return __float_as_uint(x) != kPad && !r.forced(j);
+  }
+  __device__ __forceinline__ bool is_sure(float x) const { return !all && x > sure; }
+  __device__ __forceinline__ bool is_open(float x) const { return all || (x >= maybe && !(x > sure)); }
+
+  // f(j, score) for this wave's candidates, four in a row per lane.
+  template <class F>
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int base = lo + r.lane * 4; base < hi; base += 256) {
+      const f32x4_t x = *reinterpret_cast<const f32x4_t*>(r.scores + base);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (base + i < hi) f(base + i, x[i]);
+    }
+  }
+
+  // Marks the m best of the rankable candidates: those above `sure`, and others by marks in their scores.
+  __device__ void choose(int m, float eps) {
+    zero = eps == 0.f;
+    all = zero || !(eps < INFINITY);
+    if (!all) {
+      uint32_t least = ~0u, most = 0, count = 0;
+      each([&](int j, float x) {
+        if (!rankable(j, x)) return;
+        ++count;
+        least = min(least, ordered32(x));
+        most = max(most, ordered32(x));
+      });
+      float from = unordered32(group_reduce<T>(least, s.wave_a, Least()));
+      float to = unordered32(group_reduce<T>(most, s.wave_b, Most()));
+      const int rankables = (int)group_reduce<T>(count, s.wave_a, Add());
+      all = rankables <= m;  // nothing to choose
+      int need = m;
+      for (int round = 0; round < 4 && from < to && !all; ++round) {
+        const float scale = (float)BINS / (to - from);
+        auto bin_of = [&](float x) { return min((int)((x - from) * scale), BINS - 1); };
+        for (int i = threadIdx.x; i < BINS; i += T) s.hist[i] = 0;
+        __syncthreads();
+        each([&](int j, float x) {
+          if (rankable(j, x) && x >= from && x <= to) atomicAdd(&s.hist[bin_of(x)], 1u);
+        });
+        __syncthreads();
+        find_bin<T, BINS>(s, s.hist, need);
+        const int bin = s.bin, in_bin = s.in_bin;
+        need -= s.above;
+        least = ~0u;
+        most = 0;
+        each([&](int j, float x) {
+          if (!rankable(j, x) || !(x >= from && x <= to) || bin_of(x) != bin) return;
+          least = min(least, ordered32(x));
+          most = max(most, ordered32(x));
+        });
+        from = unordered32(group_reduce<T>(least, s.wave_a, Least()));
+        to = unordered32(group_reduce<T>(most, s.wave_b, Most()));
+        if (in_bin <= LIST / 4) break;
+      }
+      // rounded outwards
+      sure = nextafterf(to + 2.f * eps, INFINITY);
+      maybe = nextafterf(from - 2.f * eps, -INFINITY);
+    }
+    // how many are sure, which are open
+    if (threadIdx.x == 0) s.count = 0;
+    __syncthreads();
+    uint32_t n_sure = 0;
+    each([&](int j, float x) {
+      if (!rankable(j, x)) return;
+      if (is_sure(x)) {
+        ++n_sure;
+      } else if (is_open(x)) {
+        const int at = atomicAdd(&s.count, 1);
+        if (at < LIST) s.list[at] = j;
+      }
+    });
+    const int need = m - (int)group_reduce<T>(n_sure, s.wave_a, Add());
+    const int open = s.count;
+    __syncthreads();
+    if (need >= open) {  // (all of them: fewer rankable candidates than asked for)
+      each([&](int j, float x) {
+        if (rankable(j, x) && is_open(x)) r.scores[j] = __uint_as_float(kWin);
+      });
+    } else if (open <= LIST && !zero) {
+      score_open<KIND, T>(r, s, open);
+      for (int i = threadIdx.x; i < open; i += T) {
+        const uint64_t x = s.score[i];
+        const int j = s.list[i];
+        int better = 0;
+        for (int y = 0; y < open; ++y)
+          better += s.score[y] > x || (s.score[y] == x && s.list[y] < j);
+        if (better < need) r.scores[j] = __uint_as_float(kWin);
+      }
+    } else {
+      choose_many(need);
+    }
+    __syncthreads();  // the marks are read by other waves
+  }
+
+  // f(n) for LIST candidates after the other, the n open ones among them in ascending order in s.list, and
+  // unless every score is 0, their scores in s.score.
+  template <class F>
+  __device__ __forceinline__ void lists(F&& f) {
+    constexpr int PER = LIST / T;
+#pragma unroll 1
+    for (int base = 0; base < r.seen; base += LIST) {
+      const int j0 = base + (int)threadIdx.x * PER;
+      uint32_t open = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (j0 + i < r.seen) {
+          const float x = r.scores[j0 + i];
+          open |= (uint32_t)(rankable(j0 + i, x) && is_open(x)) << i;
+        }
+      const int c = __popc(open), inc = wave_inclusive(c);
+      __syncthreads();  // what the last list left has been read
+      if (r.lane == 63) s.wave_a[r.wave] = (uint32_t)inc;
+      __syncthreads();
+      int at = inc - c, n = 0;
+      for (int i = 0; i < WAVES; ++i) {
+        at += i < r.wave ? (int)s.wave_a[i] : 0;
+        n += (int)s.wave_a[i];
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (open >> i & 1) s.list[at++] = j0 + i;
+      __syncthreads();
+      if (n == 0) continue;
+      if (!zero) score_open<KIND, T>(r, s, n);
+      f(n);
+    }
+    __syncthreads();
+  }
+
+  // More open candidates than the list holds (thousands of equal scores, or no error bound): the need-th
+  // largest in 64 bits is found 8 bits at a time, the scores worked out anew each time, until those that
+  // share its first bits are all equal or all wanted. (32768 equal keys of 64 heads: 6.5 ms; a candidate a wave
+  // at a time took 115.)
+  __device__ void choose_many(int need) {
+    uint64_t prefix = 0;
+    int shift = 0;
+    if (!zero) {
+      for (shift = 56;; shift -= 8) {
+        for (int i = threadIdx.x; i < 256; i += T) s.win[i] = 0;
+        if (threadIdx.x == 0) {
+          s.least = ~0ull;
+          s.most = 0;
+        }
+        uint64_t least = ~0ull, most = 0;
+        lists([&](int n) {
+          for (int i = threadIdx.x; i < n; i += T) {
+            const uint64_t x = s.score[i];
+            if (shift < 56 && x >> (shift + 8) != prefix) continue;
+            atomicAdd(&s.win[(int)(x >> shift) & 255], 1u);
+            least = min(least, x);
+            most = max(most, x);
+          }
+        });
+        atomicMin(&s.least, (unsigned long long)least);
+        atomicMax(&s.most, (unsigned long long)most);
+        __syncthreads();
+        if (s.least == s.most) {
+          prefix = s.least;
+          shift = 0;
+          break;
+        }
+        if (r.wave == 0) {  // four bins a lane, from the top
+          uint32_t c[4], sum = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum += c[i] = s.win[255 - (r.lane * 4 + i)];
+          int before = wave_inclusive((int)sum) - (int)sum;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (before < need && before + (int)c[i] >= need) {
+              s.bin = 255 - (r.lane * 4 + i);
+              s.above = before;
+              s.in_bin = (int)c[i];
+            }
+            before += (int)c[i];
+          }
+        }
+        __syncthreads();
+        prefix = prefix << 8 | (uint64_t)s.bin;
+        need -= s.above;
+        const bool done = shift == 0 || s.in_bin == need;
+        __syncthreads();
+        if (done) break;
+      }
+    }
+    // above the prefix: chosen; with it: the first ones
+    int before = 0;
+    lists([&](int n) {
+      for (int i0 = 0; i0 < n; i0 += T) {
+        const int i = i0 + (int)threadIdx.x;
+        const uint64_t x = i < n && !zero ? s.score[i] >> shift : prefix;
+        const uint64_t equal = __ballot(i < n && x == prefix);
+        if (r.lane == 0) s.wave_b[r.wave] = (uint32_t)__popcll(equal);
+        __syncthreads();
+        int mine = before + (int)__popcll(equal & ((1ull << r.lane) - 1));
+        for (int w = 0; w < WAVES; ++w) {
+          mine += w < r.wave ? (int)s.wave_b[w] : 0;
+          before += (int)s.wave_b[w];
+        }
+        __syncthreads();
+        if (i < n && (x > prefix || (x == prefix && mine < need)))
+          r.scores[s.list[i]] = __uint_as_float(kWin);
+      }
+    });
+  }
+
+  // The marked and the sure ones in ascending order (scored false: all that are not padding).
+  __device__ __forceinline__ void write(bool scored) const {
+    const int own = r.own();
+    auto is_in = [&](int j) {
+      if (j >= hi || j == own) return false;
+      if (!scored) {
+        const uint8_t* at;
+        int record;
+        return find_row<KEYS>(r.a, r.q, r.h, j, at, record);
+      }
+      const float x = r.scores[j];
+      const uint32_t b = __float_as_uint(x);
+      return b != kPad && (b == kWin || r.forced(j) || is_sure(x));
+    };
+    int mine = 0;
+    for (int base = lo; base < hi; base += 64) mine += __popcll(__ballot(is_in(base + r.lane)));
+    __syncthreads();
+    if (r.lane == 0) s.wave_a[r.wave] = (uint32_t)mine;
+    __syncthreads();
+    int at = 0, total = 0;
+    for (int i = 0; i < WAVES; ++i) {
+      if (i < r.wave) at += (int)s.wave_a[i];
+      total += (int)s.wave_a[i];
+    }
+    for (int base = lo; base < hi; base += 64) {
+      const bool in = is_in(base + r.lane);
+      const uint64_t mask = __ballot(in);
+      const int place = at + (int)__popcll(mask & ((1ull << r.lane) - 1));
+      if (in && place < r.a.top_k) r.put(place, base + r.lane);
+      at += __popcll(mask);
+    }
+    r.finish(total);
+  }
+};
 
 // eps, and the range of scores, that a long row's kernels agree on.
 struct LongRow {
