@@ -879,7 +879,7 @@ hisparse_status_t hisparse_validate_index(const hisparse_index_desc_t* index);
  *   d_index        out: one or two rows of 128 per record and kv head.
  * Bounds are exact; a NaN in a dim makes its bounds NaN. Means are summed in fp32 in a fixed order and rounded
  * to bf16 once. Index records of other records keep what they hold. If two requests share a record that
- * both write to, its row is that of one of them.
+ * both write to, each dim of its rows is that of one of them.
  * HISPARSE_ERR_INVALID_ARG for bad or differing descriptors (tokens_per_record alike in all three),
  * index kind KEYS, null or misaligned pointers (pool and index 16 bytes), a head_stride that lets kv heads'
  * index records overlap, or d_chunk_start NULL and total_tokens < num_requests * max_chunk;

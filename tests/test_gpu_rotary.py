@@ -204,3 +204,19 @@ def test_captured_and_replayed_on_another_stream():
         g.replay()
         torch.cuda.synchronize()
         check(y, d, p, v, 0)
+
+
+def test_offsets_beyond_four_gibibytes():
+    """Rows 256 MiB apart, read there, written there, and scattered there."""
+    n, apart = 20, 1 << 27
+    d, pos, x = desc(64, HALF), positions(n, 1), data((n, 1, 128), 2)
+    far = torch.empty(2 * n * apart, dtype=torch.bfloat16, device="cuda").view(2 * n, 1, apart)[..., :128]
+    far[:n] = x.cuda()
+    to = torch.arange(n, 2 * n).flip(0).cuda()
+    near = torch.zeros((n, 1, 128), dtype=torch.bfloat16, device="cuda")
+    turn(d, pos, rows_of(far[:n], near))
+    check(near, d, pos, x, 0)
+    turn(d, pos, rows_of(x.cuda(), far, 0, to))
+    check(far[n:].flip(0), d, pos, x, 0)
+    turn(d, pos, rows_of(far[:n], far[:n]))
+    check(far[:n], d, pos, x, 0)

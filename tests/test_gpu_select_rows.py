@@ -207,3 +207,20 @@ def test_two_calls_at_once(kind):
     torch.cuda.synchronize()
     a.compare()
     b.compare()
+
+
+@pytest.mark.parametrize("kind", [KEYS, BOUNDS, MEANS])
+@pytest.mark.parametrize("new", [1, 9])
+def test_offsets_beyond_four_gibibytes(kind, new):
+    """Index records 256 MiB apart."""
+    t = 16 if kind == KEYS else 1
+    c = Case(kind, t, [new], [21 * t if kind == KEYS else 21], k=5, last=1, heads=2, spare=3)
+    c.device()
+    apart = 1 << 28
+    records, row = c.index.shape[0], c.index[0].numel()
+    far = torch.empty(records * apart // 2, dtype=torch.bfloat16, device="cuda").view(records, apart // 2)
+    far[:, :row] = c.index.flatten(1).cuda()
+    c.x.record_stride = apart
+    c.call(index=far)
+    torch.cuda.synchronize()
+    c.compare()

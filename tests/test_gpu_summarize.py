@@ -228,3 +228,25 @@ def test_captured_and_replayed_on_another_stream():
         g.replay()
         torch.cuda.synchronize()
         check(ref.BOUNDS, pool, buf, expected(ref.BOUNDS, pool, s, l, table, 32, 64))
+
+
+@pytest.mark.parametrize("kind", [ref.BOUNDS, ref.MEANS])
+def test_offsets_beyond_four_gibibytes(kind):
+    """Records and index records 256 MiB apart."""
+    pool = Pool(BF, 16, 2, 20, 9)
+    table = tables(pool, 20, 1, 4)
+    apart = 1 << 28
+    wide = torch.empty(20 * apart, dtype=torch.uint8, device="cuda").view(20, apart)
+    size = pool.pool[0].numel()
+    wide[:, :size] = pool.pool.flatten(1)
+    pool.desc.record_stride = apart
+    w = ref.INDEX_ROWS[kind] * 128
+    out = torch.empty(20 * apart // 2, dtype=torch.int16, device="cuda").view(20, apart // 2)
+    out[:, :2 * w] = MARK
+    desc = hs.IndexDesc(kind, 16, 20, apart, 2 * w, 0)
+    b = hs.BatchDesc(1, 2, 320, 320, 20, 16, 20, 0)
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    hs.hisparse_summarize_records(pool.desc, desc, b, wide, ints(table), None, ints([317]), out,
+                                  torch.cuda.current_stream())
+    check(kind, pool, out[:, :2 * w].unflatten(1, (2, w)),
+          expected(kind, pool, None, [317], table, 320, 320))
