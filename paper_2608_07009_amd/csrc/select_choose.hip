@@ -186,11 +186,12 @@ struct Row {
     return (int)group_reduce<T>(n, s.wave_a, Add());
   }
 
-  // eps (0: every score is 0), the range of the scores, and the queries in LDS.
+  // eps (0: every score is 0), the range of the scores, and the queries in LDS; or the range alone.
   template <class S>
-  __device__ __forceinline__ float error_bound(S& s, float& from, float& to) const {
+  __device__ __forceinline__ float error_bound(S& s, float& from, float& to, bool range_only = false) const {
     double A = 0.0, W = 0.0, Q = 0.0;
-    if constexpr (KEYS) {  // 16 lanes a query
+    if (range_only) {
+    } else if constexpr (KEYS) {  // 16 lanes a query
       const uint16_t* qrow = a.q + (int64_t)token * a.q_stride + (int64_t)h * a.q_heads * kIndexDims;
       const int c = threadIdx.x & 15;
       for (int e = threadIdx.x >> 4; e < a.q_heads; e += T / 16) {
@@ -903,7 +904,7 @@ __global__ __launch_bounds__(T, T == 512 ? 4 : 1) void choose_kernel(SelectArgs 
 
 constexpr int kLongThreads = 1024, kLongGroups = kPart / kLongThreads / 4;
 
-// The row's histogram, a part of it each.
+// The row's histogram, a part of it each; the first part's workgroup has the error bound too.
 template <int KIND>
 __global__ __launch_bounds__(kLongThreads) void narrow_kernel(SelectArgs a) {
   using S = Shared<KIND, kLongThreads, kLongBins, 64, 32>;
@@ -916,9 +917,9 @@ __global__ __launch_bounds__(kLongThreads) void narrow_kernel(SelectArgs a) {
   if (!r.find(local, (int)slot - local * a.heads)) return;
   if (r.seen <= kRegisterRow || part * kPart >= r.seen) return;
   LongRow row;
-  row.eps = r.error_bound(s, row.from, row.to);
+  row.eps = r.error_bound(s, row.from, row.to, part != 0);
   if (part == 0 && threadIdx.x == 0) reinterpret_cast<LongRow*>(a.bound)[slot] = row;
-  if (!row.divisible()) return;
+  if (!Division<kLongBins>::divides(row.from, row.to)) return;
   const Division<kLongBins> d(row.from, row.to);
   for (int i = threadIdx.x; i < kLongBins; i += kLongThreads) s.hist[i] = 0;
   __syncthreads();
