@@ -806,7 +806,8 @@ __global__ __launch_bounds__(T, T == 512 ? 4 : 1) void choose_kernel(SelectArgs 
       else above = 0;
       __syncthreads();
       const int total = find_bin<T, BINS>(s, s.hist, m - (int)above);
-      if (total + (int)above <= m) {
+      // (later rounds see a bin of the one before, whose last candidate may be the m-th)
+      if (round == 0 && total <= m) {
         any = true;
         break;
       }
