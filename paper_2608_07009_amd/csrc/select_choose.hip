@@ -275,6 +275,9 @@ struct Row {
     const float N = __uint_as_float(norm);
     if (A == 0.0 && N < INFINITY) return 0.f;
     if (N == 0.f && A < INFINITY) return 0.f;
+    // A head whose products may leave fp32 leaves no bound, however small its weight is (their sums are NaN,
+    // or infinities that the weight does not bring back).
+    if (KEYS && !((float)Q * 1.01f * N < INFINITY)) return INFINITY;
     // the last term: what inputs and sums below the normal range are off by
     const float AN = (float)A * 1.01f * N;
     const float c = KEYS ? 0x1.4p-16f + (float)(a.q_heads + 1) * 0x1.4p-24f : 0x1.4p-15f;

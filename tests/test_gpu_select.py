@@ -448,3 +448,18 @@ def test_starts_that_do_not_ascend_stay_in_bounds():
         c.call(sel=room[2:-2])
         torch.cuda.synchronize()
         assert bool((room[:2] == MARK).all()) and bool((room[-2:] == MARK).all())
+
+
+@pytest.mark.parametrize("new,cand", [(1, 700), (5, 700), (1, 9000), (2, 33000), (9, 33000)])
+@pytest.mark.parametrize("scale,small", [(1e20, 0.0), (1e20, 1e-20), (1e21, 0.0), (1e21, 1e-21)])
+def test_products_that_leave_the_range_under_small_weights(new, cand, scale, small):
+    """Keys: the products of some heads pass the largest number of fp32 (in 64 bits they are of 1e39 or 1e40),
+    the weighted scores do not."""
+    def data(shape, g):
+        return (torch.randn(shape, generator=g) * 1e18).to(torch.bfloat16)
+    c = Case(KEYS, 1, [new], [cand], k=40, q_heads=4, data=data, seed=cand + new)
+    q = c.q.view(c.total, 4, 128)
+    q[:, 1:3] = (q[:, 1:3].float() * scale).to(torch.bfloat16)
+    c.w[:, 1] = small
+    c.w[:, 2] = -small
+    c.check()
