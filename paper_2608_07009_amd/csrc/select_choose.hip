@@ -278,10 +278,11 @@ struct Row {
     // A head whose products may leave fp32 leaves no bound, however small its weight is (their sums are NaN,
     // or infinities that the weight does not bring back).
     if (KEYS && !((float)Q * 1.01f * N < INFINITY)) return INFINITY;
-    // the last term: what inputs and sums below the normal range are off by
+    // the last term: what inputs and sums below the normal range are off by, before the weights and after
+    // (never 0: that every score is 0 has been told above)
     const float AN = (float)A * 1.01f * N;
     const float c = KEYS ? 0x1.4p-16f + (float)(a.q_heads + 1) * 0x1.4p-24f : 0x1.4p-15f;
-    return AN * c + (float)W * (N + (float)Q + 1.f) * 0x1p-118f;
+    return AN * c + ((float)W * (N + (float)Q + 1.f) + 1.f) * 0x1p-118f;
   }
 
   // Writes candidate j (-1: none) to a place of the list.

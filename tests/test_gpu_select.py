@@ -463,3 +463,17 @@ def test_products_that_leave_the_range_under_small_weights(new, cand, scale, sma
     c.w[:, 1] = small
     c.w[:, 2] = -small
     c.check()
+
+
+@pytest.mark.parametrize("new,cand", [(1, 700), (6, 700), (1, 9000), (2, 33000)])
+@pytest.mark.parametrize("scale_q,scale_x,scale_w", [(1e-18, 1e-18, 1e-10), (1e-15, 1e-15, 1e-16),
+                                                     (1.0, 1.0, 1e-42), (1e-4, 1.0, 1e-38)])
+def test_weighted_scores_below_the_range(new, cand, scale_q, scale_x, scale_w):
+    """Keys: weighted scores that fp32 holds with a few bits, or not at all; all are fine in 64 bits."""
+    def data(shape, g):
+        return (torch.randn(shape, generator=g) * scale_x).to(torch.bfloat16)
+    c = Case(KEYS, 1, [new], [cand], k=40, q_heads=4, data=data, seed=cand + new)
+    c.q = (c.q.float() * scale_q).to(torch.bfloat16)
+    c.w = c.w * scale_w
+    assert bool((c.w != 0).all())
+    c.check()
