@@ -35,7 +35,7 @@ struct RowSet {
   uint32_t items;      // pieces of a token: heads * per_head
   uint32_t per_head;   // pieces of a head
   FastDiv div_per_head;
-  int32_t first, dims;
+  int32_t first;
 };
 
 struct RotaryArgs {
@@ -43,7 +43,7 @@ struct RotaryArgs {
   double turns[kMaxPairs];  // of a pair, a position
   RowSet set[HISPARSE_ROTARY_MAX_ROWS];
   float magnitude, sign;
-  int32_t tokens, pairs, sets;
+  int32_t tokens, pairs;
   uint32_t items;           // of a token, all sets
   int32_t group_tokens;     // tokens of a workgroup
   uint32_t slice;           // items of a workgroup (of each of its tokens)
@@ -157,6 +157,46 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotaryArgs a) {
 
 bool finite(double x) { return x - x == 0.0; }
 
+// Pieces of a token that one launch turns: 65535 workgroups of it, four pieces a thread.
+constexpr int kItems = 4 * kThreads;
+constexpr int64_t kMostItems = 65535ll * kItems;
+
+// The rows of the first `sets` of a.set, in as many launches as the tokens take (of 2^32 threads).
+bool launch_rows(RotaryArgs& a, int sets, const int32_t* positions, int32_t num_tokens, bool wide, bool half,
+                 hipStream_t s) {
+  // Four items a thread where there is enough to fill the chip, one workgroup of a token otherwise. (16384
+  // tokens of 32 + 8 heads of 128: 61.0 us; with one item a thread 71.4, two 61.6, eight 63.5.)
+  const int64_t items = a.items;
+  a.slice = (uint32_t)std::min<int64_t>(items, kItems);
+  a.group_tokens = 1;
+  const int most = std::min<int>(kItems / (int)a.slice, kTableBytes / 8 / a.pairs);
+  while (a.group_tokens * 2 <= most && (int64_t)num_tokens * items / (a.group_tokens * a.slice) > 2048)
+    a.group_tokens *= 2;
+  while (a.group_tokens == 1 && a.slice > (uint32_t)kThreads &&
+         (int64_t)num_tokens * items / a.slice < 1024)
+    a.slice = (a.slice + 1) / 2;
+  a.div_slice = make_fastdiv(a.slice);
+  const int64_t slices = (items + a.slice - 1) / a.slice;
+  const int64_t step = (int64_t)UINT32_MAX / kThreads / slices * a.group_tokens;
+  for (int64_t token0 = 0; token0 < num_tokens; token0 += step) {
+    a.positions = positions + token0;
+    a.tokens = (int32_t)std::min<int64_t>(step, num_tokens - token0);
+    const dim3 grid((unsigned)((a.tokens + (int64_t)a.group_tokens - 1) / a.group_tokens), (unsigned)slices);
+    if (wide && half) hipLaunchKernelGGL((rotate_kernel<true, true>), grid, dim3(kThreads), 0, s, a);
+    else if (wide) hipLaunchKernelGGL((rotate_kernel<false, true>), grid, dim3(kThreads), 0, s, a);
+    else if (half) hipLaunchKernelGGL((rotate_kernel<true, false>), grid, dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((rotate_kernel<false, false>), grid, dim3(kThreads), 0, s, a);
+    if (hipGetLastError() != hipSuccess) return false;
+    for (int i = 0; i < sets; ++i) {
+      RowSet& x = a.set[i];
+      x.in += a.tokens * x.in_token;
+      if (x.out_rows) x.out_rows += a.tokens;
+      else x.out += a.tokens * x.out_token;
+    }
+  }
+  return true;
+}
+
 }  // namespace
 }  // namespace hisparse
 
@@ -234,60 +274,48 @@ hisparse_status_t hisparse_rotate_tokens(const hisparse_rotary_desc_t* d, int32_
   // (elements first: at most 4 * 2^47)
   if (elements >= (1ll << 38) || elements > ((1ll << 38) - 1) / num_tokens)
     return HISPARSE_ERR_UNSUPPORTED;
-  a.positions = d_positions;
-  a.tokens = num_tokens;
   a.pairs = d->dims / 2;
-  a.sets = num_rows;
   a.magnitude = (float)d->magnitude;
   a.sign = d->flags & HISPARSE_ROTARY_BACK ? -a.magnitude : a.magnitude;
   for (int i = 0; i < a.pairs; ++i) a.turns[i] /= 2.0 * M_PI;
-  int64_t items = 0;
-  for (int i = 0; i < num_rows; ++i) {
-    const hisparse_rotary_rows_t& r = rows[i];
-    RowSet& s = a.set[i];
-    s.in = reinterpret_cast<const uint16_t*>(r.d_in);
-    s.out = reinterpret_cast<uint16_t*>(r.d_out);
-    s.out_rows = r.d_out_rows;
-    s.num_out_rows = r.num_out_rows;
-    s.in_token = r.in_token_stride;
-    s.in_head = r.in_head_stride;
-    s.out_token = r.out_token_stride;
-    s.out_head = r.out_head_stride;
-    const int others = r.d_in == r.d_out ? 0 : r.dims - d->dims;
-    s.per_head = (uint32_t)(wide ? d->dims / 16 + others / 16 : a.pairs + others);
-    s.div_per_head = make_fastdiv(s.per_head);
-    s.first = r.first;
-    s.dims = r.dims;
-    items += (int64_t)r.heads * s.per_head;
-    if (items > INT32_MAX / 2) return HISPARSE_ERR_UNSUPPORTED;
-    s.items = (uint32_t)((int64_t)r.heads * s.per_head);
-  }
-  a.items = (uint32_t)items;
-  // Four items a thread where there is enough to fill the chip, one workgroup of a token otherwise. (16384
-  // tokens of 32 + 8 heads of 128: 61.0 us; with one item a thread 71.4, two 61.6, eight 63.5.)
-  constexpr int kItems = 4 * kThreads;
-  a.slice = (uint32_t)std::min<int64_t>(items, kItems);
-  a.group_tokens = 1;
-  const int most = std::min<int>(kItems / (int)a.slice, kTableBytes / 8 / a.pairs);
-  while (a.group_tokens * 2 <= most && (int64_t)num_tokens * items / (a.group_tokens * a.slice) > 2048)
-    a.group_tokens *= 2;
-  while (a.group_tokens == 1 && a.slice > (uint32_t)kThreads &&
-         (int64_t)num_tokens * items / a.slice < 1024)
-    a.slice = (a.slice + 1) / 2;
-  a.div_slice = make_fastdiv(a.slice);
-  const int64_t groups = ((int64_t)num_tokens + a.group_tokens - 1) / a.group_tokens;
-  const int64_t slices = (items + a.slice - 1) / a.slice;
-  if (slices > 65535 || groups * slices * kThreads > (int64_t)UINT32_MAX)
-    return HISPARSE_ERR_UNSUPPORTED;
   const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const StreamDevice device(s);
-  const dim3 grid((unsigned)groups, (unsigned)slices);
-  const bool half = d->layout == HISPARSE_ROTARY_HALF;
-  if (wide && half) hipLaunchKernelGGL((rotate_kernel<true, true>), grid, dim3(kThreads), 0, s, a);
-  else if (wide) hipLaunchKernelGGL((rotate_kernel<false, true>), grid, dim3(kThreads), 0, s, a);
-  else if (half) hipLaunchKernelGGL((rotate_kernel<true, false>), grid, dim3(kThreads), 0, s, a);
-  else hipLaunchKernelGGL((rotate_kernel<false, false>), grid, dim3(kThreads), 0, s, a);
-  return hipGetLastError() == hipSuccess ? HISPARSE_OK : HISPARSE_ERR_HIP;
+  // Arrays, and heads of the last one, until a launch has as many pieces of a token as its grid takes: almost
+  // always all of them. (A head has 65536 pieces at most.)
+  int32_t head0 = 0;
+  for (int i = 0; i < num_rows;) {
+    int sets = 0;
+    int64_t items = 0;
+    while (i < num_rows) {
+      const hisparse_rotary_rows_t& r = rows[i];
+      const int others = r.d_in == r.d_out ? 0 : r.dims - d->dims;
+      const uint32_t per_head = (uint32_t)(wide ? d->dims / 16 + others / 16 : a.pairs + others);
+      const int32_t heads = (int32_t)std::min<int64_t>(r.heads - head0, (kMostItems - items) / per_head);
+      if (heads == 0) break;
+      RowSet& x = a.set[sets++];
+      x.in = reinterpret_cast<const uint16_t*>(r.d_in) + head0 * r.in_head_stride;
+      x.out = reinterpret_cast<uint16_t*>(r.d_out) + head0 * r.out_head_stride;
+      x.out_rows = r.d_out_rows;
+      x.num_out_rows = r.num_out_rows;
+      x.in_token = r.in_token_stride;
+      x.in_head = r.in_head_stride;
+      x.out_token = r.out_token_stride;
+      x.out_head = r.out_head_stride;
+      x.per_head = per_head;
+      x.div_per_head = make_fastdiv(per_head);
+      x.first = r.first;
+      x.items = (uint32_t)heads * per_head;
+      items += x.items;
+      head0 += heads;
+      if (head0 < r.heads) break;
+      head0 = 0;
+      ++i;
+    }
+    a.items = (uint32_t)items;
+    if (!launch_rows(a, sets, d_positions, num_tokens, wide, d->layout == HISPARSE_ROTARY_HALF, s))
+      return HISPARSE_ERR_HIP;
+  }
+  return HISPARSE_OK;
 }
 
 }  // extern "C"

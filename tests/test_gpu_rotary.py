@@ -220,3 +220,62 @@ def test_offsets_beyond_four_gibibytes():
     check(far[n:].flip(0), d, pos, x, 0)
     turn(d, pos, rows_of(far[:n], far[:n]))
     check(far[:n], d, pos, x, 0)
+
+
+@pytest.mark.parametrize("layout", [HALF, INTER])
+def test_more_heads_than_one_launch_has_pieces_for(layout):
+    """A token of 2^20 and more heads: several launches, each of whole heads; a second array behind it."""
+    heads, whole = (1 << 20) + 50001, 130
+    d, pos = desc(126, layout), positions(1, 1)
+    x, z = data((1, heads, whole), 3).cuda(), data((1, 3, whole), 4)
+    y, zd = torch.full_like(x, 7.0), z.cuda()
+    turn(d, pos, rows_of(x, y, 3), rows_of(zd, zd, 1))
+    at = torch.cat((torch.arange(0, heads, 4099), torch.arange(heads - 70, heads)))
+    check(y[:, at.cuda()], d, pos, x[:, at.cuda()].cpu(), 3)
+    check(zd, d, pos, z, 1)
+    pair = torch.full((1,), pos.item(), dtype=torch.int32)
+    same = torch.empty((1, 5, whole), dtype=torch.bfloat16, device="cuda")
+    for h0 in range(0, heads - 5, 99991):  # the same as a call of its own
+        turn(d, pair, rows_of(x[:, h0:h0 + 5], same, 3))
+        assert torch.equal(same, y[:, h0:h0 + 5])
+
+
+def test_more_tokens_than_one_launch_has_workgroups_for():
+    """2^24 and more tokens, a workgroup each: one row read by all of them, written where a row map says so."""
+    n, dims = (1 << 24) + 77, 522
+    d = desc(2, HALF)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    x = data((1, 1, dims), 3)
+    where = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    at = torch.cat((torch.arange(0, n, 300007), torch.arange(n - 90, n)))
+    where[at.cuda()] = torch.arange(at.numel(), device="cuda").flip(0)
+    y = torch.full((at.numel() + 2, 1, dims), 7.0, dtype=torch.bfloat16, device="cuda")
+    xd = x.cuda()
+    r = hs.RotaryRows(xd.data_ptr(), y.data_ptr(), where.data_ptr(), at.numel(), 0, dims, dims, dims, 1, dims, 5)
+    hs.hisparse_rotate_tokens(d, n, pos, r, 1, torch.cuda.current_stream())
+    check(y[:-2].flip(0), d, at.int(), x.expand(at.numel(), 1, dims), 5, far=True)
+    assert bool((y[-2:] == 7.0).all())
+    r = hs.RotaryRows(xd.data_ptr(), y.data_ptr(), None, 0, 0, dims, dims, dims, 1, dims, 5)
+    hs.hisparse_rotate_tokens(d, 3, pos, r, 1, torch.cuda.current_stream())
+    check(y[:3], d, torch.arange(3).int(), x.expand(3, 1, dims), 5)
+
+
+def test_a_token_map_and_rows_of_several_launches():
+    """The same with an array in place beside it, tokens apart in memory and not read twice."""
+    n, heads = (1 << 22) + 5, 4200
+    d = desc(2, INTER)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") & 1023
+    x = torch.randn((n, 16), generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    keep = x.clone()
+    wide = data((1, heads, 2), 1).cuda()
+    where = torch.full((n,), -1, dtype=torch.int64, device="cuda")
+    y = torch.full((3, heads, 2), 7.0, dtype=torch.bfloat16, device="cuda")
+    last = torch.tensor([0, n // 2, n - 1])
+    where[last.cuda()] = torch.arange(3, device="cuda")
+    rows = (hs.RotaryRows * 2)(
+        hs.RotaryRows(x.data_ptr(), x.data_ptr(), None, 0, 16, 0, 16, 0, 1, 16, 8),
+        hs.RotaryRows(wide.data_ptr(), y.data_ptr(), where.data_ptr(), 3, 0, 2, heads * 2, 2, heads, 2, 0))
+    hs.hisparse_rotate_tokens(d, n, pos, rows, 2, torch.cuda.current_stream())
+    check(y, d, pos.cpu()[last], wide.cpu().expand(3, heads, 2), 0)
+    at = torch.cat((torch.arange(0, n, 50021), torch.arange(n - 90, n)))
+    check(x[at.cuda(), None], d, pos.cpu()[at], keep.cpu()[at][:, None], 8)
