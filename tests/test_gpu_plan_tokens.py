@@ -179,3 +179,27 @@ def test_optional_outputs():
         c.used = 0
         assert c.d["pos"].tolist()[:-1] == c.expected()[4]
         assert c.d["table"].tolist() == c.expected()[0]
+
+
+@pytest.mark.parametrize("n", [2047, 2048, 2049])
+def test_the_border_between_one_launch_and_two(n):
+    """Batches of up to 2048 rows and 2048 requests are one launch; each of the two numbers around it."""
+    new, kv = ragged(70, 60, 200, n)
+    while sum(new) > n - 3:
+        new[new.index(max(new))] //= 2
+    Case(new, kv, 16, n, 30).check()             # rows behind the last request's
+    Case([n], [5], 16, n, 200).check()           # and none
+    new, kv = ragged(n, 1, 30, 9)
+    Case(new, kv, 4, min(sum(new), 2048), 10).check()
+    new = [0] * n
+    new[0] = new[-1] = 3
+    Case(new, kv, 4, 6, 10).check()
+    for total in (n, 7000):                      # lengths and the count updated in place
+        new, kv = ragged(90, 20, 70, n)
+        c = Case(new, kv, 16, total, 12, spare=400)
+        c.device()
+        c.call(out=c.d["kv"], used_out=c.d["used"])
+        table, start, out, used, pos, slots = c.expected()
+        assert c.d["kv"].tolist() == out and c.d["used"].tolist() == [used]
+        assert c.d["start"].tolist()[:-1] == start and c.d["table"].tolist() == table
+        assert c.d["pos"].tolist()[:-1] == pos and c.d["slots"].tolist()[:-1] == slots
