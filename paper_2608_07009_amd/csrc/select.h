@@ -68,7 +68,6 @@ struct IndexShape {
 
 __device__ __forceinline__ float low_half(uint32_t x) { return __uint_as_float(x << 16); }
 __device__ __forceinline__ float high_half(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
-__device__ __forceinline__ float bf16_value(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // Candidates that the new token at position p sees.
 __device__ __forceinline__ int seen_at(const SelectArgs& a, int p) {
