@@ -776,7 +776,7 @@ typedef enum {
   HISPARSE_ROTARY_LINEAR = 1,  /* f / factor: positions of a longer context squeezed into the trained one */
   /* f * (s + (1 - s) / factor), s = (r - low_turns) / (high_turns - low_turns) held to [0, 1], r = the
    * turns that the pair makes over the trained context, original_tokens * f / (2 pi): fast pairs as they
-   * are, slow ones squeezed, a ramp between. */
+   * are, slow ones squeezed, a ramp between (over the turns; one over the pair's index is another). */
   HISPARSE_ROTARY_BY_PARTS = 2
 } hisparse_rotary_scaling_t;
 

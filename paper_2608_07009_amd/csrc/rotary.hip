@@ -103,7 +103,8 @@ __device__ __forceinline__ void wide_piece(const RowSet& r, const uint16_t* in, 
   *reinterpret_cast<any_u32x4*>(out + at + second) = y;
 }
 
-// One pair, or one of the other dims: rows whose parts are not whole pieces.
+// One pair, or one of the other dims: rows whose parts are not whole pieces. (16384 tokens of 40 heads of 126
+// dims: 212 us; of 128, in wide pieces, 65.)
 template <bool HALF>
 __device__ __forceinline__ void narrow_piece(const RowSet& r, const uint16_t* in, uint16_t* out,
                                              uint32_t piece, int pairs, const f32x2* cs) {

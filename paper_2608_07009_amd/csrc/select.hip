@@ -511,9 +511,9 @@ struct Rows32 {
 // time in LDS. The products of 32 candidates with one tile of queries run beside the sums of those before.
 // Norms of the rows, a tenth of the time where every workgroup works them out, are the request's, not a new
 // token's: the workgroup that has its last new token of this step, which sees most, has them for all.
-// 512 new tokens of 64 heads over 32768 keys: 262 us, 1.05 PFLOP/s of products, four fifths of the rate of a
-// large matrix product; the rest is the weighted sum, 32 vector instructions to 16 MFMAs, which run beside
-// each other only in part. (Measured: half of the waves moving candidates after their products instead of
+// 512 new tokens of 64 heads over 32768 keys: 253 to 284 us by the card, 0.97 to 1.09 PFLOP/s of products, three
+// quarters to four fifths of the rate of a large matrix product; the rest is the weighted sum, 32 vector
+// instructions to 16 MFMAs, which run beside each other only in part. (Measured: half of the waves moving candidates after their products instead of
 // before, 2 % slower in all; a wave priority for them, no gain.)
 template <int HEADS, int WAVES, int OCCUPANCY>
 __global__ __launch_bounds__(64 * WAVES, OCCUPANCY) void score_keys_kernel(SelectArgs a) {

@@ -5,7 +5,8 @@
 //   |s_j - exact| <= eps = 1.25 c A N,  A = sum_e |w_e| |q_e|, N = the largest |k_j| seen
 // (keys: sums of 128 products, each step off by at most 2^-23, and of the heads, 2^-24 a step and the
 // weight's product: c = 2^-16 + (heads + 1) 2^-24; the others: c = 2^-15, 256 products, their three parts and
-// what is left of q+ and q-, 2^-22, being less than the quarter added)
+// what is left of q+ and q-, 2^-22, being less than the quarter added; and a term for what is lost below the
+// normal range. Keys: none where a head's products may leave fp32, whatever its weight)
 // and with the m-th largest s in [lo, hi], candidates above hi + 2 eps are among the best m, those below
 // lo - 2 eps are not, and those between ("open") are scored again in 64 bits.
 //
@@ -13,7 +14,7 @@
 // is held in the registers of one workgroup, loaded once. Longer rows are cut down
 // first: narrow_kernel's workgroups add up the row's histogram, keep_kernel's write down the candidates
 // that its bin leaves in question or in, a part of the row each, and those few are chosen from. Rows
-// that neither way settles (thousands of open candidates, no error bound because of infinities) go over
+// that neither way settles (thousands of open candidates, no error bound) go over
 // their scores in memory as often as it takes (Stream).
 #include "select.h"
 

@@ -6,10 +6,10 @@
 // A wave owns a record of one kv head. A row of keys is 16 (bf16) or 8 (8-bit) lanes of 16 bytes, so the
 // wave takes 4 or 8 tokens at a time, four of those in flight. Its groups of lanes are joined at the end,
 // each step over half of the elements of the one before, so that 16 tokens' records are not mostly joining (all
-// elements at each step, through LDS: 8-bit bounds of 16 tokens 70 us, now 37.5). HBM-bound: the keys are
+// elements at each step, through LDS: 8-bit bounds of 16 tokens 70 us, now 36). HBM-bound: the keys are
 // read once (half of each record's bytes), one or two rows written. 4 prompts of 32768 tokens, 8 kv heads,
-// records of 64: bf16 268 MB of keys in 48 us, 5.6 TB/s; 8-bit 142 MB with the scales in 27 (means) and 31
-// (bounds). What single tokens write to, and few prompts, is a launch and a chain of loads: 3.7 us.
+// records of 64: bf16 268 MB of keys in 45 us (means) and 47 (bounds), 5.7 to 6 TB/s; 8-bit 142 MB with the
+// scales in 25 and 29. What single tokens write to, and few prompts, is a launch and a chain of loads: 3.7 us.
 //
 // Which records a wave has follows from the lengths alone: request q may own the waves from
 //   floor(start_q / t) + 2 q   on, of which it has floor(start_q+1 / t) - floor(start_q / t) + 2,
